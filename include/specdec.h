@@ -70,7 +70,8 @@ typedef enum {
                                      kernel waits for other blocks) */
 } specdec_status;
 
-enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1 };
+enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1,
+       SPECDEC_FP8 = 2 /* KV caches of bf16 models only, see specdec_kv_init_fp8 */ };
 /* Weight image formats of bf16 models (activations, KV and the LM head stay
  * bf16 in both): BF16 stores every matrix in bf16; INT4 stores the layer
  * matrices as 4-bit codes with one bf16 scale per row and group of 128
@@ -131,6 +132,7 @@ typedef struct {
   int32_t n_kv_heads, head_dim, dtype;
   int64_t len_upper;   /* host-side upper bound of max_b len[b] (kept by the library; a
                           caller may raise it before a graph capture) */
+  int32_t window;      /* SPECDEC_FP8 caches: positions of the bf16 ring (set and read for these alone) */
 } specdec_kv;
 
 /* ---------------------------------------------------------------- set-up */
@@ -219,15 +221,84 @@ SPECDEC_API int32_t specdec_kv_state_count(int32_t batch);
 SPECDEC_API specdec_status specdec_kv_init(specdec_kv* kv, const specdec_model* model, int32_t batch, int32_t capacity,
                                void* data, size_t data_bytes, int32_t* state, void* stream);
 
+/* The same for an 8-bit cache of a bf16 model (dtype SPECDEC_FP8): about half
+ * the bytes per position.  Every call that takes a specdec_kv takes one.
+ * Positions lie in blocks of 64.  The whole blocks a sequence has committed
+ * (positions below len / 64 * 64) are held as e4m3 codes with one scale 2^e
+ * per (layer, sequence, kv head, block, K or V), e the smallest integer with
+ * max|x| <= 448 * 2^e over the block's finite entries, e >= -100; code =
+ * x / 2^e rounded to the nearest e4m3 value, ties to even (NaN and infinities:
+ * NaN), and the value it stands for, code * 2^e, is exact in bf16 (for
+ * magnitudes below 2^127).  The newest positions (the incomplete block and
+ * rows not yet committed) are kept in bf16 in a ring of `window` positions; a
+ * block is rounded once, when a commit, prefill or specdec_kv_advance
+ * completes it, so drafted rows that are rolled back never change a code.
+ *  window: a multiple of 64, at least 128.  Verify, draft steps and commits
+ *    need gamma + 1 <= window - 63 (SHAPE otherwise), appends n <= window - 63;
+ *    prefill runs in chunks of at most window - 64 tokens per sequence.
+ *  capacity: a multiple of 64.  data: 256-byte aligned device memory, at least
+ *    specdec_kv_bytes_fp8 bytes, contents unspecified at first.
+ *  specdec_kv_set_state may set any length whose last len % 64 positions are
+ *    still in the ring: the last `window` positions written (by
+ *    specdec_kv_write_context, an append or a pass), less what was written
+ *    past them since.
+ * The cache needs the shape alone (desc, first n_layers_used layers), no model
+ * handle; a handle of the same n_kv_heads, head_dim and at most n_layers_used
+ * layers can use it.  Zeroes the state (asynchronous on stream).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (float32 desc). */
+SPECDEC_API size_t specdec_kv_bytes_fp8(const specdec_model_desc* desc, int32_t n_layers_used, int32_t batch,
+                                        int32_t capacity, int32_t window);
+SPECDEC_API specdec_status specdec_kv_init_fp8(specdec_kv* kv, const specdec_model_desc* desc, int32_t n_layers_used,
+                                               int32_t batch, int32_t capacity, int32_t window, void* data,
+                                               size_t data_bytes, int32_t* state, void* stream);
+
 /* Install K and V rows for sequence b, layer `layer`, positions [pos0, pos0+n):
  * k, v are device arrays [n, n_kv_heads, head_dim] of the storage type (K
  * after RoPE, as a forward pass would have stored it).  Used to set up a
- * resident context without prefill.  Asynchronous. */
+ * resident context without prefill.  Asynchronous.
+ * FP8 caches: k, v are bf16; pos0 must be a multiple of 64 (SHAPE otherwise).
+ * The blocks that end inside the range are quantized, and its last `window`
+ * rows go to the ring as well, so a following specdec_kv_set_state may set
+ * len to pos0 + n (or up to window - 63 positions less). */
 SPECDEC_API specdec_status specdec_kv_write_context(specdec_kv* kv, int32_t layer, int32_t b, int32_t pos0, int32_t n,
                                         const void* k, const void* v, void* stream);
-/* Copy K and V rows back out (same layout as specdec_kv_write_context). */
+/* Copy K and V rows back out (same layout as specdec_kv_write_context).  FP8
+ * caches: bf16 values, below len / 64 * 64 those the codes stand for, from
+ * there on the ring's (positions the ring holds). */
 SPECDEC_API specdec_status specdec_kv_read_context(const specdec_kv* kv, int32_t layer, int32_t b, int32_t pos0, int32_t n,
                                        void* k, void* v, void* stream);
+
+/* For a caller that runs its own model over an FP8 cache (FP8 caches only,
+ * UNSUPPORTED otherwise): one step of n new tokens per sequence is, per layer,
+ * specdec_kv_append and specdec_attention, then specdec_kv_advance once.
+ * append: k, v device bf16 [batch, n, n_kv_heads, head_dim] (K after RoPE) as
+ *   positions len[b] .. len[b]+n-1 of `layer`, not committed (a further append
+ *   before the advance overwrites them).
+ * advance: len[b] += n for every sequence; the blocks this completes are
+ *   quantized in every layer.  Pending tokens and the commit counter stay.
+ * Asynchronous.  Errors: INVALID_ARG, UNSUPPORTED, SHAPE (n > window - 63),
+ * KV_CAPACITY (len_upper + n > capacity). */
+SPECDEC_API specdec_status specdec_kv_append(specdec_kv* kv, int32_t layer, int32_t n, const void* k, const void* v,
+                                             void* stream);
+SPECDEC_API specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* stream);
+
+/* Grouped-query attention of the newest n rows of every sequence over one
+ * layer of an FP8 cache: q [batch, n, n_heads, head_dim] float32 (after RoPE),
+ * row i of sequence b at position len[b] + i, seeing keys 0 .. len[b]+i (the
+ * last ones appended, not committed); query head h reads kv head
+ * h / (n_heads / n_kv_heads).  out, same shape, float32:
+ * softmax(q k^T / sqrt(head_dim)) v, the sums in float32.  A key or value row
+ * with a NaN or infinity affects the rows that see it and no others.
+ * workspace: specdec_attention_workspace_bytes bytes (0 for arguments the call
+ * rejects), 256-byte aligned, dead after the call; calls that share one must be
+ * ordered on one stream (graphs captured with one, replayed in order).
+ * Graph capture: sized from kv->len_upper, as the passes are (see above).
+ * Asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (other caches), SHAPE
+ * (n_heads not a multiple of n_kv_heads, n > window - 63), KV_CAPACITY. */
+SPECDEC_API size_t specdec_attention_workspace_bytes(const specdec_kv* kv, int32_t n_heads, int32_t n);
+SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_heads, int32_t n,
+                                             const float* q, float* out, void* workspace, size_t workspace_bytes,
+                                             void* stream);
 
 /* Set lengths and pending tokens from HOST arrays: len[B], pending[2B]
  * (right-aligned: pending[2b+1] is the newest token), n_pending[B] in {1,2}.
@@ -415,6 +486,52 @@ SPECDEC_API specdec_status specdec_event_query(void* event, int32_t* done);
 SPECDEC_API specdec_status specdec_sample(int32_t batch, int32_t vocab, const float* probs, int64_t ld, const uint32_t* rand,
                               uint64_t seed, uint64_t step, int32_t purpose, int32_t index, int32_t* out,
                               void* stream);
+
+/* Sampling rules of a batch of requests: device arrays of `batch` entries, one
+ * per sequence, each optional (NULL: the rule is off for all). */
+typedef struct {
+  const float* temperature; /* NULL: 1; 0: greedy (argmax, lowest index on ties) */
+  const int32_t* top_k;     /* <= 0: off */
+  const float* top_p;       /* >= 1: off; <= 0: the most likely token alone */
+  const float* min_p;       /* <= 0: off; above 1 counts as 1 */
+} specdec_sampling;
+
+/* The distribution a request's rules leave, and a token drawn from it, for
+ * `rows` rows of logits per sequence: row (b, i) at logits + (b*rows + i)*ld
+ * (first `vocab` entries used; -inf marks a token that may not be drawn).
+ * With m = max l and e_j = exp((l_j - m) / T) (float64), W_j = floor(e_j 2^43):
+ *  - min_p: tokens with e_j >= min_p (a share of the most likely token's
+ *    probability) are candidates, in the order of falling l_j, the lower index
+ *    first on ties;
+ *  - top_k: the first top_k of them;
+ *  - top_p: of these the shortest prefix whose mass (sum of W) is at least
+ *    max(1, ceil(top_p * mass of the top_k)).
+ * probs (optional, row (b, i) at probs + (b*rows + i)*ld_probs):
+ *   fl32(e_j 2^43 / mass of the kept) for kept tokens, 0 elsewhere (greedy: 1
+ *   for the argmax).  May not overlap logits.
+ * out (optional, entry (b, i) at out + (b*rows + i)*ld_out): the fixed-point
+ *   draw of specdec_sample from those probabilities with the 32-bit word
+ *   rand[b*rows + i], or, rand == NULL, Philox(seed, b, step, purpose, index + i)
+ *   (step_dev: as for specdec_draft_step).
+ * Decisions are made on integer masses of float64 exponentials, so they do not
+ * depend on how sums are split.  The accept rule takes such rows as p
+ * (SPECDEC_INPUT_PROBS, temperature 1) and q.
+ * A row with a NaN or +inf, without a finite entry, or with a NaN rule or a
+ * negative temperature sets *status = SPECDEC_ERR_NONFINITE (device int32,
+ * sticky, may be NULL) and writes NaN to probs and -1 to out (an accept over
+ * such a row then fails for its sequence, and the commit leaves it alone).
+ * workspace: specdec_sample_logits_workspace_bytes bytes (0 for sizes the call
+ * rejects), 256-byte aligned, needs no initialisation, dead after the call;
+ * calls that share one must be ordered on one stream.
+ * Asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (vocab above 2^20, batch *
+ * rows above 65535), HIP. */
+SPECDEC_API size_t specdec_sample_logits_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab);
+SPECDEC_API specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab, const float* logits,
+                                                 int64_t ld, const specdec_sampling* rules, const uint32_t* rand,
+                                                 uint64_t seed, uint64_t step, const uint64_t* step_dev,
+                                                 int32_t purpose, int32_t index, float* probs, int64_t ld_probs,
+                                                 int32_t* out, int64_t ld_out, int32_t* status, void* workspace,
+                                                 size_t workspace_bytes, void* stream);
 
 /* Philox4x32-10 (Salmon et al., SC'11) word 0 for each b in [0, batch):
  * key = (seed & 0xffffffff, seed >> 32),

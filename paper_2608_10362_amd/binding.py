@@ -18,7 +18,7 @@ import numpy as np
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecdec.so")
 
-SPECDEC_F32, SPECDEC_BF16 = 0, 1
+SPECDEC_F32, SPECDEC_BF16, SPECDEC_FP8 = 0, 1, 2
 ROLE_TARGET, ROLE_DRAFT = 0, 1
 INPUT_PROBS, INPUT_LOGITS = 0, 1
 PURPOSE_DRAFT, PURPOSE_ACCEPT, PURPOSE_RESAMPLE = 0, 1, 2
@@ -59,7 +59,13 @@ class Weights(ctypes.Structure):
 class KV(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("state", ctypes.c_void_p), ("batch", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("len_upper", ctypes.c_int64)]
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("len_upper", ctypes.c_int64),
+                ("window", ctypes.c_int32)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
 
 
 _lib = None
@@ -125,6 +131,25 @@ _SIGS = {
     "specdec_sample": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
                                       ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int32,
                                       ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
+    "specdec_kv_bytes_fp8": (ctypes.c_size_t, [ctypes.POINTER(ModelDesc), ctypes.c_int32, ctypes.c_int32,
+                                               ctypes.c_int32, ctypes.c_int32]),
+    "specdec_kv_init_fp8": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.POINTER(ModelDesc), ctypes.c_int32,
+                                           ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]),
+    "specdec_kv_append": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_void_p]),
+    "specdec_kv_advance": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_void_p]),
+    "specdec_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32]),
+    "specdec_attention": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                         ctypes.c_void_p]),
+    "specdec_sample_logits_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "specdec_sample_logits": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                             ctypes.c_int64, ctypes.POINTER(Sampling), ctypes.c_void_p,
+                                             ctypes.c_uint64, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_int32,
+                                             ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                             ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                             ctypes.c_void_p]),
     "specdec_draw_u32": (ctypes.c_int, [ctypes.c_int32, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int32,
                                         ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
     "specdec_device_status": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_void_p, ctypes.c_void_p]),
@@ -285,6 +310,7 @@ class Model:
         self.dw = dw
         self.shape = dw.shape
         self.n_layers = n_layers
+        self.max_rows = max_rows
         self.desc = make_desc(dw.shape.with_layers(dw.n_layers))
         nbytes = lib().specdec_workspace_bytes(ctypes.byref(self.desc), max_rows, max_ctx)
         if nbytes == 0:
@@ -328,8 +354,9 @@ class KVCache:
         return self.kv.batch
 
     def storage_dtype(self):
+        """Type of the K and V rows that go in and out (FP8 caches: bf16)."""
         import torch
-        return torch.bfloat16 if self.kv.dtype == SPECDEC_BF16 else torch.float32
+        return torch.float32 if self.kv.dtype == SPECDEC_F32 else torch.bfloat16
 
     def write_context(self, layer: int, b: int, pos0: int, k, v, stream=None):
         n = k.shape[0]
@@ -372,6 +399,37 @@ class KVCache:
         """The commit counter's value (synchronizes the current stream)."""
         B = self.batch
         return int(self.state[4 * B + 2:4 * B + 4].cpu().numpy().view(np.uint64)[0])
+
+
+class Fp8KVCache(KVCache):
+    """An 8-bit cache (see specdec_kv_init_fp8): takes the place of a KVCache of
+    a bf16 model in every call, or serves a caller's own model through
+    specdec_kv_append, specdec_attention and specdec_kv_advance.  ``of``: the
+    Model that uses it, or a model shape (then ``n_layers`` of it).  ``window``:
+    positions of the bf16 ring, by default 128 and what the handle's rows fill."""
+
+    def __init__(self, of, batch: int, capacity: int, window: Optional[int] = None, n_layers: Optional[int] = None,
+                 device="cuda", stream=None):
+        import torch
+        self.model = of if isinstance(of, Model) else None
+        if self.model is not None:
+            desc, device = of.desc, of.workspace.device
+            n_layers = of.n_layers if n_layers is None else n_layers
+        else:
+            desc = make_desc(of)
+            n_layers = of.n_layers if n_layers is None else n_layers
+        if window is None:
+            rows = of.max_rows // batch if self.model is not None else 0
+            window = max(128, (rows + 64 + 63) // 64 * 64)
+        nbytes = lib().specdec_kv_bytes_fp8(ctypes.byref(desc), n_layers, batch, capacity, window)
+        if nbytes == 0:
+            raise SpecdecError(-2, "specdec_kv_bytes_fp8")
+        self.data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.state = torch.zeros(lib().specdec_kv_state_count(batch), dtype=torch.int32, device=device)
+        self.kv = KV()
+        _check(lib().specdec_kv_init_fp8(ctypes.byref(self.kv), ctypes.byref(desc), n_layers, batch, capacity, window,
+                                         self.data.data_ptr(), nbytes, self.state.data_ptr(), _stream(stream)),
+               "specdec_kv_init_fp8")
 
 
 # ---------------------------------------------------------------- draft reload
@@ -453,6 +511,50 @@ def specdec_prefill(model: Model, kv: KVCache, tokens, stream=None):
         raise ValueError("tokens: expected [batch, n]")
     _check(lib().specdec_prefill(model.handle, ctypes.byref(kv.kv), tokens.shape[1], tokens.data_ptr(),
                                  _stream(stream)), "specdec_prefill")
+
+
+def specdec_kv_append(kv: KVCache, layer: int, k, v, stream=None):
+    """k, v: device bf16 [batch, n, n_kv_heads, head_dim]."""
+    import torch
+    shp = (kv.batch, k.shape[1] if k.dim() == 4 else 0, kv.kv.n_kv_heads, kv.kv.head_dim)
+    for name, t in (("k", k), ("v", v)):
+        _on_current(t, name, torch.bfloat16)
+        if tuple(t.shape) != shp or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous [batch, n, {shp[2]}, {shp[3]}] tensor of one shape")
+    _check(lib().specdec_kv_append(ctypes.byref(kv.kv), layer, shp[1], k.data_ptr(), v.data_ptr(), _stream(stream)),
+           "specdec_kv_append")
+
+
+def specdec_kv_advance(kv: KVCache, n: int, stream=None):
+    _check(lib().specdec_kv_advance(ctypes.byref(kv.kv), n, _stream(stream)), "specdec_kv_advance")
+
+
+def attention_workspace(kv: KVCache, n_heads: int, n: int):
+    """A device buffer large enough for specdec_attention's workspace."""
+    import torch
+    nbytes = lib().specdec_attention_workspace_bytes(ctypes.byref(kv.kv), n_heads, n)
+    if nbytes == 0:
+        raise ValueError("specdec_attention does not support this cache or these sizes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=kv.data.device)
+
+
+def specdec_attention(kv: KVCache, layer: int, q, out, workspace=None, stream=None):
+    """q, out: device float32 [batch, n, n_heads, head_dim].  `workspace` (from
+    attention_workspace) is allocated per call when not given."""
+    import torch
+    if q.dim() != 4 or q.shape[0] != kv.batch or q.shape[3] != kv.kv.head_dim or out.shape != q.shape:
+        raise ValueError("q, out: expected [batch, n, n_heads, head_dim]")
+    for name, t in (("q", q), ("out", out)):
+        _on_current(t, name, torch.float32)
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
+    n, n_heads = q.shape[1], q.shape[2]
+    if workspace is None:
+        workspace = attention_workspace(kv, n_heads, n)
+    _dev(workspace, "workspace", torch.uint8, 1)
+    _same_device(workspace, "workspace", q)
+    _check(lib().specdec_attention(ctypes.byref(kv.kv), layer, n_heads, n, q.data_ptr(), out.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel(), _stream(stream)), "specdec_attention")
 
 
 def specdec_draft_step(draft: Model, kv: KVCache, gamma: int, slot: int, temperature: float, seed: int, step: int,
@@ -565,6 +667,114 @@ def specdec_sample(probs, rand, seed: int, step: int, purpose: int, index: int, 
                                 out.data_ptr(), _stream(stream)), "specdec_sample")
 
 
+class SamplingRules:
+    """Per-sequence sampling rules (see specdec_sampling): device tensors of one
+    entry per sequence, float32 (top_k: int32), or None where a rule is off."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        import torch
+        given = {"temperature": temperature, "top_k": top_k, "top_p": top_p, "min_p": min_p}
+        self.tensors = {k: t for k, t in given.items() if t is not None}
+        sizes = set()
+        for k, t in self.tensors.items():
+            _dev(t, k, torch.int32 if k == "top_k" else torch.float32, 1)
+            sizes.add(t.numel())
+        if len(sizes) > 1:
+            raise ValueError("rules: one entry per sequence in each tensor")
+        self.batch = sizes.pop() if sizes else None
+        self.c = Sampling(*[_ptr(given[k]) for k in ("temperature", "top_k", "top_p", "min_p")])
+
+
+def sample_workspace(batch: int, rows: int, vocab: int, device="cuda"):
+    """A device buffer large enough for specdec_sample_logits' workspace."""
+    import torch
+    n = lib().specdec_sample_logits_workspace_bytes(batch, rows, vocab)
+    if n == 0:
+        raise ValueError("specdec_sample_logits does not support these sizes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def specdec_sample_logits(logits, rules: Optional[SamplingRules] = None, rand=None, seed: int = 0, step: int = 0,
+                          purpose: int = PURPOSE_RESAMPLE, index: int = 0, probs=None, out=None, status=None,
+                          workspace=None, stream=None, step_dev=None):
+    """logits [batch, rows, vocab] or [batch, vocab] float32; probs: the same
+    shape; out: int32 [batch, rows].  probs and out may be strided over their
+    leading dimensions (a slot of a larger buffer) if one stride covers them.
+    `workspace` is allocated per call when not given."""
+    import torch
+    _on_current(logits, "logits", torch.float32)
+    if logits.dim() not in (2, 3):
+        raise ValueError("logits: expected [batch, rows, vocab] or [batch, vocab]")
+    batch, vocab = logits.shape[0], logits.shape[-1]
+    rows = logits.shape[1] if logits.dim() == 3 else 1
+    ld = _row_stride(logits, "logits", vocab)
+    if rules is not None:
+        if rules.batch is not None and rules.batch != batch:
+            raise ValueError(f"rules: {rules.batch} entries for a batch of {batch}")
+        for k, t in rules.tensors.items():
+            _same_device(t, k, logits)
+    if rand is not None:
+        _dev(rand, "rand", None, batch * rows)
+        if rand.dtype not in (torch.int32, torch.uint32):
+            raise ValueError("rand: expected 32-bit words")
+        _same_device(rand, "rand", logits)
+    ld_probs = ld_out = 0
+    if probs is not None:
+        if probs.shape != logits.shape:
+            raise ValueError("probs: expected the shape of logits")
+        _on_current(probs, "probs", torch.float32)
+        ld_probs = _row_stride(probs, "probs", vocab)
+    if out is not None:
+        if out.numel() != batch * rows:
+            raise ValueError("out: expected one entry per row")
+        _on_current(out, "out", torch.int32)
+        ld_out = _row_stride(out.reshape(batch, rows, 1) if out.is_contiguous() else out.unsqueeze(-1), "out", 1)
+    if status is not None:
+        _dev(status, "status", torch.int32, 1)
+        _same_device(status, "status", logits)
+    if workspace is None:
+        workspace = sample_workspace(batch, rows, vocab, logits.device)
+    _dev(workspace, "workspace", torch.uint8, 1)
+    _same_device(workspace, "workspace", logits)
+    _check(lib().specdec_sample_logits(batch, rows, vocab, logits.data_ptr(), ld,
+                                       None if rules is None else ctypes.byref(rules.c), _ptr(rand), seed, step,
+                                       step_dev, purpose, index, _ptr(probs), ld_probs, _ptr(out), ld_out,
+                                       _ptr(status), workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "specdec_sample_logits")
+
+
+def _on_current(t, name: str, dtype):
+    """Check a tensor argument's type, and that it is on the current device (where the call launches)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name}: expected a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _same_device(t, name: str, other):
+    if t.device != other.device:
+        raise ValueError(f"{name}: on {t.device}, expected {other.device}")
+
+
+def _row_stride(t, name: str, width: int) -> int:
+    """The one stride between the rows of t [batch, rows, width] (or [batch, width])."""
+    if width > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    lead = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+    if not lead:
+        return width
+    ld = lead[-1][1]
+    for (_, s), (n1, s1) in zip(lead[:-1], lead[1:]):
+        if s != n1 * s1:
+            raise ValueError(f"{name}: rows need one stride")
+    if ld < width:
+        raise ValueError(f"{name}: rows overlap")
+    return ld
+
+
 def specdec_draw_u32(batch: int, seed: int, step: int, purpose: int, index: int, out, stream=None):
     _dev(out, "out", out.dtype if out is not None else None, batch)
     if out.element_size() != 4:
@@ -624,10 +834,15 @@ class SpecDecoder:
     the device.  With device_step the Philox step of every draw is the target
     cache's commit counter, read on the device (the `step` arguments below are
     then ignored), so a captured iteration draws fresh words on each replay.
+    With ``rules`` (per-sequence SamplingRules, one entry per sequence; their
+    temperatures take the place of ``temperature``) the draft proposes from the
+    distribution the rules leave of its logits, and the accept tests it against
+    the one they leave of the target's: the emitted tokens are distributed as
+    sampling from the target under the rules.
     """
 
     def __init__(self, target: Model, draft: Model, kv_t: KVCache, kv_d: KVCache, gamma: int,
-                 temperature: float, seed: int, device_step: bool = False):
+                 temperature: float, seed: int, device_step: bool = False, rules: Optional[SamplingRules] = None):
         import torch
         self.target, self.draft, self.kv_t, self.kv_d = target, draft, kv_t, kv_d
         self.gamma, self.temperature, self.seed = gamma, temperature, seed
@@ -636,21 +851,41 @@ class SpecDecoder:
         dev = kv_t.data.device
         self.B, self.V = B, V
         self.d = torch.zeros((B, gamma), dtype=torch.int32, device=dev)
-        self.q = torch.zeros((B, gamma, V), dtype=torch.float32, device=dev) if temperature > 0 else None
+        self.rules = rules
+        if rules is not None and rules.batch not in (None, B):
+            raise ValueError(f"rules: {rules.batch} entries for a batch of {B}")
+        sampled = temperature > 0 or rules is not None
+        self.q = torch.zeros((B, gamma, V), dtype=torch.float32, device=dev) if sampled else None
         self.logits = torch.empty((B, gamma + 1, V), dtype=torch.float32, device=dev)
         self.n_acc = torch.zeros(B, dtype=torch.int32, device=dev)
         self.next = torch.zeros(B, dtype=torch.int32, device=dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.accept_ws = accept_workspace(B, gamma, V, dev)
+        if rules is not None:
+            self.p = torch.empty((B, gamma + 1, V), dtype=torch.float32, device=dev)
+            self.draft_logits = torch.empty((B, V), dtype=torch.float32, device=dev)
+            self.rules_ws = sample_workspace(B, gamma + 1, V, dev)
 
     def draft_phase(self, step: int, stream=None):
         for s in range(self.gamma):
+            if self.rules is not None:
+                specdec_draft_step(self.draft, self.kv_d, self.gamma, s, 0.0, self.seed, step, None, None, self.d,
+                                   self.gamma, self.draft_logits, stream, step_dev=self.step_dev)
+                specdec_sample_logits(self.draft_logits, self.rules, seed=self.seed, step=step, purpose=PURPOSE_DRAFT,
+                                      index=s, probs=self.q[:, s], out=self.d[:, s], status=self.status,
+                                      workspace=self.rules_ws, stream=stream, step_dev=self.step_dev)
+                continue
             specdec_draft_step(self.draft, self.kv_d, self.gamma, s, self.temperature, self.seed, step, None, self.q,
                                self.d, self.gamma, None, stream, step_dev=self.step_dev)
 
     def verify_phase(self, step: int, stream=None):
         specdec_verify(self.target, self.kv_t, self.gamma, self.d, self.gamma, self.logits, stream)
-        specdec_accept(self.B, self.gamma, self.V, INPUT_LOGITS, self.temperature, self.logits, self.q, self.d,
+        kind, temperature, scores = INPUT_LOGITS, self.temperature, self.logits
+        if self.rules is not None:
+            specdec_sample_logits(self.logits, self.rules, probs=self.p, status=self.status, workspace=self.rules_ws,
+                                  stream=stream)
+            kind, temperature, scores = INPUT_PROBS, 1.0, self.p
+        specdec_accept(self.B, self.gamma, self.V, kind, temperature, scores, self.q, self.d,
                        self.gamma, None, self.seed, step, self.n_acc, self.next, self.status, self.accept_ws, stream,
                        step_dev=self.step_dev)
 

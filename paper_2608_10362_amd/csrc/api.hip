@@ -23,6 +23,7 @@ struct specdec_model {
   std::vector<const uint16_t*> sq, sk, sv, so, sg, su, sd;  // ... and these their group scales
   // workspace carve
   RowDesc* rows;
+  RowDesc* rows_kv;  // FP8 caches: rows, each at its slot of the ring
   float* rope_cs;
   float* h;
   float* xg;
@@ -100,7 +101,7 @@ int elem_bytes(int dtype) { return dtype == SPECDEC_BF16 ? 2 : 4; }
 
 // Workspace layout (in order); shared by specdec_workspace_bytes and create.
 struct WsLayout {
-  size_t rows, rope, h, xg, ss, qkv, qr, o_part, ml_part, o, u, logits, samp, xs_d, xs_f, ypart, cnt, total;
+  size_t rows, rows_kv, rope, h, xg, ss, qkv, qr, o_part, ml_part, o, u, logits, samp, xs_d, xs_f, ypart, cnt, total;
   int ss_parts, chunk, n_split;
   size_t ypart_floats;
 };
@@ -119,6 +120,7 @@ WsLayout ws_layout(const specdec_model_desc* d, int max_rows, int max_ctx) {
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t at = off; off = align_up(off + bytes); return at; };
   w.rows = take(R * sizeof(RowDesc));
+  w.rows_kv = take(d->dtype == SPECDEC_BF16 ? R * sizeof(RowDesc) : 0);
   w.rope = take(R * hd * 4);
   w.h = take(R * d->d_model * 4);
   // (bf16 passes of more than 16 rows hand x over in the stacked operands only)
@@ -242,11 +244,37 @@ KvLayout kv_layout(const specdec_kv* kv) {
   return KvLayout{kv->data, kv->batch, kv->capacity, kv->n_kv_heads, kv->head_dim, kv->dtype};
 }
 
+bool is_fp8(const specdec_kv* kv) { return kv->dtype == SPECDEC_FP8; }
+Kv8Layout kv8_of(const specdec_kv* kv) {
+  return kv8_layout(kv->data, kv->state, kv->n_layers, kv->batch, kv->n_kv_heads, kv->head_dim, kv->capacity,
+                    kv->window);
+}
+// Rows a sequence may have in the ring past its sealed blocks' end (FP8 caches):
+// up to 63 committed ones, and n new ones.
+bool ring_holds(const specdec_kv* kv, int64_t n) { return !is_fp8(kv) || n <= kv->window - (kF8Block - 1); }
+
 specdec_status check_kv(const specdec_model* m, const specdec_kv* kv) {
   if (!m || !kv || !kv->data || !kv->state) return SPECDEC_ERR_INVALID_ARG;
   if (kv->n_layers < m->n_layers || kv->n_kv_heads != m->desc.n_kv_heads || kv->head_dim != m->desc.head_dim ||
-      kv->dtype != m->desc.dtype)
+      (is_fp8(kv) ? m->desc.dtype != SPECDEC_BF16 : kv->dtype != m->desc.dtype))
     return SPECDEC_ERR_SHAPE;
+  return SPECDEC_OK;
+}
+
+specdec_status check_fp8(const specdec_model_desc* d, int n_layers, int batch, int capacity, int window) {
+  const specdec_status st = check_desc(d);
+  if (st != SPECDEC_OK) return st;
+  if (n_layers <= 0 || n_layers > d->n_layers || batch <= 0 || capacity <= 0 || window <= 0)
+    return SPECDEC_ERR_INVALID_ARG;
+  if (d->dtype != SPECDEC_BF16) return SPECDEC_ERR_UNSUPPORTED;
+  if (capacity % kF8Block || window % kF8Block || window < 2 * kF8Block) return SPECDEC_ERR_SHAPE;
+  return SPECDEC_OK;
+}
+
+specdec_status check_attention(const specdec_kv* kv, int n_heads, int n) {
+  if (!kv || !kv->data || !kv->state || n_heads <= 0 || n <= 0) return SPECDEC_ERR_INVALID_ARG;
+  if (!is_fp8(kv)) return SPECDEC_ERR_UNSUPPORTED;
+  if (n_heads % kv->n_kv_heads || !ring_holds(kv, n) || n > kv->capacity) return SPECDEC_ERR_SHAPE;
   return SPECDEC_OK;
 }
 
@@ -303,6 +331,8 @@ specdec_status forward(const specdec_model* m, specdec_kv* kv, RowsArgs ra, int 
   ra.gain = m->attn_norm[0];
   ra.xg = m->xg;
   ra.rows = m->rows;
+  ra.rows_kv = is_fp8(kv) ? m->rows_kv : nullptr;
+  ra.window = is_fp8(kv) ? kv->window : 1;
   ra.rope_cs = m->rope_cs;
   ra.h = m->h;
   ra.ss = m->ss;
@@ -367,6 +397,10 @@ specdec_status forward(const specdec_model* m, specdec_kv* kv, RowsArgs ra, int 
   at.counters = m->attn_cnt;
   at.xs = stk ? m->xs_f : nullptr;
   at.stt = stt;
+  if (is_fp8(kv)) {
+    at.f8 = kv8_of(kv);
+    at.c0 = ra.mode == ROWS_PREFILL ? ra.c0 : 0;  // (the chunks before this one are sealed as they end)
+  }
 
   for (int l = 0; l < m->n_layers; ++l) {
     const bool last_kv = kv_only && l + 1 == m->n_layers;
@@ -379,6 +413,7 @@ specdec_status forward(const specdec_model* m, specdec_kv* kv, RowsArgs ra, int 
     if (dt == SPECDEC_BF16) {  // RoPE, the query store and the KV append run in the GEMM epilogue
       q.kind = EPI_QKV;
       q.rows = m->rows; q.rope_cs = m->rope_cs; q.qr = m->qr; q.kv = kv_layout(kv); q.layer = l;
+      if (is_fp8(kv)) { q.rows = m->rows_kv; q.kv = at.f8.ring; }
       q.n_heads = H; q.n_kv_heads = G; q.head_dim = hd;
     }
     if (q4) { q.q4 = 1; q.wscale[0] = m->sq[l]; q.wscale[1] = m->sk[l]; q.wscale[2] = m->sv[l]; }
@@ -622,6 +657,7 @@ specdec_status specdec_model_create_fmt(const specdec_model_desc* desc, const sp
   }
   char* base = (char*)workspace;
   m->rows = (RowDesc*)(base + L.rows);
+  m->rows_kv = (RowDesc*)(base + L.rows_kv);
   m->rope_cs = (float*)(base + L.rope);
   m->h = (float*)(base + L.h);
   m->xg = (float*)(base + L.xg);
@@ -675,12 +711,99 @@ specdec_status specdec_kv_init(specdec_kv* kv, const specdec_model* model, int32
   return hip_status(hipMemsetAsync(state, 0, sizeof(int32_t) * specdec_kv_state_count(batch), (hipStream_t)stream));
 }
 
+size_t specdec_kv_bytes_fp8(const specdec_model_desc* desc, int32_t n_layers_used, int32_t batch, int32_t capacity,
+                            int32_t window) {
+  if (check_fp8(desc, n_layers_used, batch, capacity, window) != SPECDEC_OK) return 0;
+  return kv8_bytes(n_layers_used, batch, desc->n_kv_heads, desc->head_dim, capacity, window);
+}
+
+specdec_status specdec_kv_init_fp8(specdec_kv* kv, const specdec_model_desc* desc, int32_t n_layers_used, int32_t batch,
+                                   int32_t capacity, int32_t window, void* data, size_t data_bytes, int32_t* state,
+                                   void* stream) {
+  if (!kv || !data || !state || misaligned8(state) || (uintptr_t)data % kAlign) return SPECDEC_ERR_INVALID_ARG;
+  const specdec_status st = check_fp8(desc, n_layers_used, batch, capacity, window);
+  if (st != SPECDEC_OK) return st;
+  if (data_bytes < kv8_bytes(n_layers_used, batch, desc->n_kv_heads, desc->head_dim, capacity, window))
+    return SPECDEC_ERR_INVALID_ARG;
+  kv->data = data;
+  kv->state = state;
+  kv->batch = batch;
+  kv->capacity = capacity;
+  kv->n_layers = n_layers_used;
+  kv->n_kv_heads = desc->n_kv_heads;
+  kv->head_dim = desc->head_dim;
+  kv->dtype = SPECDEC_FP8;
+  kv->window = window;
+  kv->len_upper = 0;
+  return hip_status(launch_fill_u32((uint32_t*)state, (size_t)specdec_kv_state_count(batch), 0u, (hipStream_t)stream));
+}
+
+specdec_status specdec_kv_append(specdec_kv* kv, int32_t layer, int32_t n, const void* k, const void* v, void* stream) {
+  if (!kv || !kv->data || !kv->state || !k || !v || layer < 0 || layer >= kv->n_layers || n <= 0)
+    return SPECDEC_ERR_INVALID_ARG;
+  if (!is_fp8(kv)) return SPECDEC_ERR_UNSUPPORTED;
+  if (!ring_holds(kv, n)) return SPECDEC_ERR_SHAPE;
+  if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  return hip_status(launch_kv8_append(kv8_of(kv), layer, n, k, v, kv_status(kv), kv->capacity, (hipStream_t)stream));
+}
+
+specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* stream) {
+  if (!kv || !kv->data || !kv->state || n <= 0) return SPECDEC_ERR_INVALID_ARG;
+  if (!is_fp8(kv)) return SPECDEC_ERR_UNSUPPORTED;
+  if (!ring_holds(kv, n)) return SPECDEC_ERR_SHAPE;
+  if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  hipStream_t s = (hipStream_t)stream;
+  SD_TRY(launch_kv8_seal(kv8_of(kv), kv->n_layers, 0, n, nullptr, s));
+  SD_TRY(launch_kv_advance(kv->batch, n, kv_len(kv), s));
+  kv->len_upper += n;
+  return SPECDEC_OK;
+}
+
+size_t specdec_attention_workspace_bytes(const specdec_kv* kv, int32_t n_heads, int32_t n) {
+  if (check_attention(kv, n_heads, n) != SPECDEC_OK) return 0;
+  const size_t parts = (size_t)attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->capacity);
+  const size_t slots = (size_t)kv->batch * n * n_heads * parts;
+  return align_up(slots * kv->head_dim * 4) + align_up(slots * 2 * 4);
+}
+
+specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_heads, int32_t n, const float* q,
+                                 float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const specdec_status st = check_attention(kv, n_heads, n);
+  if (st != SPECDEC_OK) return st;
+  if (!q || !out || layer < 0 || layer >= kv->n_layers || !workspace || (uintptr_t)workspace % kAlign ||
+      workspace_bytes < specdec_attention_workspace_bytes(kv, n_heads, n))
+    return SPECDEC_ERR_INVALID_ARG;
+  if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  AttnArgs a{};
+  a.M = kv->batch * n;
+  a.rps = n;
+  a.n_heads = n_heads;
+  a.n_kv_heads = kv->n_kv_heads;
+  a.head_dim = kv->head_dim;
+  a.qr = const_cast<float*>(q);
+  a.kv = kv_layout(kv);
+  a.layer = layer;
+  a.max_ctx = (int)kv->len_upper + n;
+  a.n_split = attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->capacity);
+  a.o_part = (float*)workspace;
+  a.ml_part = (float*)((char*)workspace + align_up((size_t)a.M * n_heads * a.n_split * kv->head_dim * 4));
+  a.o = out;
+  a.status = kv_status(kv);
+  a.f8 = kv8_of(kv);
+  Timed t(SPECDEC_KERNEL_ATTENTION, (hipStream_t)stream);
+  return hip_status(launch_attention8(a, (hipStream_t)stream));
+}
+
 specdec_status specdec_kv_write_context(specdec_kv* kv, int32_t layer, int32_t b, int32_t pos0, int32_t n,
                                         const void* k, const void* v, void* stream) {
   if (!kv || !kv->data || !k || !v || layer < 0 || layer >= kv->n_layers || b < 0 || b >= kv->batch || pos0 < 0 ||
       n < 0)
     return SPECDEC_ERR_INVALID_ARG;
-  if (pos0 + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  if (n > kv->capacity - pos0) return SPECDEC_ERR_KV_CAPACITY;
+  if (is_fp8(kv)) {
+    if (pos0 % kF8Block) return SPECDEC_ERR_SHAPE;
+    return hip_status(launch_kv8_write(kv8_of(kv), layer, b, pos0, n, k, v, (hipStream_t)stream));
+  }
   return hip_status(launch_kv_copy(kv_layout(kv), layer, b, pos0, n, k, v, nullptr, nullptr, (hipStream_t)stream));
 }
 
@@ -689,7 +812,8 @@ specdec_status specdec_kv_read_context(const specdec_kv* kv, int32_t layer, int3
   if (!kv || !kv->data || !k || !v || layer < 0 || layer >= kv->n_layers || b < 0 || b >= kv->batch || pos0 < 0 ||
       n < 0)
     return SPECDEC_ERR_INVALID_ARG;
-  if (pos0 + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  if (n > kv->capacity - pos0) return SPECDEC_ERR_KV_CAPACITY;
+  if (is_fp8(kv)) return hip_status(launch_kv8_read(kv8_of(kv), layer, b, pos0, n, k, v, (hipStream_t)stream));
   return hip_status(launch_kv_copy(kv_layout(kv), layer, b, pos0, n, nullptr, nullptr, k, v, (hipStream_t)stream));
 }
 
@@ -744,8 +868,9 @@ specdec_status specdec_prefill(const specdec_model* model, specdec_kv* kv, int32
   if (kv->len_upper + n - 1 > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
   hipStream_t s = (hipStream_t)stream;
   // Chunks of as many tokens per sequence as the handle's rows allow (bf16: passes
-  // of more than 64 rows run the wide GEMM; float32 models keep 64-row chunks).
-  const int per = model->max_rows / B;
+  // of more than 64 rows run the wide GEMM; float32 models keep 64-row chunks;
+  // FP8 caches: as many as the ring takes).
+  const int per = std::min(model->max_rows / B, is_fp8(kv) ? kv->window - kF8Block : model->max_rows);
   const int C = std::max(1, model->desc.dtype == SPECDEC_BF16 ? per : std::min(per, 64));
   if (model->max_rows < B) return SPECDEC_ERR_SHAPE;
   for (int c0 = 0; c0 < n - 1; c0 += C) {
@@ -759,6 +884,10 @@ specdec_status specdec_prefill(const specdec_model* model, specdec_kv* kv, int32
     ra.c0 = c0;
     st = forward(model, kv, ra, (int)std::min<int64_t>(kv->len_upper + c0 + rps, kv->capacity), model->logits, true, s);
     if (st != SPECDEC_OK) return st;
+    if (is_fp8(kv)) {
+      Timed t(SPECDEC_KERNEL_COMMIT, s);
+      SD_TRY(launch_kv8_seal(kv8_of(kv), model->n_layers, c0, rps, nullptr, s));
+    }
   }
   hipLaunchKernelGGL(prefill_finish_kernel, dim3(1), dim3(64), 0, s, B, n, tokens, kv_len(kv), kv_pending(kv),
                      kv_npending(kv));
@@ -779,6 +908,7 @@ specdec_status specdec_draft_step(const specdec_model* draft, specdec_kv* kv, in
   if (temperature > 0.f && !q_out) return SPECDEC_ERR_INVALID_ARG;
   const int B = kv->batch;
   if (kv->len_upper + slot + 2 > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  if (!ring_holds(kv, gamma + 1)) return SPECDEC_ERR_SHAPE;
   hipStream_t s = (hipStream_t)stream;
   RowsArgs ra{};
   if (slot == 0) {
@@ -824,6 +954,7 @@ specdec_status specdec_verify(const specdec_model* target, specdec_kv* kv, int32
   if (!logits_out || gamma < 0 || (gamma > 0 && (!d || ld_d < gamma))) return SPECDEC_ERR_INVALID_ARG;
   const int B = kv->batch;
   if (kv->len_upper + gamma + 1 > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  if (!ring_holds(kv, gamma + 1)) return SPECDEC_ERR_SHAPE;
   RowsArgs ra{};
   ra.mode = ROWS_VERIFY;
   ra.rps = gamma + 1;
@@ -911,6 +1042,12 @@ specdec_status check_accept(int32_t batch, int32_t gamma, int32_t vocab, int32_t
   if (input_kind != SPECDEC_INPUT_PROBS && input_kind != SPECDEC_INPUT_LOGITS) return SPECDEC_ERR_INVALID_ARG;
   if (gamma > 0 && (!d || ld_d < gamma)) return SPECDEC_ERR_INVALID_ARG;
   if (temperature > 0.f && gamma > 0 && !q) return SPECDEC_ERR_INVALID_ARG;
+  return SPECDEC_OK;
+}
+
+specdec_status check_rules(int32_t batch, int32_t rows, int32_t vocab) {
+  if (batch <= 0 || rows <= 0 || vocab <= 0) return SPECDEC_ERR_INVALID_ARG;
+  if (vocab > kRulesMaxVocab || (int64_t)batch * rows > 65535) return SPECDEC_ERR_UNSUPPORTED;
   return SPECDEC_OK;
 }
 }  // namespace
@@ -1005,8 +1142,11 @@ specdec_status specdec_kv_commit(specdec_kv* kv, int32_t gamma, int32_t role, co
   c.next_token = next_token;
   c.counter = kv_counter(kv);
   specdec_status st;
+  if (is_fp8(kv) && !ring_holds(kv, gamma + 1)) return SPECDEC_ERR_SHAPE;
   {
     Timed t(SPECDEC_KERNEL_COMMIT, (hipStream_t)stream);
+    // (before the lengths change: the blocks that the commit completes)
+    if (is_fp8(kv)) SD_TRY(launch_kv8_seal(kv8_of(kv), kv->n_layers, 0, 0, &c, (hipStream_t)stream));
     st = hip_status(launch_commit(c, (hipStream_t)stream));
   }
   if (st == SPECDEC_OK) kv->len_upper += gamma + 1;
@@ -1018,6 +1158,55 @@ specdec_status specdec_sample(int32_t batch, int32_t vocab, const float* probs, 
                               void* stream) {
   if (batch <= 0 || vocab <= 0 || !probs || !out || ld < vocab) return SPECDEC_ERR_INVALID_ARG;
   return hip_status(launch_sample(batch, vocab, probs, ld, rand, seed, step, purpose, index, out, (hipStream_t)stream));
+}
+
+size_t specdec_sample_logits_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab) {
+  if (check_rules(batch, rows, vocab) != SPECDEC_OK) return 0;
+  return rules_scratch_bytes(batch * rows, vocab);
+}
+
+specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab, const float* logits, int64_t ld,
+                                     const specdec_sampling* rules, const uint32_t* rand, uint64_t seed, uint64_t step,
+                                     const uint64_t* step_dev, int32_t purpose, int32_t index, float* probs,
+                                     int64_t ld_probs, int32_t* out, int64_t ld_out, int32_t* status, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  const specdec_status st = check_rules(batch, rows, vocab);
+  if (st != SPECDEC_OK) return st;
+  if (!logits || ld < vocab || (!probs && !out) || (probs && ld_probs < vocab) || (out && ld_out < 1) ||
+      misaligned8(step_dev) || purpose < 0 || purpose > 0xffff || index < 0 || index > 0xffff - (rows - 1) ||
+      !workspace || (uintptr_t)workspace % kAlign || workspace_bytes < rules_scratch_bytes(batch * rows, vocab))
+    return SPECDEC_ERR_INVALID_ARG;
+  if (probs) {  // (the draw reads logits again after other workgroups have stored probabilities)
+    const int64_t n = (int64_t)batch * rows - 1;
+    const char *p0 = (const char*)probs, *p1 = (const char*)(probs + n * ld_probs + vocab);
+    const char *l0 = (const char*)logits, *l1 = (const char*)(logits + n * ld + vocab);
+    if (p0 < l1 && l0 < p1) return SPECDEC_ERR_INVALID_ARG;
+  }
+  RulesArgs a{};
+  a.B = batch;
+  a.rows = rows;
+  a.V = vocab;
+  a.logits = logits;
+  a.ld = ld;
+  if (rules) {
+    a.temperature = rules->temperature;
+    a.top_k = rules->top_k;
+    a.top_p = rules->top_p;
+    a.min_p = rules->min_p;
+  }
+  a.rand = rand;
+  a.seed = seed;
+  a.step = step;
+  a.step_dev = step_dev;
+  a.purpose = purpose;
+  a.index = index;
+  a.probs = probs;
+  a.ld_probs = ld_probs;
+  a.out = out;
+  a.ld_out = ld_out;
+  a.status = status;
+  a.scratch = workspace;
+  return hip_status(launch_rules(a, (hipStream_t)stream));
 }
 
 specdec_status specdec_draw_u32(int32_t batch, uint64_t seed, uint64_t step, int32_t purpose, int32_t index,

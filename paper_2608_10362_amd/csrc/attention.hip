@@ -1374,6 +1374,7 @@ size_t attention_counter_count(int n_heads, int n_kv_heads, int max_rows) {
 }
 
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s) {
+  if (a.kv.dtype == SPECDEC_FP8) return launch_attention8(a, s);
   const int B = a.M / a.rps;
   AttnArgs ab = a;  // the bf16 path chooses its own parts
   if (a.kv.dtype == SPECDEC_BF16) {

@@ -1,0 +1,22 @@
+// Device pieces of the FP8 cache shared by its copy and attention kernels.
+#pragma once
+
+#include "device_common.h"
+
+namespace specdec {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));  // (callers' rows: bf16 alignment)
+
+// 8 e4m3 codes (four in each word, low byte first) times the power of two
+// `scale`, exact in bf16.
+__device__ __forceinline__ bf16x8 fp8x8_to_bf16(uint32_t lo, uint32_t hi, float scale) {
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
+  return __builtin_bit_cast(bf16x8, o);
+}
+
+}  // namespace specdec

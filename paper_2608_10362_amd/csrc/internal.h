@@ -48,6 +48,69 @@ template <> struct KvIndex<uint16_t> {
   }
 };
 
+// ------------------------------------------------------------------ FP8 KV cache layout
+// Positions in blocks of 64.  A sequence's committed whole blocks (positions
+// below sealed = len / 64 * 64) are held as e4m3 codes with one float32 scale
+// 2^e per (layer, sequence, kv head, block, K or V): e is the smallest integer
+// with max|x| <= 448 * 2^e over the block's finite entries, and at least -100.
+// A power of two costs a floating-point code nothing (the relative step of
+// e4m3 is the same at every scale), makes x / scale exact, and makes code *
+// scale exact in bf16, which v_cvt_scalef32_pk_bf16_fp8 gives in one
+// instruction for two codes.  Positions from sealed on (the incomplete block
+// and rows not yet committed) are bf16 in a ring of `window` positions
+// (position p at p % window, a KvLayout of capacity `window`): a block is
+// rounded once, when it is complete, and rows that are rolled back never
+// touch a code.
+//  data: ring of every layer, scales, codes (kv8_bytes; regions 256-byte
+//  aligned).  Per (layer, sequence, kv head) 2 * capacity / 64 scales (K, V of
+//  block 0, of block 1, ...) and 2 * capacity * head_dim code bytes: block i's
+//  K codes at 128 * head_dim * i, its V codes 64 * head_dim further on, each
+//  head_dim / 16 fragments of 1 KB, lane l = 16c + i holding 16 bytes:
+//   K (head_dim >= 64): fragment (2s + t) * head_dim / 64 + n: position
+//     32s + 8 (i / 4) + 4t + i % 4, dims 64n + 16c .. +15;
+//   K (head_dim 32): fragment s: bytes 8t .. 8t+7: that position, dims 8c .. +7;
+//   V: fragment dt: dim 16 dt + i, positions 8c .. +7, then 32 + 8c .. +7.
+//  (The K rows are in the order that leaves lane group c of K Q^T's product
+//  with positions 8c .. 8c+7 of a 32-position step, the k order of V: the
+//  probabilities feed P V from the registers they were made in.)
+constexpr int kF8Block = 64;
+constexpr int kF8MinExp = -100;
+struct Kv8Layout {
+  unsigned char* codes;
+  float* scales;
+  KvLayout ring;       // data, batch, capacity = window, n_kv_heads, head_dim, dtype = bf16
+  const int32_t* len;  // [batch] committed lengths
+  int capacity;
+  __device__ __forceinline__ size_t unit(int layer, int b, int g) const {
+    return ((size_t)layer * ring.batch + b) * ring.n_kv_heads + g;
+  }
+  __device__ __forceinline__ unsigned char* code_base(int layer, int b, int g) const {
+    return codes + unit(layer, b, g) * 2 * (size_t)capacity * ring.head_dim;
+  }
+  __device__ __forceinline__ float* scale_base(int layer, int b, int g) const {
+    return scales + unit(layer, b, g) * 2 * (size_t)(capacity / kF8Block);
+  }
+};
+size_t kv8_bytes(int n_layers, int batch, int n_kv_heads, int head_dim, int capacity, int window);
+Kv8Layout kv8_layout(void* data, const int32_t* len, int n_layers, int batch, int n_kv_heads, int head_dim,
+                     int capacity, int window);
+// Rows k, v [n, h_kv, hd] (bf16) as positions pos0 .. pos0+n-1 of sequence b (pos0
+// a multiple of 64): every block that ends inside becomes codes, the last
+// `window` rows go to the ring.
+hipError_t launch_kv8_write(const Kv8Layout& kv, int layer, int b, int pos0, int n, const void* k, const void* v,
+                            hipStream_t s);
+// The values back: below sealed what the codes stand for, above it the ring's.
+hipError_t launch_kv8_read(const Kv8Layout& kv, int layer, int b, int pos0, int n, void* k, void* v, hipStream_t s);
+// k, v [batch, n, h_kv, hd] into the ring at positions len[b] .. len[b]+n-1.
+hipError_t launch_kv8_append(const Kv8Layout& kv, int layer, int n, const void* k, const void* v, int32_t* status,
+                             int pos_limit, hipStream_t s);
+// Seals, in every layer, the blocks that sequence b completes when its length
+// goes from len[b] + c0 to that plus its step: n, or what a commit adds.
+struct CommitArgs;
+hipError_t launch_kv8_seal(const Kv8Layout& kv, int n_layers, int c0, int n, const CommitArgs* commit, hipStream_t s);
+// len[b] += n.
+hipError_t launch_kv_advance(int batch, int n, int32_t* len, hipStream_t s);
+
 // ------------------------------------------------------------------ GEMM
 // y = (x (.) gain) W^T, optional per-row scale s_m = 1/sqrt(mean_k h_mk^2 + eps)
 // taken from partial sums of squares, W bf16 or f32 row-major [N, K] split in
@@ -155,6 +218,8 @@ struct RowsArgs {
   const void* embed;      // [V, d] storage type
   const void* gain;       // [d] first layer's attention RMSNorm gain
   RowDesc* rows;          // out [M]
+  RowDesc* rows_kv;       // or null (FP8 caches): out [M], pos replaced by pos % window
+  int window;
   float* rope_cs;         // out [M, head_dim]: cos j<hd/2 then sin
   float* h;               // out [M, d]
   float* xg;              // out [M, d] h * gain
@@ -194,6 +259,11 @@ struct AttnArgs {
   // then starts on data already in the last-level cache.
   const unsigned char* next_w;
   uint32_t next_w_bytes;
+  // FP8 caches (kv.dtype SPECDEC_FP8): the cache, and the positions past len
+  // that count as committed in this pass (earlier chunks of a prefill).  rows
+  // may be null there: row i of sequence b is at len[b] + i.
+  Kv8Layout f8;
+  int c0;
 };
 constexpr uint32_t kNextWeightsPerBlock = 48u << 10;
 constexpr int kMaxParts = 64;  // parts of one head that the one-round in-kernel and the long-context combine take (one per lane)
@@ -203,6 +273,10 @@ hipError_t launch_fill_u32(uint32_t* p, size_t n, uint32_t v, hipStream_t s);
 int attention_chunk(int dtype, int head_dim);  // keys per split of the attention kernel
 int device_compute_units();                    // CUs of the current device (cached)
 hipError_t launch_rope_append(const AttnArgs& a, hipStream_t s);
+// FP8 caches (attention8.hip): parts of one (row, head) the launch may write
+// (o_part holds M * n_heads * parts * head_dim floats, ml_part 2 per part).
+int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int max_ctx);
+hipError_t launch_attention8(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------------------------ sampling / bookkeeping
@@ -263,7 +337,37 @@ struct CommitArgs {
   const int32_t* next_token;
   uint64_t* counter;  // the cache's commit counter, +1 per launch
 };
+// Positions a commit adds to sequence b's length (0 after an accept error).
+__device__ __forceinline__ int commit_step(const CommitArgs& a, int b) {
+  const int A = a.n_accepted[b], g = a.gamma;
+  if (A < 0 || A > g) return 0;
+  return a.role == SPECDEC_ROLE_TARGET ? A + 1 : a.n_pending[b] + (A < g - 1 ? A : g - 1);
+}
 hipError_t launch_commit(const CommitArgs& a, hipStream_t s);
+
+// Sampling rules (rules.hip).
+constexpr int kRulesMaxVocab = 1 << 20;  // (integer masses of 43 bits: their sums stay below 2^63)
+size_t rules_scratch_bytes(int n_rows, int V);
+struct RulesArgs {
+  int B, rows, V;
+  const float* logits;
+  int64_t ld;
+  const float* temperature;  // [B] each, or null: 1, off, off, off
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const uint32_t* rand;      // [B, rows] or null
+  uint64_t seed, step;
+  const uint64_t* step_dev;
+  int purpose, index;
+  float* probs;              // or null
+  int64_t ld_probs;
+  int32_t* out;              // or null
+  int64_t ld_out;
+  int32_t* status;
+  void* scratch;             // rules_scratch_bytes(B * rows, V)
+};
+hipError_t launch_rules(const RulesArgs& a, hipStream_t s);
 
 // Streaming-read ceiling probe (stream.hip): reads bytes / 1024 KB-chunks of buf.
 hipError_t launch_stream_read(const void* buf, size_t bytes, uint32_t* sink, hipStream_t s);

@@ -11,6 +11,7 @@
 
 #include "device_common.h"
 #include "internal.h"
+#include "sampling_common.h"
 
 namespace specdec {
 
@@ -18,19 +19,6 @@ namespace {
 
 constexpr int kSampThreads = 1024;
 constexpr int kMaxGamma = 31;
-
-__device__ __forceinline__ uint64_t fp_weight(float r) {
-  return r > 0.f ? (uint64_t)(r * 1099511627776.0f) : 0ull;  // exact: r * 2^40, truncation = floor
-}
-// floor(x * S / 2^32) without a 128-bit product (S < 2^56, x < 2^32).
-__device__ __forceinline__ uint64_t scale_word(uint32_t x, uint64_t S) {
-  return (uint64_t)x * (S >> 32) + (((uint64_t)x * (S & 0xffffffffull)) >> 32);
-}
-
-__device__ __forceinline__ uint64_t shfl_up_u64(uint64_t v, int o) {
-  uint32_t lo = __shfl_up((uint32_t)v, o, kWave), hi = __shfl_up((uint32_t)(v >> 32), o, kWave);
-  return ((uint64_t)hi << 32) | lo;
-}
 
 struct SampShared {
   uint64_t wave_tot[kSampThreads / kWave];
@@ -160,6 +148,7 @@ __global__ __launch_bounds__(256) void rows_embed_kernel(RowsArgs a) {
   }
   if (first) {
     a.rows[r] = RowDesc{b, pos, tok, valid};
+    if (a.rows_kv) a.rows_kv[r] = RowDesc{b, pos % a.window, tok, valid};
   }
   const ET* e = (const ET*)a.embed + (size_t)tok * a.d_model;
   const ET* gn = (const ET*)a.gain;
@@ -229,24 +218,6 @@ __host__ __device__ inline Scratch carve(void* base, int B, int rows, int V) {
   p += align256(sizeof(StatPart) * (size_t)B * rows * NC);
   s.draw = (DrawPart*)p;
   return s;
-}
-
-// Four consecutive entries of a row of V from j (a multiple of 4), `pad` past
-// j1 (a multiple of 4, or V).
-__device__ __forceinline__ void load_quad(const float* row, int j, int j1, int V, float pad, float (&v)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = pad;
-  if ((V & 3) == 0 || j + 4 <= j1) {  // (first test uniform: whole quads need no second path)
-    if (j < j1) {
-      const f32x4 t = *(const f32x4_a4*)(row + j);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = t[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j + e < j1) v[e] = row[j + e];
-  }
 }
 
 // stats: grid (NC, B * rows_per_seq), block 256.  Row i of sequence b is

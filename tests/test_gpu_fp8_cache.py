@@ -1,0 +1,546 @@
+"""The 8-bit KV cache and the attention over it, against the float64 oracle.
+
+Quantization is exact arithmetic (a power-of-two scale, one rounding to e4m3),
+so stored values are compared bit for bit.  Attention: the float32 queries and
+probabilities enter the products as hi + lo bf16 parts.  A part sum is off by at
+most (2^-9)^2 of its value (two roundings of half a step 2^-9 each), a float32
+dot product of n terms by n 2^-24 of the sum of the terms' magnitudes; an error
+ds of a score changes its probability by the factor 1 + ds.  The bound used:
+  ds  = (2^-18 + (hd + 2) 2^-24) max_j sum_d |q_d k_jd| / sqrt(hd) + 2^-22 max|s|
+  |o - ref| <= (2 ds + 2^-17 + 2^-22 + (keys + 64) 2^-24) max|v| over the row's keys
+(2 ds: numerator and normaliser; 2^-17: the split of p, twice; 2^-22: exp2 and
+the division; the last: the float32 sums.)
+"""
+import dataclasses
+
+import numpy as np
+import pytest
+
+from oracle import fp8
+from paper_2608_10362_amd import binding, synth
+from tests.gpu_util import i32, log, torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+
+def _shape(hd, H, G, n_layers=2):
+    return synth.ModelShape(n_layers, max(64, H * hd), H, G, hd, 128, 64)
+
+
+def _bf16(x):
+    torch = torch_cuda()
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda().to(torch.bfloat16)
+
+
+def _np(t):
+    return t.float().cpu().numpy()
+
+
+def _rows(rng, n, G, hd, spread=True):
+    """bf16 rows whose heads differ in magnitude."""
+    x = rng.normal(0, 1.3, (n, G, hd))
+    if spread:
+        x *= 2.0 ** rng.integers(-12, 12, (1, G, 1))
+    return _np(_bf16(x))
+
+
+def _cache(shape, B, cap, window=128, dirt=255):
+    kv = binding.Fp8KVCache(shape, B, cap, window)
+    kv.data.fill_(dirt)  # (stale contents: NaN codes, NaN scales and NaN rows)
+    return kv
+
+
+# ---------------------------------------------------------------- storage
+@pytest.mark.parametrize("hd,G", [(32, 2), (64, 3), (128, 1), (128, 5)])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 128, 200, 333])
+def test_write_then_read(hd, G, n):
+    rng = np.random.default_rng(n + hd)
+    shape = _shape(hd, 2 * G, G)
+    kv = _cache(shape, 3, 384)
+    log(f"write hd={hd} G={G} n={n}")
+    x = {(l, b): (_rows(rng, n, G, hd), _rows(rng, n, G, hd)) for l in range(2) for b in (0, 2)}
+    for (l, b), (k, v) in x.items():
+        kv.write_context(l, b, 0, _bf16(k), _bf16(v))
+    kv.set_state([n, 0, n], [[0, 1]] * 3, [1] * 3)
+    for (l, b), (k, v) in x.items():
+        gk, gv = kv.read_context(l, b, 0, n)
+        np.testing.assert_array_equal(_np(gk), fp8.stored(k, n // 64 * 64))
+        np.testing.assert_array_equal(_np(gv), fp8.stored(v, n // 64 * 64))
+        lo = n // 3  # a range that starts and ends inside blocks
+        gk, gv = kv.read_context(l, b, lo, n - lo - n // 5)
+        np.testing.assert_array_equal(_np(gk), fp8.stored(k, n // 64 * 64)[lo:n - n // 5])
+        np.testing.assert_array_equal(_np(gv), fp8.stored(v, n // 64 * 64)[lo:n - n // 5])
+
+
+def test_write_in_pieces_and_what_it_leaves():
+    """A context installed by two calls; other sequences, layers and later positions keep their contents."""
+    rng = np.random.default_rng(5)
+    shape = _shape(64, 4, 2)
+    kv = _cache(shape, 2, 384)
+    a, c = _rows(rng, 300, 2, 64), _rows(rng, 300, 2, 64)
+    for b in range(2):
+        kv.write_context(0, b, 0, _bf16(a), _bf16(c))
+        kv.write_context(1, b, 0, _bf16(c), _bf16(a))
+    k2, v2 = _rows(rng, 150, 2, 64), _rows(rng, 150, 2, 64)
+    kv.write_context(1, 0, 128, _bf16(k2[:100]), _bf16(v2[:100]))
+    kv.set_state([228, 300], [[0, 1]] * 2, [1] * 2)
+    gk, gv = kv.read_context(1, 0, 0, 228)
+    want_k, want_v = np.concatenate([c[:128], k2[:100]]), np.concatenate([a[:128], v2[:100]])
+    np.testing.assert_array_equal(_np(gk), fp8.stored(want_k, 192))
+    np.testing.assert_array_equal(_np(gv), fp8.stored(want_v, 192))
+    for l, b in ((0, 1), (1, 1)):
+        gk, gv = kv.read_context(l, b, 0, 300)
+        np.testing.assert_array_equal(_np(gk), fp8.stored((a, c)[l], 256))
+        np.testing.assert_array_equal(_np(gv), fp8.stored((c, a)[l], 256))
+
+
+def test_extreme_blocks():
+    """Zero blocks, the smallest and largest magnitudes, one outlier, NaN and infinities."""
+    hd, G = 64, 8
+    x = np.random.default_rng(6).normal(0, 1, (64, G, hd))
+    x[:, 0] = 0
+    x[:, 1] *= 2.0 ** -125
+    x[:, 2] *= 2.0 ** 120
+    x[5, 3, 7] = 2.0 ** 20
+    x[9, 4, 0], x[10, 4, 1], x[11, 4, 2] = np.nan, np.inf, -np.inf
+    x[:, 5] = 448.0
+    x[:, 6] = -449.0
+    x[:, 7] = np.nan
+    x = _np(_bf16(x))
+    kv = _cache(_shape(hd, G, G, 1), 1, 64)
+    kv.write_context(0, 0, 0, _bf16(x), _bf16(-x))
+    kv.set_state([64], [[0, 1]], [1])
+    k, v = kv.read_context(0, 0, 0, 64)
+    ref = fp8.stored(x, 64)
+    np.testing.assert_array_equal(_np(k), ref)
+    np.testing.assert_array_equal(_np(v), -ref)
+
+
+@pytest.mark.parametrize("hd,G,window", [(32, 4, 128), (64, 1, 192), (128, 3, 128)])
+def test_append_and_advance(hd, G, window):
+    """Ragged sequences grown by steps of every kind; drafted rows that were overwritten leave nothing."""
+    rng = np.random.default_rng(hd)
+    B, cap = 3, 640
+    shape = _shape(hd, G, G)
+    kv = _cache(shape, B, cap, window)
+    start = [0, 61, 130]
+    text = [[(_rows(rng, cap, G, hd), _rows(rng, cap, G, hd)) for _ in range(2)] for _ in range(B)]
+    for b in range(B):
+        for l in range(2):
+            if start[b]:
+                k, v = text[b][l]
+                kv.write_context(l, b, 0, _bf16(k[:start[b]]), _bf16(v[:start[b]]))
+    kv.set_state(start, [[0, 1]] * B, [1] * B)
+    length = list(start)
+    for n in (1, 2, 63, 1, 5, window - 63, 1, 64, 7):
+        for l in range(2):
+            k = np.stack([text[b][l][0][length[b]:length[b] + n] for b in range(B)])
+            v = np.stack([text[b][l][1][length[b]:length[b] + n] for b in range(B)])
+            junk = np.full((B, window - 63, G, hd), 3e38, np.float32)  # (rows that are never committed)
+            binding.specdec_kv_append(kv, l, _bf16(junk), _bf16(junk))
+            binding.specdec_kv_append(kv, l, _bf16(k), _bf16(v))
+        binding.specdec_kv_advance(kv, n)
+        length = [x + n for x in length]
+        st = kv.read_state()
+        assert list(st["len"]) == length and st["status"] == 0
+        log(f"advance {n}: {length}")
+        for b in range(B):
+            for l in range(2):
+                gk, gv = kv.read_context(l, b, 0, length[b])
+                sealed = length[b] // 64 * 64
+                np.testing.assert_array_equal(_np(gk), fp8.stored(text[b][l][0][:length[b]], sealed))
+                np.testing.assert_array_equal(_np(gv), fp8.stored(text[b][l][1][:length[b]], sealed))
+
+
+# ---------------------------------------------------------------- attention
+def _fill(kv, rng, lens, n, G, hd, layer=0, spread=False):
+    """Contexts and n appended rows; returns what each sequence's keys and values are."""
+    out = []
+    kn, vn = [], []
+    for b, L in enumerate(lens):
+        k, v = _rows(rng, L + n, G, hd, spread), _rows(rng, L + n, G, hd, spread)
+        if L:
+            kv.write_context(layer, b, 0, _bf16(k[:L]), _bf16(v[:L]))
+        out.append([fp8.stored(k, L // 64 * 64), fp8.stored(v, L // 64 * 64)])
+        kn.append(k[L:])
+        vn.append(v[L:])
+    kv.set_state(lens, [[0, 1]] * len(lens), [1] * len(lens))
+    binding.specdec_kv_append(kv, layer, _bf16(np.stack(kn)), _bf16(np.stack(vn)))
+    return out
+
+
+def _check(got, q, kvs, lens, rows=None):
+    """Every row (or those listed) within the bound above; returns the worst error."""
+    B, n, H, hd = q.shape
+    worst = 0.0
+    for b in range(B):
+        k, v = kvs[b]
+        g = np.arange(H) // (H // k.shape[1])
+        for i in range(n) if rows is None else rows:
+            m = lens[b] + i + 1
+            kk, vv = k[:m][:, g], v[:m][:, g]  # [m, H, hd]
+            s = np.einsum("mhd,hd->mh", kk, q[b, i].astype(np.float64)) / np.sqrt(hd)
+            e = np.exp(s - s.max(0))
+            ref = np.einsum("mh,mhd->hd", e, vv) / e.sum(0)[:, None]
+            mag = np.einsum("mhd,hd->mh", np.abs(kk), np.abs(q[b, i]).astype(np.float64)).max(0) / np.sqrt(hd)
+            ds = (2.0 ** -18 + (hd + 2) * 2.0 ** -24) * mag + 2.0 ** -22 * np.abs(s).max(0)
+            tol = (2 * ds + 2.0 ** -17 + 2.0 ** -22 + (m + 64) * 2.0 ** -24) * np.abs(vv).max((0, 2))
+            err = np.abs(got[b, i] - ref).max(1)
+            assert (err <= tol).all(), (b, i, err.max(), tol.min())
+            worst = max(worst, float(err.max()))
+    return worst
+
+
+def _attend(kv, q, layer=0, ws=None):
+    torch = torch_cuda()
+    qd = torch.from_numpy(q).cuda()
+    out = torch.full_like(qd, float("nan"))
+    binding.specdec_attention(kv, layer, qd, out, ws)
+    return out.cpu().numpy()
+
+
+CASES = [  # hd, H, G, lens, n, window
+    (128, 4, 4, [0], 1, 128),
+    (128, 4, 4, [1], 1, 128),
+    (64, 8, 1, [63], 1, 128),
+    (64, 8, 1, [64], 2, 128),
+    (32, 6, 3, [65, 127, 128, 300, 0], 5, 128),
+    (128, 8, 8, [2047], 1, 128),
+    (64, 32, 4, [301, 1023, 700, 512], 5, 128),
+    (128, 8, 2, [777, 64], 9, 128),
+    (32, 16, 1, [500], 17, 128),
+    (64, 4, 2, [190, 3], 65, 128),
+    (128, 4, 4, [1000], 100, 192),
+    (128, 2, 1, [130], 300, 384),
+    (32, 2, 2, [0], 321, 384),
+    (64, 2, 1, [20000], 1, 128),
+    (64, 8, 4, [5000, 1, 1, 1, 4000], 3, 128),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"hd{c[0]}-{c[1]}:{c[2]}-len{max(c[3])}-n{c[4]}")
+def test_attention(case):
+    hd, H, G, lens, n, window = case
+    log(f"attention {case}")
+    rng = np.random.default_rng(sum(lens) + n + hd)
+    cap = (max(lens) + n + 63) // 64 * 64
+    kv = _cache(_shape(hd, H, G, 1), len(lens), cap, window)
+    kvs = _fill(kv, rng, lens, n, G, hd)
+    q = rng.normal(0, 1.5, (len(lens), n, H, hd)).astype(np.float32)
+    got = _attend(kv, q)
+    rows = None if n * max(lens + [1]) < 40000 else sorted({0, 1, n // 2, n - 2, n - 1})
+    worst = _check(got, q, kvs, lens, rows)
+    log(f"worst error {worst:.3g}")
+    assert kv.read_state()["status"] == 0
+
+
+def test_attention_many_sequences():
+    """More sequences than a wave has lanes, of lengths that share workgroups."""
+    rng = np.random.default_rng(11)
+    B = 150
+    lens = [int(x) for x in rng.integers(0, 400, B)]
+    kv = _cache(_shape(64, 4, 2, 1), B, 448)
+    kvs = _fill(kv, rng, lens, 2, 2, 64)
+    q = rng.normal(0, 1, (B, 2, 4, 64)).astype(np.float32)
+    _check(_attend(kv, q), q, kvs, lens)
+
+
+def test_attention_scores_of_every_size():
+    """One key far above the rest, in a code block and in the ring; equal scores; large values."""
+    rng = np.random.default_rng(12)
+    for at in (10, 130):
+        lens, hd = [140], 64
+        kv = _cache(_shape(hd, 2, 1, 1), 1, 192)
+        k, v = _rows(rng, 141, 1, hd, False), _rows(rng, 141, 1, hd, False) * 64
+        k[at] *= 30
+        kv.write_context(0, 0, 0, _bf16(k[:140]), _bf16(v[:140]))
+        kv.set_state(lens, [[0, 1]], [1])
+        binding.specdec_kv_append(kv, 0, _bf16(k[None, 140:]), _bf16(v[None, 140:]))
+        k, v = _np(_bf16(k)), _np(_bf16(v))
+        kvs = [[fp8.stored(k, 128), fp8.stored(v, 128)]]
+        q = rng.normal(0, 3, (1, 1, 2, hd)).astype(np.float32)
+        _check(_attend(kv, q), q, kvs, lens)
+        q[:] = 0  # (every key alike)
+        _check(_attend(kv, q), q, kvs, lens)
+
+
+def test_rows_that_are_not_seen_change_nothing():
+    """NaN and infinities in rows later than a query's, in slots of the ring past
+    the newest row, and in codes past the sealed ones; the rows that see them get NaN or infinity."""
+    rng = np.random.default_rng(13)
+    hd, H, G, L, n = 64, 4, 2, 150, 6
+    for bad in (np.nan, np.inf):
+        kv = _cache(_shape(hd, H, G, 1), 1, 256)
+        kvs = _fill(kv, rng, [L], n, G, hd)
+        k, v = kvs[0][0][L:].astype(np.float32), kvs[0][1][L:].astype(np.float32)
+        q = rng.normal(0, 1, (1, n, H, hd)).astype(np.float32)
+        vb, kb = v.copy(), k.copy()
+        vb[3, 0, 5] = bad     # row 3's value of kv head 0
+        vb[3, 0, 6] = -bad
+        kb[4, 1, 2] = np.nan  # row 4's key of kv head 1
+        binding.specdec_kv_append(kv, 0, _bf16(kb[None]), _bf16(vb[None]))
+        got = _attend(kv, q)
+        _check(got, q, kvs, [L], rows=[0, 1, 2])
+        assert not np.isfinite(got[0, 3:, :2, 5]).any() and not np.isfinite(got[0, 3:, :2, 6]).any()
+        assert np.isnan(got[0, 4:, 2:]).all()
+        _check(got[:, :4, 2:], q[:, :4, 2:], [[kvs[0][0][:, 1:], kvs[0][1][:, 1:]]], [L])
+        # the other dims of kv head 0 are those of a value without these two
+        got[:, :, :, 5:7], kvs[0][1][:, :, 5:7] = 0, 0
+        _check(got[:, :, :2], q[:, :, :2], [[kvs[0][0][:, :1], kvs[0][1][:, :1]]], [L])
+
+
+def test_attention_offsets_past_32_bits():
+    """The last sequence of a cache of more than 4 GiB of codes."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(14)
+    shape = _shape(128, 32, 32, 1)
+    B, cap = 36, 16384
+    kv = binding.Fp8KVCache(shape, B, cap, 128)
+    assert B * 32 * 2 * cap * 128 > 2 ** 32
+    L = [1] * (B - 1) + [cap - 2]
+    k = torch.empty((cap - 2, 32, 128), dtype=torch.bfloat16, device="cuda").normal_(0, 1)
+    v = torch.empty_like(k).normal_(0, 1)
+    for b in range(B - 1):
+        kv.write_context(0, b, 0, k[:1].contiguous(), v[:1].contiguous())
+    kv.write_context(0, B - 1, 0, k, v)
+    kv.set_state(L, [[0, 1]] * B, [1] * B)
+    binding.specdec_kv_append(kv, 0, k[:1][None].expand(B, -1, -1, -1).contiguous(),
+                              v[:1][None].expand(B, -1, -1, -1).contiguous())
+    q = rng.normal(0, 1, (B, 1, 32, 128)).astype(np.float32)
+    got = _attend(kv, q)
+    ek, ev = kv.read_context(0, B - 1, 0, cap - 2)
+    ek, ev = (torch.cat([a, b[:1]]).double() for a, b in ((ek, k), (ev, v)))
+    for h in (0, 17, 31):
+        s = ek[:, h] @ torch.from_numpy(q[B - 1, 0, h]).double().cuda() / np.sqrt(128)
+        ref = (torch.softmax(s, 0) @ ev[:, h]).cpu().numpy()
+        np.testing.assert_allclose(got[B - 1, 0, h], ref, atol=2e-4)
+    np.testing.assert_allclose(got[0, 0], _np(v[0]), rtol=2.0 ** -16, atol=1e-6)  # (two equal keys and values)
+    np.testing.assert_array_equal(_np(kv.read_context(0, B - 1, cap - 66, 2)[0]),
+                                  fp8.stored(_np(k[cap - 128:cap - 64]), 64)[62:64])
+
+
+def test_streams_graphs_and_shared_workspace():
+    """A captured step (append, attention, advance) replayed with new rows equals
+    the eager steps; two graphs share one workspace; a stream other than the default."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(15)
+    hd, H, G, L, n, steps = 64, 8, 2, 120, 2, 5
+    kvs = [_cache(_shape(hd, H, G, 1), 1, 192) for _ in range(3)]
+    for kv in kvs:
+        _fill(kv, np.random.default_rng(1), [L], n, G, hd)
+    k = [_bf16(_rows(rng, n, G, hd, False)[None]) for _ in range(steps)]
+    v = [_bf16(_rows(rng, n, G, hd, False)[None]) for _ in range(steps)]
+    q = [torch.from_numpy(rng.normal(0, 1, (1, n, H, hd)).astype(np.float32)).cuda() for _ in range(steps)]
+    ws = binding.attention_workspace(kvs[0], H, n)
+    eager, out = [], torch.empty_like(q[0])
+    for i in range(steps):
+        binding.specdec_kv_append(kvs[0], 0, k[i], v[i])
+        binding.specdec_attention(kvs[0], 0, q[i], out, ws)
+        binding.specdec_kv_advance(kvs[0], n)
+        eager.append(out.clone())
+    ks, vs, qs = k[0].clone(), v[0].clone(), q[0].clone()
+    outs, graphs = [torch.empty_like(out) for _ in range(2)], []
+    side = torch.cuda.Stream()
+    for j, kv in enumerate(kvs[1:]):
+        kv.kv.len_upper = L + steps * n - n  # (the bound the last replay starts from)
+        side.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(g, stream=side):
+                binding.specdec_kv_append(kv, 0, ks, vs)
+                binding.specdec_attention(kv, 0, qs, outs[j], ws)
+                binding.specdec_kv_advance(kv, n)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for i in range(steps):
+        ks.copy_(k[i])
+        vs.copy_(v[i])
+        qs.copy_(q[i])
+        for j, g in enumerate(graphs):
+            g.replay()
+        torch.cuda.synchronize()
+        for j in range(2):
+            # Other grids than the eager call's (the bound was higher at capture): both
+            # are within the bound above, whose largest term is 2 (2^-18 + 66 2^-24) * 12 *
+            # max|v| = 1e-3 here (sum |q k| / 8 up to 12, |v| up to 5.5).
+            torch.testing.assert_close(outs[j], eager[i], rtol=0, atol=2.5e-3)
+        torch.testing.assert_close(outs[0], outs[1], rtol=0, atol=0)
+    assert list(kvs[1].read_state()["len"]) == [L + steps * n]
+    with torch.cuda.stream(side):  # the same call on a stream of its own
+        kvs[0].set_state([L + (steps - 1) * n], [[0, 1]], [1], stream=side)
+        o2 = torch.empty_like(out)
+        binding.specdec_kv_append(kvs[0], 0, k[-1], v[-1])
+        binding.specdec_attention(kvs[0], 0, q[-1], o2)
+    side.synchronize()
+    torch.testing.assert_close(o2, eager[-1], rtol=0, atol=0)
+
+
+# ---------------------------------------------------------------- refusals
+def test_refusals():
+    torch = torch_cuda()
+    shape = _shape(64, 4, 2, 1)
+    kv = binding.Fp8KVCache(shape, 2, 256, 128)
+    r = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    f = lambda *s: torch.zeros(s, dtype=torch.float32, device="cuda")  # noqa: E731
+
+    def status(fn, code):
+        with pytest.raises(binding.SpecdecError) as e:
+            fn()
+        assert e.value.status == code
+
+    status(lambda: kv.write_context(0, 0, 32, r(10, 2, 64), r(10, 2, 64)), -2)
+    status(lambda: kv.write_context(0, 0, 192, r(65, 2, 64), r(65, 2, 64)), -3)
+    status(lambda: kv.write_context(1, 0, 0, r(1, 2, 64), r(1, 2, 64)), -1)
+    status(lambda: binding.specdec_kv_append(kv, 0, r(2, 66, 2, 64), r(2, 66, 2, 64)), -2)
+    status(lambda: binding.specdec_attention(kv, 0, f(2, 1, 3, 64), f(2, 1, 3, 64),
+                                             torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")), -2)
+    status(lambda: binding.specdec_attention(kv, 2, f(2, 1, 4, 64), f(2, 1, 4, 64)), -1)
+    status(lambda: binding.specdec_attention(kv, 0, f(2, 1, 4, 64), f(2, 1, 4, 64),
+                                             torch.zeros(16, dtype=torch.uint8, device="cuda")), -1)
+    kv.set_state([250, 3], [[0, 1]] * 2, [1] * 2)
+    status(lambda: binding.specdec_kv_advance(kv, 7), -3)
+    status(lambda: binding.specdec_kv_append(kv, 0, r(2, 7, 2, 64), r(2, 7, 2, 64)), -3)
+    status(lambda: binding.specdec_attention(kv, 0, f(2, 7, 4, 64), f(2, 7, 4, 64)), -3)
+    binding.specdec_kv_advance(kv, 6)
+    with pytest.raises(ValueError):
+        binding.specdec_kv_append(kv, 0, r(2, 1, 2, 32), r(2, 1, 2, 32))
+    with pytest.raises(ValueError):
+        binding.specdec_attention(kv, 0, f(2, 1, 4, 64).transpose(0, 1), f(1, 2, 4, 64))
+    with pytest.raises(ValueError):
+        binding.specdec_attention(kv, 0, f(2, 1, 4, 64), f(2, 1, 4, 64).to(torch.float64))
+    with pytest.raises(ValueError):
+        binding.specdec_attention(kv, 0, f(2, 1, 4, 64).cpu(), f(2, 1, 4, 64))
+
+
+# ---------------------------------------------------------------- the framework's passes over it
+@pytest.fixture(scope="module")
+def model():
+    torch_cuda()
+    shape = dataclasses.replace(synth.LLAMA_1B, n_layers=2, vocab=1024)
+    W = synth.make_weights(shape, n_layers=2)
+    return shape, W, binding.DeviceWeights(shape, W)
+
+
+def _oracle_on(shape, W, kv, b, length):
+    """The oracle's model and a cache that holds what the device's stands for."""
+    from oracle import model as om
+    m, c = om.Model(shape, W), om.KVCache(shape, 2, 512)
+    for l in range(2):
+        k, v = kv.read_context(l, b, 0, length)
+        c.k[l][:length], c.v[l][:length] = _np(k), _np(v)
+    c.length = length
+    return m, c
+
+
+@pytest.mark.parametrize("window,rows", [(128, 64), (384, 512), (192, 300)])
+def test_prefill_stores_the_rounded_rows(model, window, rows):
+    """Layer 0's rows do not depend on the cache: over an 8-bit cache they are the bf16 cache's, rounded."""
+    shape, W, dw = model
+    target = binding.Model(dw, 2, max_rows=rows, max_ctx=512)
+    n = 300
+    tok = i32(synth.make_prompt(n, shape.vocab, batch=2))
+    kv, kv16 = binding.Fp8KVCache(target, 2, 512, window), binding.KVCache(target, 2, 512)
+    kv.data.fill_(255)
+    binding.specdec_prefill(target, kv, tok)
+    binding.specdec_prefill(target, kv16, tok)
+    assert list(kv.read_state()["len"]) == [n - 1] * 2 and kv.read_state()["status"] == 0
+    for b in range(2):
+        ref = kv16.read_context(0, b, 0, n - 1)
+        for got, want in zip(kv.read_context(0, b, 0, n - 1), ref):
+            got, want = _np(got), _np(want)
+            # (bf16 rows of other chunk sizes may differ by an ulp of bf16 where a GEMM sums in another order)
+            ref8 = fp8.stored(want, 256)
+            same = (got == ref8).mean()
+            assert same > 0.98, same
+            assert (np.abs(got - want) <= np.abs(want) * (2.0 ** -4 + 2.0 ** -7) + 2.0 ** -9).all()
+        for got in kv.read_context(1, b, 0, n - 1):
+            assert np.isfinite(_np(got)).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_verify_draft_and_commit(model, fmt):
+    """Whole passes over 8-bit caches against the oracle fed with what the caches
+    hold (the bf16 passes' bound, 2e-2); commits seal what they complete."""
+    torch = torch_cuda()
+    from oracle.quant import int4_model_weights
+    shape, W, dw = model
+    if fmt == "int4":
+        dw = binding.DeviceWeights(shape, W, weight_format="int4")
+        W = int4_model_weights(W)
+    B, g = 2, 4
+    target, draft = binding.Model(dw, 2, max_rows=64, max_ctx=512), binding.Model(dw, 1, max_rows=64, max_ctx=512)
+    kv_t, kv_d = binding.Fp8KVCache(target, B, 512, 128), binding.Fp8KVCache(draft, B, 512, 128)
+    kv_t.data.fill_(255)
+    kv_d.data.fill_(255)
+    prompts = synth.make_prompt(188, shape.vocab, batch=B)
+    binding.specdec_prefill(target, kv_t, i32(prompts))
+    binding.specdec_prefill(draft, kv_d, i32(prompts))
+    sd = binding.SpecDecoder(target, draft, kv_t, kv_d, g, 0.0, seed=3)
+    for step in range(4):
+        st = kv_t.read_state()
+        L, pend = st["len"].copy(), st["pending"][:, 1].copy()
+        log(f"{fmt} step {step}: lengths {L.tolist()}")
+        sd.draft_phase(step)
+        sd.verify_phase(step)
+        torch.cuda.synchronize()
+        logits, d = sd.logits.cpu().numpy(), sd.d.cpu().numpy()
+        for b in range(B):
+            m, c = _oracle_on(shape, W, kv_t, b, int(L[b]))
+            ref = m.forward_block([int(pend[b])] + [int(x) for x in d[b]], int(L[b]), c)
+            assert np.abs(logits[b] - ref).max() < 2e-2
+        before = {(l, b): [_np(t) for t in kv_t.read_context(l, b, 0, int(L[b]))] for l in range(2) for b in range(B)}
+        # rows the commit will take, as the ring holds them
+        A = sd.n_acc.cpu().numpy()
+        fresh = {(l, b): [_np(t) for t in kv_t.read_context(l, b, int(L[b]), int(A[b]) + 1)] for (l, b) in before}
+        sd.commit_phase()
+        st = kv_t.read_state()
+        assert (st["len"] == L + A + 1).all() and st["status"] == 0 and kv_d.read_state()["status"] == 0
+        for (l, b), (k0, v0) in before.items():
+            new = int(st["len"][b])
+            for got, was, row in zip(kv_t.read_context(l, b, 0, new), (k0, v0), fresh[l, b]):
+                got, sealed0, sealed1 = _np(got), int(L[b]) // 64 * 64, new // 64 * 64
+                np.testing.assert_array_equal(got[:sealed0], was[:sealed0])
+                want = np.concatenate([was[sealed0:], row])
+                np.testing.assert_array_equal(got[sealed0:], fp8.stored(want, sealed1 - sealed0))
+
+
+def test_draft_step_logits(model):
+    torch = torch_cuda()
+    shape, W, dw = model
+    draft = binding.Model(dw, 2, max_rows=64, max_ctx=512)
+    kv = binding.Fp8KVCache(draft, 1, 512)
+    prompt = synth.make_prompt(130, shape.vocab)
+    binding.specdec_prefill(draft, kv, i32(prompt))
+    g = 3
+    d = torch.zeros((1, g), dtype=torch.int32, device="cuda")
+    lo = torch.zeros((1, shape.vocab), dtype=torch.float32, device="cuda")
+    for n_pend in (1, 2):
+        L = 130 - n_pend
+        kv.set_state([L], [[int(prompt[0, -2]), int(prompt[0, -1])]], [n_pend])
+        m, c = _oracle_on(shape, W, kv, 0, L)
+        for s in range(g):
+            binding.specdec_draft_step(draft, kv, g, s, 0.0, 0, 0, None, None, d, g, lo)
+            toks = [int(x) for x in prompt[0, -n_pend:]] if s == 0 else [int(d[0, s - 1].item())]
+            ref = m.forward_block(toks, L if s == 0 else L + n_pend + s - 1, c)[-1]
+            assert np.abs(lo.cpu().numpy()[0] - ref).max() < 2e-2
+    assert kv.read_state()["status"] == 0
+
+
+def test_pass_refusals(model):
+    torch = torch_cuda()
+    shape, W, dw = model
+    target = binding.Model(dw, 2, max_rows=256, max_ctx=512)
+    kv = binding.Fp8KVCache(target, 1, 512, 128)
+    d = torch.zeros((1, 70), dtype=torch.int32, device="cuda")
+    lg = torch.empty((1, 71, shape.vocab), dtype=torch.float32, device="cuda")
+    with pytest.raises(binding.SpecdecError) as e:
+        binding.specdec_verify(target, kv, 65, d, 70, lg)  # 66 new rows: the ring takes 65
+    assert e.value.status == -2
+    binding.specdec_verify(target, kv, 64, d, 70, lg)
+    other = binding.Fp8KVCache(dataclasses.replace(shape, n_kv_heads=8), 1, 512)
+    with pytest.raises(binding.SpecdecError) as e:
+        binding.specdec_verify(target, other, 4, d, 70, lg)
+    assert e.value.status == -2
+    tiny = binding.Model(binding.DeviceWeights(synth.TINY, synth.make_weights(synth.TINY)), 1, 16, 128)
+    with pytest.raises(binding.SpecdecError):
+        binding.Fp8KVCache(tiny, 1, 128)  # (float32 models have no 8-bit cache)
