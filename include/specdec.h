@@ -234,10 +234,12 @@ SPECDEC_API specdec_status specdec_kv_init(specdec_kv* kv, const specdec_model* 
  * block is rounded once, when a commit, prefill or specdec_kv_advance
  * completes it, so drafted rows that are rolled back never change a code.
  *  window: a multiple of 64, at least 128.  Verify, draft steps and commits
- *    need gamma + 1 <= window - 63 (SHAPE otherwise), appends n <= window - 63;
+ *    need gamma + 1 <= window - 63 (draft steps gamma <= 64 as well; SHAPE
+ *    otherwise), appends n <= window - 63;
  *    prefill runs in chunks of at most window - 64 tokens per sequence.
  *  capacity: a multiple of 64.  data: 256-byte aligned device memory, at least
- *    specdec_kv_bytes_fp8 bytes, contents unspecified at first.
+ *    specdec_kv_bytes_fp8 bytes (the call zeroes a region of counters in it, the
+ *    rest needs no contents).  At most 128 query heads per kv head.
  *  specdec_kv_set_state may set any length whose last len % 64 positions are
  *    still in the ring: the last `window` positions written (by
  *    specdec_kv_write_context, an append or a pass), less what was written
@@ -245,7 +247,8 @@ SPECDEC_API specdec_status specdec_kv_init(specdec_kv* kv, const specdec_model* 
  * The cache needs the shape alone (desc, first n_layers_used layers), no model
  * handle; a handle of the same n_kv_heads, head_dim and at most n_layers_used
  * layers can use it.  Zeroes the state (asynchronous on stream).
- * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (float32 desc). */
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (float32 desc; capacity * head_dim of
+ * 2^31 or nearly). */
 SPECDEC_API size_t specdec_kv_bytes_fp8(const specdec_model_desc* desc, int32_t n_layers_used, int32_t batch,
                                         int32_t capacity, int32_t window);
 SPECDEC_API specdec_status specdec_kv_init_fp8(specdec_kv* kv, const specdec_model_desc* desc, int32_t n_layers_used,
@@ -294,7 +297,8 @@ SPECDEC_API specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* s
  * ordered on one stream (graphs captured with one, replayed in order).
  * Graph capture: sized from kv->len_upper, as the passes are (see above).
  * Asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (other caches), SHAPE
- * (n_heads not a multiple of n_kv_heads, n > window - 63), KV_CAPACITY. */
+ * (n_heads not a multiple of n_kv_heads or above 128 times it, n > window -
+ * 63), KV_CAPACITY. */
 SPECDEC_API size_t specdec_attention_workspace_bytes(const specdec_kv* kv, int32_t n_heads, int32_t n);
 SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_heads, int32_t n,
                                              const float* q, float* out, void* workspace, size_t workspace_bytes,

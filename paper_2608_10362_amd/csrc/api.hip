@@ -268,13 +268,17 @@ specdec_status check_fp8(const specdec_model_desc* d, int n_layers, int batch, i
     return SPECDEC_ERR_INVALID_ARG;
   if (d->dtype != SPECDEC_BF16) return SPECDEC_ERR_UNSUPPORTED;
   if (capacity % kF8Block || window % kF8Block || window < 2 * kF8Block) return SPECDEC_ERR_SHAPE;
+  if (d->n_heads / d->n_kv_heads > kF8MaxGroup) return SPECDEC_ERR_SHAPE;
+  // (a unit's codes are addressed by 32 bits)
+  if (((size_t)capacity + 1024) * 2 * d->head_dim >= (size_t)1 << 32) return SPECDEC_ERR_UNSUPPORTED;
   return SPECDEC_OK;
 }
 
 specdec_status check_attention(const specdec_kv* kv, int n_heads, int n) {
   if (!kv || !kv->data || !kv->state || n_heads <= 0 || n <= 0) return SPECDEC_ERR_INVALID_ARG;
   if (!is_fp8(kv)) return SPECDEC_ERR_UNSUPPORTED;
-  if (n_heads % kv->n_kv_heads || !ring_holds(kv, n) || n > kv->capacity) return SPECDEC_ERR_SHAPE;
+  if (n_heads % kv->n_kv_heads || n_heads / kv->n_kv_heads > kF8MaxGroup || !ring_holds(kv, n) || n > kv->capacity)
+    return SPECDEC_ERR_SHAPE;
   return SPECDEC_OK;
 }
 
@@ -735,6 +739,7 @@ specdec_status specdec_kv_init_fp8(specdec_kv* kv, const specdec_model_desc* des
   kv->dtype = SPECDEC_FP8;
   kv->window = window;
   kv->len_upper = 0;
+  SD_TRY(launch_kv8_init(kv8_of(kv), (hipStream_t)stream));
   return hip_status(launch_fill_u32((uint32_t*)state, (size_t)specdec_kv_state_count(batch), 0u, (hipStream_t)stream));
 }
 
@@ -908,7 +913,7 @@ specdec_status specdec_draft_step(const specdec_model* draft, specdec_kv* kv, in
   if (temperature > 0.f && !q_out) return SPECDEC_ERR_INVALID_ARG;
   const int B = kv->batch;
   if (kv->len_upper + slot + 2 > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
-  if (!ring_holds(kv, gamma + 1)) return SPECDEC_ERR_SHAPE;
+  if (!ring_holds(kv, gamma + 1) || (is_fp8(kv) && gamma > kF8MaxDraft)) return SPECDEC_ERR_SHAPE;
   hipStream_t s = (hipStream_t)stream;
   RowsArgs ra{};
   if (slot == 0) {

@@ -6,145 +6,213 @@
 //
 // The scores are taken as K Q^T: D[4 (l/16) + r][l % 16] is a key row and a
 // query column, so a lane holds scores of one query, and with the K rows in the
-// cache's order lane group c holds positions 8c .. 8c+7 of a 32-position step,
-// the k order of V: the probabilities feed O^T = V^T P^T from the registers
-// they were made in, and no value crosses lanes but the row maximum.  Codes
-// become bf16 by v_cvt_scalef32_pk_bf16_fp8 (exact); queries and probabilities
-// are split into hi + lo bf16 parts (the result is float32: a bf16 probability
-// alone would be off by 2^-9), so each product runs twice.
+// cache's order lane group c holds positions 8c .. 8c+7 of 32, the k order of V:
+// the probabilities feed O^T = V^T P^T from the registers they were made in,
+// and no value crosses lanes but the row maximum.  Codes become bf16 by
+// v_cvt_scalef32_pk_bf16_fp8 (exact).  Queries and probabilities are float32:
+// each enters its product as three bf16 parts (8 significant bits each, 2^-27
+// left; two parts leave 2^-18, 3.5e-6 of the result over 2048 keys against 7e-7
+// for a float32 computation, one leaves 2^-9).
+//
+// Work: a line of sub-chunks of 32 keys, sequence by sequence, unit by unit (kv
+// head, query tile); workgroup i takes the i-th `per` of them, so all stream the
+// same bytes whatever the lengths, and its NW waves take every NW-th.  Within a
+// unit's segment each wave keeps (max, sum, O), then they merge in LDS.  A unit
+// inside one workgroup is finished there; otherwise each stores its part and
+// the last to count itself adds the parts.
 #include <algorithm>
 
 #include "device_common.h"
 #include "fp8.h"
+#include "gemm_common.h"
 #include "internal.h"
 
 namespace specdec {
 
 namespace {
 
-constexpr int kWaves8 = 4;      // per workgroup, each on a 64-position block of its own
 constexpr int kPartsMax8 = 64;  // parts of one unit (one per lane of the combining wave)
 
-__device__ __forceinline__ void split8(const float (&v)[8], bf16x8& hi, bf16x8& lo) {
+// v as a sum of three bf16 values, each of what the ones before leave.
+__device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&part)[3]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const __bf16 h = (__bf16)v[j];
-    hi[j] = h;
-    lo[j] = (__bf16)(v[j] - (float)h);
+    const float r = v[j] - (float)h;
+    const __bf16 m = (__bf16)r;
+    part[0][j] = h;
+    part[1][j] = m;
+    part[2][j] = (__bf16)(r - (float)m);
   }
 }
 
-__device__ __forceinline__ RowDesc row_of(const AttnArgs& a, int r) {
-  if (a.rows) return a.rows[r];
-  const int b = r / a.rps;
-  return RowDesc{b, a.f8.len[b] + r % a.rps, 0, 1};
-}
-// Blocks of 64 positions sequence b's rows see (its last row bounds them; the
-// host's count where that row is invalid).
-__device__ __forceinline__ int blocks_of(const AttnArgs& a, int b) {
-  const RowDesc last = row_of(a, b * a.rps + a.rps - 1);
-  const int most = (a.max_ctx + kF8Block - 1) / kF8Block;
-  return last.valid ? max(1, min(most, last.pos / kF8Block + 1)) : most;
+// Maximum over the four lane groups of 16 (the same query).
+__device__ __forceinline__ float groups_max(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float m = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// The work is a line: sequence by sequence, unit by unit (kv head, query tile),
-// block by block; workgroup i takes blocks [i * per, (i + 1) * per).
-struct Line {
-  int total, per;
-};
+// Row i of sequence b.
+__device__ __forceinline__ RowDesc row_of(const AttnArgs& a, int b, int i) {
+  if (a.rows) return a.rows[b * a.rps + i];
+  return RowDesc{b, a.f8.len[b] + i, 0, 1};
+}
+// Sub-chunks sequence b's rows see (its last row bounds them; the host's count
+// where that row is invalid).
+__device__ __forceinline__ int subs_of(const AttnArgs& a, int b) {
+  const RowDesc last = row_of(a, b, a.rps - 1);
+  const int most = (a.max_ctx + kF8Sub - 1) / kF8Sub;
+  return last.valid ? max(1, min(most, last.pos / kF8Sub + 1)) : most;
+}
+
 __device__ __forceinline__ int lane_sum(int v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
   return __builtin_amdgcn_readfirstlane(v);
 }
-__device__ __forceinline__ Line line_of(const AttnArgs& a, int B, int U, int nwg, int n0) {
-  const int lane = threadIdx.x & 63;
-  int t = 0;
-  for (int c = 0; c < B; c += kWave) t += lane_sum(c == 0 ? n0 : (c + lane < B ? blocks_of(a, c + lane) : 0));
-  const int most = (a.max_ctx + kF8Block - 1) / kF8Block;
-  Line l;
-  l.total = t * U;
-  l.per = max((l.total + nwg - 1) / nwg, (most + kPartsMax8 - 3) / (kPartsMax8 - 2));
-  return l;
+
+// Agent-scope accesses of the parts: visible to a combining workgroup on any XCD
+// once completed.
+__device__ __forceinline__ void put2(float* p, float x, float y) {
+  __hip_atomic_store((unsigned long long*)p, ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// Blocks before sequence b on the line of one unit.
-__device__ __forceinline__ int before_of(const AttnArgs& a, int b, int n0) {
-  const int lane = threadIdx.x & 63;
-  int t = 0;
-  for (int c = 0; c < b; c += kWave) t += lane_sum(c + lane >= b ? 0 : (c == 0 ? n0 : blocks_of(a, c + lane)));
-  return t;
+__device__ __forceinline__ float2 get2(const float* p) {
+  const unsigned long long v =
+      __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-__device__ __forceinline__ void put_row(const AttnArgs& a, int row, int head, int d, float v) {
-  if (a.xs) put_stacked(a.xs, a.stt, row, head * a.head_dim + d, v);
-  else a.o[((size_t)row * a.n_heads + head) * a.head_dim + d] = v;
+// Four consecutive dims of the output of row i of sequence b, o * inv (0 for an invalid row).
+__device__ __forceinline__ void finish_row(const AttnArgs& a, int b, int i, int head, int d, f32x4 o, float inv) {
+  const RowDesc rd = row_of(a, b, i);
+  const int row = b * a.rps + i;
+  if (!rd.valid) o = f32x4{0.f, 0.f, 0.f, 0.f};
+  else o *= inv;
+  if (rd.valid && rd.pos + 1 > a.max_ctx && d == 0) set_status(a.status, kStatusKvCapacity);  // the host's bound was wrong
+  if (a.xs) put_stacked4(a.xs, a.stt, row, head * a.head_dim + d, o);
+  else *(f32x4_a4*)(a.o + ((size_t)row * a.n_heads + head) * a.head_dim + d) = o;
 }
 
+// n / d for 0 <= n < 2^20 by the reciprocal of d (the quotient plus half a step
+// is far from the next whole number compared with the product's rounding).
+__device__ __forceinline__ int div_small(int n, float inv) { return (int)(((float)n + 0.5f) * inv); }
+
+constexpr int kWaves8 = 8;  // per workgroup
+
+// LDS: the queries' parts; then ring rows (a K fragment per tile and step, V's
+// fragments), one slot per sub-chunk in work, reused by the merge.  With one
+// query tile a wave (at most 64 rows, at most 65 of them not committed) at most
+// 4 sub-chunks of a sequence lie in the ring (63 + 65 rows from a multiple of
+// 64), sub-chunk j in slot j % 4; otherwise a slot per wave.
 template <int HD, int QT>
-__global__ __launch_bounds__(64 * kWaves8, QT > 2 ? 1 : 2) void attn8_kernel(AttnArgs a, int n_tiles, int parts) {
-  constexpr int KST = HD / 32, DT = HD / 16, F = HD / 16, OS = HD + 4, NW = kWaves8;
-  __shared__ float s_o[NW][16][OS];
-  __shared__ float s_ml[NW][16][2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c16 = lane & 15, grp = lane >> 4;
-  const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, nq = rps * group, B = a.M / rps;
-  const int U = G * n_tiles, window = a.f8.ring.capacity;
-  const int n0 = lane < B ? blocks_of(a, lane) : 0;  // (the first 64 sequences stay in a register)
-  const Line ln = line_of(a, B, U, (int)gridDim.x, n0);
-  auto blocks = [&](int s) { return s < kWave ? __builtin_amdgcn_readlane(n0, s) : blocks_of(a, s); };
-  int x = (int)blockIdx.x * ln.per;
-  const int hi = min(ln.total, x + ln.per);
+struct Lds8 {
+  static constexpr int KST = HD / 32, DT = HD / 16, OS = HD + 4, NW = kWaves8, NR = QT == 1 ? 4 : NW;
+  bf16x8 q[QT][KST][3][kWave];
+  union {
+    u32x4 ring[NR][2 * KST + DT][kWave];
+    struct {
+      float o[NW][16][OS];
+      float ml[NW][16][2];
+    } m;
+  };
+  int last;
+};
+
+// Workgroups: LINE: the line of all units' sub-chunks, `per` to a workgroup (x);
+// otherwise part x of unit y of sequence z, every part of a sequence `per` long.
+template <int HD, int QT, bool LINE>
+__global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(AttnArgs a, int n_tiles, int parts, int per0) {
+  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, RK = 2 * KST, NW = kWaves8;
+  __shared__ Lds8<HD, QT> sh;
+  const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, nq = rps * group;
+  const int window = a.f8.ring.capacity;
   const float qscale = 1.44269504088896341f / sqrtf((float)HD);  // (scores in powers of two)
+  const float inv_group = 1.0f / (float)group;
 
-  int b = 0, base = 0, nb = blocks(0);  // the sequence that holds x; base: the line where it starts
-  while (x < hi) {
-    while (x >= base + nb * U) {
-      base += nb * U;
-      ++b;
-      nb = blocks(b);
-    }
-    const int u = (x - base) / nb, k_lo = (x - base) % nb, k_hi = min(nb, k_lo + (hi - x));
-    const int unit0 = base + u * nb;  // the line where the unit starts
-    const int g = u / n_tiles, tile = u % n_tiles;
-    x += k_hi - k_lo;
-    const int sealed = (a.f8.len[b] + a.c0) / kF8Block;
+  // One segment: sub-chunks [k_lo, k_hi) of unit (b, g, tile), part `part` of its n.
+  auto segment = [&](int b, int g, int tile, int k_lo, int k_hi, int part, int n) {
+    // (opaque: what a segment derives from it stays in the segment, not in registers across all of them)
+    int lane = lane0;
+    asm volatile("" : "+v"(lane));
+    const int c16 = lane & 15, grp = lane >> 4;
+    const int sealed = (a.f8.len[b] + a.c0) / kF8Block * (kF8Block / kF8Sub);
+    if (QT == 1) k_hi = min(k_hi, sealed + 4);  // (no valid row is past it: the ring's slots)
 
-    // This lane's query of each tile, its position, and the tiles' position range.
-    int qpos[QT];
-    bf16x8 qhi[QT][KST], qlo[QT][KST];
-    int vis = 0, lowest = 0x7fffffff;
+    // Codes and scales through buffer descriptors that end with the sealed ones: a
+    // wave's loads past its last sub-chunk read nothing, so none needs a branch
+    // (with one, the compiler waits for every load at the loop's head).
+    const int j_sealed = min(k_hi, sealed);
+    const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, b, g), (uint32_t)j_sealed * 2 * kF8Sub * HD);
+    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, b, g), (uint32_t)((j_sealed + 1) & ~1) * 4);
+    u32x4 kc[FS], vc[FS];
+    float ks, vs;
+    auto load_k = [&](int j) {
+      const uint32_t at = (uint32_t)j * 2 * kF8Sub * HD + lane * 16;
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-      const int qa = (tile * QT + q) * 16 + c16;
-      const bool in = qa < nq;
-      const int row = b * rps + (in ? qa / group : 0), head = g * group + (in ? qa % group : 0);
-      const RowDesc rd = row_of(a, row);
-      qpos[q] = in && rd.valid ? rd.pos : -1;
-      if (qpos[q] >= 0) {
-        vis = max(vis, qpos[q] + 1);
-        lowest = min(lowest, qpos[q]);
-      }
-      const float* qp = a.qr + ((size_t)row * H + head) * HD;
+      for (int f = 0; f < FS; ++f) kc[f] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + f * 1024, 0, 0));
+      ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j & ~1) * 4, 0, 0));
+    };
+    auto load_v = [&](int j) {
+      const uint32_t at = (uint32_t)j * 2 * kF8Sub * HD + kF8Sub * HD + lane * 16;
 #pragma unroll
-      for (int s = 0; s < KST; ++s) {
-        const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
-        const f32x4 v0 = *(const f32x4_a4*)(qp + d), v1 = *(const f32x4_a4*)(qp + d + 4);
-        float v[8];
+      for (int f = 0; f < FS; ++f) vc[f] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + f * 1024, 0, 0));
+      vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j | 1) * 4, 0, 0));
+    };
+    // The ring's rows go to this wave's part of LDS without passing the registers.
+    const uint16_t* ring = k_block<uint16_t>(a.f8.ring, a.layer, b, g);
+    auto slot_of = [&](int j) { return QT == 1 ? j & 3 : wave; };
+    auto load_ring = [&](int j) {
+      const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&sh.ring[slot_of(j)][0][0];
+      const __amdgpu_buffer_rsrc_t rr = make_rsrc(ring, (uint32_t)window * HD * 4u);
+      int l = lane;
+      asm volatile("" : "+v"(l));  // (addresses computed here, not kept)
+      const int w0 = j * kF8Sub % window, i = l & 15, c = l >> 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[j] = in ? v0[j] * qscale : 0.f;
-          v[4 + j] = in ? v1[j] * qscale : 0.f;
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < KST; ++s) {
+          const int d = HD >= 64 ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 32 * s + 8 * c;
+          const int pos = w0 + 8 * (i >> 2) + 4 * t + (i & 3);
+          load_lds16(lds0 + (t * KST + s) * 1024u, (uint32_t)KvIndex<uint16_t>::k(pos, d, HD, window) * 2u, rr);
         }
-        split8(v, qhi[q][s], qlo[q][s]);
-      }
-    }
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) {
-      vis = max(vis, __shfl_xor(vis, o, kWave));
-      lowest = min(lowest, __shfl_xor(lowest, o, kWave));
+      for (int dt = 0; dt < DT; ++dt)
+        load_lds16(lds0 + (RK + dt) * 1024u, (uint32_t)KvIndex<uint16_t>::v(w0 + 8 * c, 16 * dt + i, HD, window) * 2u, rr);
+    };
+
+    // This wave's sub-chunks: j, j + NW, ...; the first codes, and the first ring
+    // rows, are on their way while the queries are made ready.
+    int j = k_lo + wave;
+    int jr = max(j, j + (sealed - j + NW - 1) / NW * NW);  // the first of them in the ring
+    if (jr < k_hi) load_ring(jr);
+    load_k(j);
+    load_v(j);
+
+    for (int i = wave; i < QT * KST; i += NW) {  // (wave-uniform) one 32-dim step of one tile
+      const int q = i / KST, s = i % KST, qa = (tile * QT + q) * 16 + c16;
+      const bool in = qa < nq;
+      const int qr = in ? div_small(qa, inv_group) : 0;
+      const int row = b * rps + qr, head = g * group + (in ? qa - qr * group : 0);
+      const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
+      const float* qp = a.qr + ((size_t)row * H + head) * HD + d;
+      const f32x4 v0 = *(const f32x4_a4*)qp, v1 = *(const f32x4_a4*)(qp + 4);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = in ? v0[e] * qscale : 0.f;
+        v[4 + e] = in ? v1[e] * qscale : 0.f;
+      }
+      bf16x8 p3[3];
+      split8(v, p3);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) sh.q[q][s][k][lane] = p3[k];
     }
-    vis = __builtin_amdgcn_readfirstlane(vis);
-    lowest = __builtin_amdgcn_readfirstlane(lowest);
+    __syncthreads();
 
     floatx4 of[QT][DT];
     float mx[QT], sm[QT];
@@ -155,15 +223,29 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 2 ? 1 : 2) void attn8_kernel(Att
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) of[q][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    // New scores of tile q: the running maximum and sum,
-    // then the scores become probabilities relative to it.
-    auto softmax = [&](int q, auto& p) {
-      constexpr int n = sizeof(p) / sizeof(float);
-      float m = p[0];
+    // kk(t, s): K rows of tile t, dims of step s; the scores of this lane's 8 positions, tile by tile.
+    auto scores = [&](auto kk, floatx4 (&acc)[QT][2]) {
+      int ql = lane;
+      asm volatile("" : "+v"(ql));  // (the queries stay in LDS: hoisted out of the loop they would fill the registers)
 #pragma unroll
-      for (int j = 1; j < n; ++j) m = fmaxf(m, p[j]);
-      m = fmaxf(m, __shfl_xor(m, 16, kWave));
-      m = fmaxf(m, __shfl_xor(m, 32, kWave));
+      for (int q = 0; q < QT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KST; ++s) {
+        const bf16x8 k0 = kk(0, s), k1 = kk(1, s);
+#pragma unroll
+        for (int k = 2; k >= 0; --k)  // (small parts first)
+#pragma unroll
+          for (int q = 0; q < QT; ++q) {
+            const bf16x8 qq = sh.q[q][s][k][ql];
+            acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qq, acc[q][0], 0, 0, 0);
+            acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qq, acc[q][1], 0, 0, 0);
+          }
+      }
+    };
+    // The running maximum and sum of tile q over 8 new scores, which become probabilities relative to it.
+    auto softmax = [&](int q, float (&p)[8]) {
+      float m = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+      m = groups_max(m);
       const float mnew = fmaxf(mx[q], m);
       if (__any(mnew > mx[q])) {  // (rescaled only where a maximum rose)
         const float alpha = mx[q] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx[q] - mnew);
@@ -173,166 +255,141 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 2 ? 1 : 2) void attn8_kernel(Att
         mx[q] = mnew;
       }
 #pragma unroll
-      for (int j = 0; j < n; ++j) {
+      for (int e = 0; e < 8; ++e) {
         // (a query that has seen no key yet keeps the maximum -inf)
-        p[j] = mx[q] == -INFINITY && p[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p[j] - mx[q]);
-        sm[q] += p[j];
+        p[e] = mx[q] == -INFINITY && p[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p[e] - mx[q]);
+        sm[q] += p[e];
       }
     };
 
-    for (int kb = k_lo + wave; kb < k_hi; kb += NW) {  // (wave-uniform)
-      if (kb < sealed) {  // codes: every query sees the whole block
-        const unsigned char* codes = a.f8.code_base(a.layer, b, g) + (size_t)kb * 2 * kF8Block * HD + lane * 16;
-        const float* sc = a.f8.scale_base(a.layer, b, g) + 2 * (size_t)kb;
-        u32x4 kc[F], vc[F];
+    for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
+      floatx4 acc[QT][2];
+      scores(
+          [&](int t, int s) {
+            const u32x4 w = HD >= 64 ? kc[t * (HD / 64) + s / 2] : kc[0];
+            const int h = HD >= 64 ? s & 1 : t;
+            return fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
+          },
+          acc);
+      // (a wave's next K is on its way through the softmax and P V, its next V through the next scores)
+      load_k(j + NW);
+      bf16x8 pp[QT][3];
 #pragma unroll
-        for (int f = 0; f < F; ++f) kc[f] = *(const u32x4*)(codes + f * 1024);
+      for (int q = 0; q < QT; ++q) {
+        float p[8];
 #pragma unroll
-        for (int f = 0; f < F; ++f) vc[f] = *(const u32x4*)(codes + kF8Block * HD + f * 1024);
-        const float ks = sc[0], vs = sc[1];
-        float p[QT][16];
+        for (int e = 0; e < 8; ++e) p[e] = acc[q][e >> 2][e & 3];
+        softmax(q, p);
+        split8(p, pp[q]);
+      }
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+      for (int dt = 0; dt < DT; ++dt) {
+        const bf16x8 vv = fp8x8_to_bf16(vc[dt / 2][2 * (dt & 1)], vc[dt / 2][2 * (dt & 1) + 1], vs);
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            floatx4 acc[QT];
+        for (int k = 2; k >= 0; --k)
 #pragma unroll
-            for (int q = 0; q < QT; ++q) acc[q] = floatx4{0.f, 0.f, 0.f, 0.f};
+          for (int q = 0; q < QT; ++q)
+            of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pp[q][k], of[q][dt], 0, 0, 0);
+      }
+      load_v(j + NW);
+    }
+
+    if (jr < k_hi) {  // the ring
+      // This lane's query of each tile: its position; the tiles' range.
+      int qpos[QT], vis = 0, lowest = 0x7fffffff;
 #pragma unroll
-            for (int st = 0; st < KST; ++st) {
-              bf16x8 kk;
-              if constexpr (HD >= 64) {
-                const u32x4 w = kc[(2 * s + t) * (HD / 64) + st / 2];
-                kk = fp8x8_to_bf16(w[2 * (st & 1)], w[2 * (st & 1) + 1], ks);
-              } else {
-                kk = fp8x8_to_bf16(kc[s][2 * t], kc[s][2 * t + 1], ks);
-              }
+      for (int q = 0; q < QT; ++q) {
+        const int qa = (tile * QT + q) * 16 + c16;
+        const RowDesc rd = row_of(a, b, qa < nq ? div_small(qa, inv_group) : 0);
+        qpos[q] = qa < nq && rd.valid ? rd.pos : -1;
+        if (qpos[q] >= 0) {
+          vis = max(vis, qpos[q] + 1);
+          lowest = min(lowest, qpos[q]);
+        }
+      }
 #pragma unroll
-              for (int q = 0; q < QT; ++q) {
-                acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qhi[q][st], acc[q], 0, 0, 0);
-                acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qlo[q][st], acc[q], 0, 0, 0);
-              }
-            }
+      for (int o = 1; o < 16; o <<= 1) {
+        vis = max(vis, __shfl_xor(vis, o, kWave));
+        lowest = min(lowest, __shfl_xor(lowest, o, kWave));
+      }
+      vis = __builtin_amdgcn_readfirstlane(vis);
+      lowest = __builtin_amdgcn_readfirstlane(lowest);
+      for (;;) {
+        const int k0 = jr * kF8Sub;
+        const u32x4(*rows)[kWave] = sh.ring[slot_of(jr)];
+        if (k0 >= vis) {
+          wait_vm<0>();  // (its rows' loads to LDS have ended)
+          break;
+        }
+        wait_vm<0>();
+        __builtin_amdgcn_wave_barrier();
+        floatx4 acc[QT][2];
+        scores([&](int t, int s) { return __builtin_bit_cast(bf16x8, rows[t * KST + s][lane]); }, acc);
+        bool odd = false;  // a NaN or infinity among the V entries seen
+        // Slots past the newest visible position hold stale values: their V entries
+        // are zeroed, never multiplied by a zero probability.
+        const int nvalid = vis - (k0 + 8 * grp);
+        auto v_of = [&](int dt, bool finite_only) {
+          u32x4 v = rows[RK + dt][lane];
 #pragma unroll
-            for (int q = 0; q < QT; ++q)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) p[q][8 * s + 4 * t + r] = acc[q][r];
+          for (int w = 0; w < 4; ++w) {
+            if (2 * w >= nvalid) v[w] = 0u;
+            else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
+            const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
+            odd |= lo || up;
+            if (finite_only && lo) v[w] &= 0xffff0000u;
+            if (finite_only && up) v[w] &= 0xffffu;
           }
-        bf16x8 phi[QT][2], plo[QT][2];
+          return v;
+        };
+        // A NaN or infinity that only later rows see must not reach the others
+        // through 0 * inf: where some query does not see all, such entries leave the
+        // product and are added by themselves to the queries that see them.
+        const bool diagonal = k0 + kF8Sub - 1 > lowest;
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-          softmax(q, p[q]);
+          float p[8];
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            float v[8];
+          for (int e = 0; e < 8; ++e) p[e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
+          softmax(q, p);
+          bf16x8 pp[3];
+          split8(p, pp);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = p[q][8 * s + j];
-            split8(v, phi[q][s], plo[q][s]);
+          for (int dt = 0; dt < DT; ++dt) {
+            const bf16x8 vv = __builtin_bit_cast(bf16x8, v_of(dt, diagonal));
+#pragma unroll
+            for (int k = 2; k >= 0; --k)
+              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pp[k], of[q][dt], 0, 0, 0);
           }
-        }
+          if (diagonal && __any(odd)) {
+            for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
+              float pi = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+              for (int e = 0; e < 8; ++e) pi = (i & 7) == e ? p[e] : pi;
+              pi = __shfl(pi, 16 * (i >> 3) + c16, kWave);
+              // (V fragment dt: lane 16 (i / 8) + d, entry i % 8)
+              const uint16_t* vrow = (const uint16_t*)&rows[RK][16 * (i >> 3)] + (i & 7);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const bf16x8 vv = fp8x8_to_bf16(vc[dt][2 * s], vc[dt][2 * s + 1], vs);
+              for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int q = 0; q < QT; ++q) {
-              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, phi[q][s], of[q][dt], 0, 0, 0);
-              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, plo[q][s], of[q][dt], 0, 0, 0);
-            }
-          }
-      } else {  // the ring, 32 positions at a time
-        const uint16_t* kr = k_block<uint16_t>(a.f8.ring, a.layer, b, g);
-        for (int s = 0; s < 2; ++s) {
-          const int k0 = kb * kF8Block + 32 * s, w0 = k0 % window;
-          if (k0 >= vis) break;
-          u32x4 vf[DT];
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            vf[dt] = *(const u32x4*)(kr + KvIndex<uint16_t>::v(w0 + 8 * grp, 16 * dt + c16, HD, window));
-          float p[QT][8];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            floatx4 acc[QT];
-#pragma unroll
-            for (int q = 0; q < QT; ++q) acc[q] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int st = 0; st < KST; ++st) {
-              const int d = HD >= 64 ? 64 * (st >> 1) + 16 * grp + 8 * (st & 1) : 32 * st + 8 * grp;
-              const int pos = w0 + 8 * (c16 >> 2) + 4 * t + (c16 & 3);
-              const bf16x8 kk = __builtin_bit_cast(bf16x8, *(const u32x4*)(kr + KvIndex<uint16_t>::k(pos, d, HD, window)));
-#pragma unroll
-              for (int q = 0; q < QT; ++q) {
-                acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qhi[q][st], acc[q], 0, 0, 0);
-                acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qlo[q][st], acc[q], 0, 0, 0);
-              }
-            }
-#pragma unroll
-            for (int q = 0; q < QT; ++q)
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                p[q][4 * t + r] = k0 + 8 * grp + 4 * t + r > qpos[q] ? -INFINITY : acc[q][r];
-          }
-          // Slots past the newest visible position hold stale values: their V
-          // entries are zeroed, never multiplied by a zero probability.
-          const int nvalid = vis - (k0 + 8 * grp);
-          bool odd = false;  // a NaN or infinity among the V entries
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              if (2 * w >= nvalid) vf[dt][w] = 0u;
-              else if (2 * w + 1 >= nvalid) vf[dt][w] &= 0xffffu;
-              odd |= (vf[dt][w] & 0x7f80u) == 0x7f80u || (vf[dt][w] & 0x7f800000u) == 0x7f800000u;
-            }
-          // One that only later rows see must not reach the others through
-          // 0 * inf: such entries leave the product and are added by themselves
-          // to the queries that see them.
-          const bool apart = k0 + 31 > lowest && __any(odd);
-          if (apart) {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                if ((vf[dt][w] & 0x7f80u) == 0x7f80u) vf[dt][w] &= 0xffff0000u;
-                if ((vf[dt][w] & 0x7f800000u) == 0x7f800000u) vf[dt][w] &= 0xffffu;
-              }
-          }
-#pragma unroll
-          for (int q = 0; q < QT; ++q) {
-            softmax(q, p[q]);
-            bf16x8 phi, plo;
-            split8(p[q], phi, plo);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              const bf16x8 vv = __builtin_bit_cast(bf16x8, vf[dt]);
-              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, phi, of[q][dt], 0, 0, 0);
-              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, plo, of[q][dt], 0, 0, 0);
-            }
-            if (apart) {
-              for (int j = 0; j < 32; ++j) {  // (position k0 + j; its probability lies in lane group j / 8)
-                float pj = 0.f;
-#pragma unroll
-                for (int t = 0; t < 8; ++t) pj = (j & 7) == t ? p[q][t] : pj;
-                pj = __shfl(pj, 16 * (j >> 3) + c16, kWave);
-                if (k0 + j > qpos[q]) continue;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                  for (int r = 0; r < 4; ++r) {
-                    const float v = bf16_bits_to_f32(kr[KvIndex<uint16_t>::v(w0 + j, 16 * dt + 4 * grp + r, HD, window)]);
-                    if (!isfinite(v)) of[q][dt][r] += pj * v;
-                  }
-              }
+                for (int r = 0; r < 4; ++r) {
+                  const float v = bf16_bits_to_f32(vrow[(size_t)dt * kWave * 8 + (4 * grp + r) * 8]);
+                  if (k0 + i <= qpos[q] && !isfinite(v)) of[q][dt][r] += pi * v;
+                }
             }
           }
         }
+        jr += NW;
+        if (jr >= k_hi) break;
+        __builtin_amdgcn_wave_barrier();  // (every lane is done with these rows)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load_ring(jr);
       }
     }
 
-    // Merge the waves of this segment, tile by tile, in LDS (fixed order).
-    const bool whole = k_lo == 0 && k_hi == nb;
-    const int part = (int)blockIdx.x - unit0 / ln.per;
+    // Merge the waves of this segment in LDS, tile by tile (fixed order).
+    // Thread: 4 dims of a row.
+    const bool whole = n == 1;
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
       const int n_here = min(16, nq - (tile * QT + q) * 16);
@@ -340,93 +397,146 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 2 ? 1 : 2) void attn8_kernel(Att
       float sum = sm[q];
       sum += __shfl_xor(sum, 16, kWave);
       sum += __shfl_xor(sum, 32, kWave);
-      __syncthreads();  // (the tile or segment before is read out)
+      __syncthreads();  // (the ring's rows, or the tile before, are read)
+      if (c16 < n_here) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *(floatx4*)&s_o[wave][c16][16 * dt + 4 * grp] = of[q][dt];
-      if (grp == 0) {
-        s_ml[wave][c16][0] = mx[q];
-        s_ml[wave][c16][1] = sum;
+        for (int dt = 0; dt < DT; ++dt) *(floatx4*)&sh.m.o[wave][c16][16 * dt + 4 * grp] = of[q][dt];
+        if (grp == 0) {
+          sh.m.ml[wave][c16][0] = mx[q];
+          sh.m.ml[wave][c16][1] = sum;
+        }
       }
       __syncthreads();
-      for (int i = wave; i < n_here; i += NW) {
-        float M = -INFINITY, L = 0.f, e[NW];
+      const int d = threadIdx.x % (HD / 4) * 4;
+      for (int i = threadIdx.x / (HD / 4); i < n_here; i += 64 * NW / (HD / 4)) {
+        float M = -INFINITY, L = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, s_ml[w][i][0]);
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, sh.m.ml[w][i][0]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          // (a wave without keys: maximum -inf, sum and outputs 0; NaN scores leave the maximum -inf but a NaN sum)
-          const float m = s_ml[w][i][0], l = s_ml[w][i][1];
-          e[w] = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - M);
-          L += e[w] * l;
+          // (a wave without keys: maximum -inf, sum and outputs 0; NaN scores alone: maximum -inf, a NaN sum)
+          const float m = sh.m.ml[w][i][0], l = sh.m.ml[w][i][1];
+          const float e = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - M);
+          L += e * l;
+          o += e * *(const f32x4*)&sh.m.o[w][i][d];
         }
-        const int qa = (tile * QT + q) * 16 + i, row = b * rps + qa / group, head = g * group + qa % group;
-        const RowDesc rd = row_of(a, row);
-        if (rd.valid && rd.pos + 1 > a.max_ctx && lane == 0) set_status(a.status, kStatusKvCapacity);  // the host's bound was wrong
-        const size_t slot = ((size_t)row * H + head) * parts + part;
-        for (int d = lane; d < HD; d += kWave) {
-          float o = 0.f;
-#pragma unroll
-          for (int w = 0; w < NW; ++w) o += e[w] * s_o[w][i][d];
-          if (whole) put_row(a, row, head, d, rd.valid ? o / L : 0.f);
-          else a.o_part[slot * HD + d] = o;
-        }
-        if (!whole && lane == 0) {
-          a.ml_part[2 * slot] = M;
-          a.ml_part[2 * slot + 1] = L;
+        const int qa = (tile * QT + q) * 16 + i, qr = div_small(qa, inv_group);
+        const int row = b * rps + qr, head = g * group + qa - qr * group;
+        if (whole) {
+          finish_row(a, b, qr, head, d, o, 1.0f / L);
+        } else {
+          const size_t slot = ((size_t)row * H + head) * parts + part;
+          put2(a.o_part + slot * HD + d, o[0], o[1]);
+          put2(a.o_part + slot * HD + d + 2, o[2], o[3]);
+          if (d == 0) put2(a.ml_part + 2 * slot, M, L);
         }
       }
+    }
+
+    // The last workgroup of a unit that spans several adds its parts: one wave a
+    // row, lane p the (max, sum) of part p, then LP lanes of 4 dims per part.
+    if (!whole) {
+      uint32_t* ctr = a.f8.counters + ((size_t)b * G + g) * n_tiles + tile;
+      wait_vm<0>();  // (this wave's stores have completed)
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const uint32_t old = __hip_atomic_fetch_add(ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sh.last = old == (uint32_t)(n - 1);
+        if (sh.last) __hip_atomic_store(ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      if (sh.last) {
+        constexpr int LP = HD / 4, PI = kWave / LP, BT = 8;  // parts a load covers, loads in flight
+        const int n_rows = min(16 * QT, nq - tile * QT * 16);
+        for (int i = wave; i < n_rows; i += NW) {  // (wave-uniform)
+          const int qa = tile * QT * 16 + i, qr = div_small(qa, inv_group), head = g * group + qa - qr * group;
+          const size_t slot = ((size_t)(b * rps + qr) * H + head) * parts;
+          const float2 ml = lane < n ? get2(a.ml_part + 2 * (slot + lane)) : make_float2(-INFINITY, 0.f);
+          const int pg = lane / LP, d = lane % LP * 4;
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+          float wgt = 0.f, inv = 0.f;
+          for (int p0 = 0; p0 < n; p0 += BT * PI) {
+            float2 lo[BT], up[BT];
+#pragma unroll
+            for (int k = 0; k < BT; ++k) {
+              const float* src = a.o_part + (slot + min(p0 + k * PI + pg, n - 1)) * HD + d;
+              lo[k] = get2(src);
+              up[k] = get2(src + 2);
+            }
+            if (p0 == 0) {
+              const float M = wave_max(ml.x);
+              wgt = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
+              inv = 1.0f / wave_sum(wgt * ml.y);
+            }
+#pragma unroll
+            for (int k = 0; k < BT; ++k) {
+              const int p = p0 + k * PI + pg;
+              const float w = __shfl(wgt, p & 63, kWave);
+              if (p < n) acc += w * f32x4{lo[k].x, lo[k].y, up[k].x, up[k].y};
+            }
+          }
+#pragma unroll
+          for (int o = LP; o < kWave; o <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, kWave);
+          if (lane < LP) finish_row(a, b, qr, head, d, acc, inv);
+        }
+      }
+    }
+  };
+
+  if constexpr (!LINE) {
+    const int b = blockIdx.z, u = blockIdx.y, part = blockIdx.x;
+    const int nb = subs_of(a, b), k_lo = part * per0;
+    if (k_lo >= nb) return;  // (workgroup-uniform)
+    const int g = u / n_tiles;
+    segment(b, g, u - g * n_tiles, k_lo, min(nb, k_lo + per0), part, (nb + per0 - 1) / per0);
+  } else {
+    const int B = a.M / rps, U = G * n_tiles;
+    const int n0 = lane0 < B ? subs_of(a, lane0) : 0;  // (the first 64 sequences stay in a register)
+    int total = 0;
+    for (int c = 0; c < B; c += kWave) total += lane_sum(c == 0 ? n0 : (c + lane0 < B ? subs_of(a, c + lane0) : 0));
+    total *= U;
+    const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, per0);
+    auto subs = [&](int s) { return s < kWave ? __builtin_amdgcn_readlane(n0, s) : subs_of(a, s); };
+    int x = (int)blockIdx.x * per;
+    const int hi = min(total, x + per);
+    int b = 0, base = 0, nb = subs(0);  // the sequence that holds x; base: the line where it starts
+    while (x < hi) {
+      while (x >= base + nb * U) {
+        base += nb * U;
+        ++b;
+        nb = subs(b);
+      }
+      const int u = (x - base) / nb, unit0 = base + u * nb;  // unit0: the line where the unit starts
+      const int k_lo = x - unit0, k_hi = min(nb, k_lo + (hi - x)), first = unit0 / per, g = u / n_tiles;
+      x += k_hi - k_lo;
+      segment(b, g, u - g * n_tiles, k_lo, k_hi, (int)blockIdx.x - first, (unit0 + nb - 1) / per - first + 1);
+      __syncthreads();  // (LDS is free for the next segment)
     }
   }
 }
 
-// Grid (heads, rows), one wave: adds the parts of a (row, head) whose unit
-// spans workgroups.
-template <int HD>
-__global__ __launch_bounds__(64) void attn8_combine_kernel(AttnArgs a, int n_tiles, int qt, int parts, int nwg) {
-  const int head = blockIdx.x, row = blockIdx.y, lane = threadIdx.x;
-  const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, B = a.M / rps, b = row / rps;
-  const int n0 = lane < B ? blocks_of(a, lane) : 0;
-  const Line ln = line_of(a, B, G * n_tiles, nwg, n0);
-  const int nb = b < kWave ? __builtin_amdgcn_readlane(n0, b) : blocks_of(a, b), tile = ((row % rps) * group + head % group) / (16 * qt);
-  const int unit0 = before_of(a, b, n0) * G * n_tiles + ((head / group) * n_tiles + tile) * nb;
-  const int first = unit0 / ln.per, n = (unit0 + nb - 1) / ln.per - first + 1;
-  if (n == 1) return;  // (finished by its workgroup)
-  const RowDesc rd = row_of(a, row);
-  const size_t slot = ((size_t)row * H + head) * parts;
-  const float m = lane < n ? a.ml_part[2 * (slot + lane)] : -INFINITY, l = lane < n ? a.ml_part[2 * (slot + lane) + 1] : 0.f;
-  const float M = wave_max(m);
-  const float e = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - M);
-  const float inv = 1.0f / wave_sum(e * l);
-  constexpr int DPL = HD >= 64 ? HD / 64 : 1;
-  float acc[DPL] = {};
-  for (int p = 0; p < n; ++p) {
-    const float w = __shfl(e, p, kWave);
-#pragma unroll
-    for (int j = 0; j < DPL; ++j)
-      if (lane + 64 * j < HD) acc[j] += w * a.o_part[(slot + p) * HD + lane + 64 * j];
-  }
-#pragma unroll
-  for (int j = 0; j < DPL; ++j)
-    if (lane + 64 * j < HD) put_row(a, row, head, lane + 64 * j, rd.valid ? acc[j] * inv : 0.f);
-}
-
-// Query tiles of 16 a wave takes at once (they share a block's codes).
-int query_tiles(int nq) { return nq <= 16 ? 1 : (nq <= 32 ? 2 : 4); }
-
 struct Plan {
-  int qt, n_tiles, nwg, parts;
+  int qt, n_tiles, line, nwg, per, parts;
 };
 Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int max_ctx) {
   Plan p;
   const int nq = rps * (n_heads / n_kv_heads);
-  p.qt = query_tiles(nq);
+  p.qt = nq <= 64 ? 1 : 2;
   p.n_tiles = (nq + 16 * p.qt - 1) / (16 * p.qt);
-  const long nb = (max_ctx + kF8Block - 1) / kF8Block, units = (long)n_kv_heads * p.n_tiles;
-  const long most = nb * units * batch;
-  // one block a wave until the card is full, then 2 workgroups a CU
-  p.nwg = (int)std::max(1L, std::min((most + kWaves8 - 1) / kWaves8, 2L * device_compute_units()));
-  // a unit of the longest sequence spans at most this many workgroups, whatever the other lengths
-  p.parts = (int)std::min<long>({nb, p.nwg / units + 2, (long)kPartsMax8});
+  const long nb = (max_ctx + kF8Sub - 1) / kF8Sub, units = (long)n_kv_heads * p.n_tiles;
+  const long slots = (p.qt == 1 ? 2L : 1L) * device_compute_units();  // workgroups resident at once
+  const long per = std::max((nb * units * batch + slots - 1) / slots, (nb + kPartsMax8 - 3) / (kPartsMax8 - 2));
+  // Several sequences of unlike lengths and more than four sub-chunks a wave: the line.
+  p.line = batch > 1 && per > 4 * kWaves8;
+  p.per = (int)(p.line ? (nb + kPartsMax8 - 3) / (kPartsMax8 - 2) : per);
+  p.nwg = (int)(p.line ? slots : (nb + per - 1) / per);
+  // Parts of a unit, at most: a workgroup takes at least nb * units / slots of the
+  // longest sequence's line, whatever the other lengths.  (Grows with max_ctx:
+  // a workspace for the capacity holds every call's.)
+  p.parts = (int)std::min<long>({nb, slots / units + 2, (long)kPartsMax8});
   return p;
 }
 
@@ -439,21 +549,23 @@ int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int max_ct
 hipError_t launch_attention8(const AttnArgs& a, hipStream_t s) {
   const int B = a.M / a.rps;
   const Plan p = plan_of(a.rps, B, a.n_heads, a.n_kv_heads, a.max_ctx);
-  if (p.parts > a.n_split || (a.max_ctx + kF8Block - 1L) / kF8Block * a.n_kv_heads * p.n_tiles * B > 1L << 30)
+  const long units = (long)a.n_kv_heads * p.n_tiles;
+  if (p.parts > a.n_split || p.n_tiles > kF8TilesPerSlot * a.f8.ring.capacity || units > 65535 || B > 65535 ||
+      (a.max_ctx + kF8Sub - 1L) / kF8Sub * units * B > 1L << 30)
     return hipErrorInvalidValue;
-#define SD_A8(HDV)                                                                                              \
-  {                                                                                                             \
-    if (p.qt == 1) hipLaunchKernelGGL((attn8_kernel<HDV, 1>), dim3(p.nwg), dim3(64 * kWaves8), 0, s, a, p.n_tiles, p.parts); \
-    else if (p.qt == 2) hipLaunchKernelGGL((attn8_kernel<HDV, 2>), dim3(p.nwg), dim3(64 * kWaves8), 0, s, a, p.n_tiles, p.parts); \
-    else hipLaunchKernelGGL((attn8_kernel<HDV, 4>), dim3(p.nwg), dim3(64 * kWaves8), 0, s, a, p.n_tiles, p.parts); \
-    hipLaunchKernelGGL((attn8_combine_kernel<HDV>), dim3(a.n_heads, a.M), dim3(64), 0, s, a, p.n_tiles, p.qt, p.parts, p.nwg); \
-  }
+  const dim3 grid = p.line ? dim3(p.nwg) : dim3(p.nwg, (unsigned)units, B), block(64 * kWaves8);
+#define SD_A8(HDV, QT)                                                                                         \
+  if (p.line) hipLaunchKernelGGL((attn8_kernel<HDV, QT, true>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per); \
+  else hipLaunchKernelGGL((attn8_kernel<HDV, QT, false>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per);
+#define SD_A8_HD(HDV) \
+  if (p.qt == 1) { SD_A8(HDV, 1) } else { SD_A8(HDV, 2) }
   switch (a.head_dim) {
-    case 32: SD_A8(32) break;
-    case 64: SD_A8(64) break;
-    case 128: SD_A8(128) break;
+    case 32: SD_A8_HD(32) break;
+    case 64: SD_A8_HD(64) break;
+    case 128: SD_A8_HD(128) break;
     default: return hipErrorInvalidValue;
   }
+#undef SD_A8_HD
 #undef SD_A8
   return hipGetLastError();
 }

@@ -61,25 +61,31 @@ template <> struct KvIndex<uint16_t> {
 // (position p at p % window, a KvLayout of capacity `window`): a block is
 // rounded once, when it is complete, and rows that are rolled back never
 // touch a code.
-//  data: ring of every layer, scales, codes (kv8_bytes; regions 256-byte
-//  aligned).  Per (layer, sequence, kv head) 2 * capacity / 64 scales (K, V of
-//  block 0, of block 1, ...) and 2 * capacity * head_dim code bytes: block i's
-//  K codes at 128 * head_dim * i, its V codes 64 * head_dim further on, each
-//  head_dim / 16 fragments of 1 KB, lane l = 16c + i holding 16 bytes:
-//   K (head_dim >= 64): fragment (2s + t) * head_dim / 64 + n: position
-//     32s + 8 (i / 4) + 4t + i % 4, dims 64n + 16c .. +15;
-//   K (head_dim 32): fragment s: bytes 8t .. 8t+7: that position, dims 8c .. +7;
-//   V: fragment dt: dim 16 dt + i, positions 8c .. +7, then 32 + 8c .. +7.
+//  data: counters of the attention's combine, ring of every layer, scales,
+//  codes (kv8_bytes; regions 256-byte aligned).  Per (layer, sequence, kv head)
+//  2 * capacity / 64 scales (K, V of block 0, of block 1, ...) and 2 * capacity *
+//  head_dim code bytes: the 32 positions from 32j at 64 * head_dim * j, K's
+//  head_dim / 32 fragments of 1 KB, then as many of V, lane l = 16c + i of a
+//  fragment holding 16 bytes:
+//   K (head_dim >= 64): fragment t * head_dim / 64 + n: position 8 (i / 4) + 4t
+//     + i % 4 of the 32, dims 64n + 16c .. +15;
+//   K (head_dim 32): bytes 8t .. 8t+7: that position, dims 8c .. +7;
+//   V: fragment f, bytes 8e .. 8e+7: dim 16 (2f + e) + i, positions 8c .. +7.
 //  (The K rows are in the order that leaves lane group c of K Q^T's product
-//  with positions 8c .. 8c+7 of a 32-position step, the k order of V: the
-//  probabilities feed P V from the registers they were made in.)
+//  with positions 8c .. 8c+7, the k order of V: the probabilities feed P V from
+//  the registers they were made in.)
 constexpr int kF8Block = 64;
 constexpr int kF8MinExp = -100;
+constexpr int kF8Sub = 32;            // positions an attention wave takes at a time
+constexpr int kF8TilesPerSlot = 4;    // query tiles of a (sequence, kv head), per ring position
+constexpr int kF8MaxGroup = 128;      // query heads per kv head (32 queries a tile: 4 tiles a row at most)
+constexpr int kF8MaxDraft = 64;       // drafted tokens of a draft step's iteration (its one-row passes see them in the ring)
 struct Kv8Layout {
   unsigned char* codes;
   float* scales;
   KvLayout ring;       // data, batch, capacity = window, n_kv_heads, head_dim, dtype = bf16
   const int32_t* len;  // [batch] committed lengths
+  uint32_t* counters;  // [batch * n_kv_heads * kF8TilesPerSlot * window], zero between launches
   int capacity;
   __device__ __forceinline__ size_t unit(int layer, int b, int g) const {
     return ((size_t)layer * ring.batch + b) * ring.n_kv_heads + g;
@@ -94,6 +100,8 @@ struct Kv8Layout {
 size_t kv8_bytes(int n_layers, int batch, int n_kv_heads, int head_dim, int capacity, int window);
 Kv8Layout kv8_layout(void* data, const int32_t* len, int n_layers, int batch, int n_kv_heads, int head_dim,
                      int capacity, int window);
+// Zeroes the combine's counters.
+hipError_t launch_kv8_init(const Kv8Layout& kv, hipStream_t s);
 // Rows k, v [n, h_kv, hd] (bf16) as positions pos0 .. pos0+n-1 of sequence b (pos0
 // a multiple of 64): every block that ends inside becomes codes, the last
 // `window` rows go to the ring.

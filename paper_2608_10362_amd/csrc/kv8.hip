@@ -17,18 +17,32 @@ namespace {
 
 constexpr int kCopyThreads = 256;
 
-// Position (in its block) and first dim of the 8 codes at bytes 8e .. 8e+7 of
-// lane 16c + i of K fragment f.
+// Position (in its block of 64) and first dim of the 8 codes at bytes 8e .. 8e+7
+// of lane 16c + i of the block's K fragment f (HD / 32 of its first half, then of
+// its second); the dim whose 8 positions from `pos` V's fragment f holds there.
 template <int HD>
 __device__ __forceinline__ void k_place(int f, int c, int i, int e, int& pos, int& dim) {
+  constexpr int FS = HD / 32;
+  const int s = f / FS, r = f % FS;
   if constexpr (HD >= 64) {
-    const int st = f / (HD / 64), n = f % (HD / 64);
-    pos = 32 * (st >> 1) + 8 * (i >> 2) + 4 * (st & 1) + (i & 3);
-    dim = 64 * n + 16 * c + 8 * e;
+    pos = 32 * s + 8 * (i >> 2) + 4 * (r / (HD / 64)) + (i & 3);
+    dim = 64 * (r % (HD / 64)) + 16 * c + 8 * e;
   } else {
-    pos = 32 * f + 8 * (i >> 2) + 4 * e + (i & 3);
+    pos = 32 * s + 8 * (i >> 2) + 4 * e + (i & 3);
     dim = 8 * c;
   }
+}
+template <int HD>
+__device__ __forceinline__ void v_place(int f, int c, int i, int e, int& pos, int& dim) {
+  constexpr int FS = HD / 32;
+  pos = 32 * (f / FS) + 8 * c;
+  dim = 16 * (2 * (f % FS) + e) + i;
+}
+// Byte of fragment f in the block's codes.
+template <int HD>
+__device__ __forceinline__ int frag_at(bool is_v, int f) {
+  constexpr int FS = HD / 32;
+  return (2 * (f / FS) + is_v) * 32 * HD + f % FS * 1024;
 }
 
 // Largest |x| among the finite of 8 bf16 values, as its bits.
@@ -84,10 +98,11 @@ __device__ __forceinline__ void quantize_block(KF k8, VF v8, unsigned char* code
     const int f = (wave & 1) * FW + j;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      int pos, dim;
       if (is_v) {
-        x[j][e] = v8(32 * e + 8 * c, 16 * f + i);
+        v_place<HD>(f, c, i, e, pos, dim);
+        x[j][e] = v8(pos, dim);
       } else {
-        int pos, dim;
         k_place<HD>(f, c, i, e, pos, dim);
         x[j][e] = k8(pos, dim);
       }
@@ -109,7 +124,7 @@ __device__ __forceinline__ void quantize_block(KF k8, VF v8, unsigned char* code
   for (int j = 0; j < FW; ++j) {
     const int f = (wave & 1) * FW + j;
     const u32x2 a = codes8(x[j][0], inv), b = codes8(x[j][1], inv);
-    *(u32x4*)(codes + (is_v ? kF8Block * HD : 0) + f * 1024 + lane * 16) = u32x4{a[0], a[1], b[0], b[1]};
+    *(u32x4*)(codes + frag_at<HD>(is_v, f) + lane * 16) = u32x4{a[0], a[1], b[0], b[1]};
   }
   if (lane == 0 && (wave & 1) == 0) scales[is_v] = __uint_as_float((uint32_t)(ex + 127) << 23);
 }
@@ -187,8 +202,8 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, in
     for (int j = 0; j < FW; ++j) {
       const int f = wave * FW + j;
       if (f < F) {
-        kc[j] = *(const u32x4*)(codes + f * 1024 + lane * 16);
-        vc[j] = *(const u32x4*)(codes + kF8Block * HD + f * 1024 + lane * 16);
+        kc[j] = *(const u32x4*)(codes + frag_at<HD>(false, f) + lane * 16);
+        vc[j] = *(const u32x4*)(codes + frag_at<HD>(true, f) + lane * 16);
       }
     }
 #pragma unroll
@@ -202,10 +217,11 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, in
         const u32x4 x = __builtin_bit_cast(u32x4, fp8x8_to_bf16(kc[j][2 * e], kc[j][2 * e + 1], ks));
         if (in(pos)) *(u32x4_a2*)(k + at(pos) + dim) = x;
         const u32x4 y = __builtin_bit_cast(u32x4, fp8x8_to_bf16(vc[j][2 * e], vc[j][2 * e + 1], vs));
+        v_place<HD>(f, c, i, e, pos, dim);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          sv[32 * e + 8 * c + 2 * q][16 * f + i] = (uint16_t)y[q];
-          sv[32 * e + 8 * c + 2 * q + 1][16 * f + i] = (uint16_t)(y[q] >> 16);
+          sv[pos + 2 * q][dim] = (uint16_t)y[q];
+          sv[pos + 2 * q + 1][dim] = (uint16_t)(y[q] >> 16);
         }
       }
     }
@@ -279,13 +295,15 @@ __global__ void kv_advance_kernel(int B, int n, int32_t* len) {
 }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+size_t counter_count(int B, int G, int window) { return (size_t)B * G * kF8TilesPerSlot * window; }
 size_t ring_bytes(int L, int B, int G, int hd, int window) { return align256((size_t)L * B * G * 2 * window * hd * 2); }
 size_t scale_bytes(int L, int B, int G, int cap) { return align256((size_t)L * B * G * 2 * (cap / kF8Block) * 4); }
 
 }  // namespace
 
 size_t kv8_bytes(int n_layers, int batch, int n_kv_heads, int head_dim, int capacity, int window) {
-  return ring_bytes(n_layers, batch, n_kv_heads, head_dim, window) + scale_bytes(n_layers, batch, n_kv_heads, capacity) +
+  return align256(counter_count(batch, n_kv_heads, window) * 4) +
+         ring_bytes(n_layers, batch, n_kv_heads, head_dim, window) + scale_bytes(n_layers, batch, n_kv_heads, capacity) +
          (size_t)n_layers * batch * n_kv_heads * 2 * (size_t)capacity * head_dim;
 }
 
@@ -293,6 +311,8 @@ Kv8Layout kv8_layout(void* data, const int32_t* len, int n_layers, int batch, in
                      int capacity, int window) {
   char* p = (char*)data;
   Kv8Layout l{};
+  l.counters = (uint32_t*)p;
+  p += align256(counter_count(batch, n_kv_heads, window) * 4);
   l.ring = KvLayout{p, batch, window, n_kv_heads, head_dim, SPECDEC_BF16};
   p += ring_bytes(n_layers, batch, n_kv_heads, head_dim, window);
   l.scales = (float*)p;
@@ -301,6 +321,10 @@ Kv8Layout kv8_layout(void* data, const int32_t* len, int n_layers, int batch, in
   l.len = len;
   l.capacity = capacity;
   return l;
+}
+
+hipError_t launch_kv8_init(const Kv8Layout& kv, hipStream_t s) {
+  return launch_fill_u32(kv.counters, counter_count(kv.ring.batch, kv.ring.n_kv_heads, kv.ring.capacity), 0u, s);
 }
 
 #define SD_BY_HEAD_DIM(hd, CALL)              \

@@ -26,7 +26,8 @@ def test_cache_sizes_and_init_errors(lib):
     L, B, cap, win = 32, 2, 2048, 128
     codes, ring = L * B * 32 * 2 * cap * 128, L * B * 32 * 2 * win * 128 * 2
     scales = L * B * 32 * 2 * (cap // 64) * 4
-    assert size(L, B, cap, win) == codes + ring + scales
+    counters = B * 32 * 4 * win * 4
+    assert size(L, B, cap, win) == codes + ring + scales + counters
     assert size(L, B, cap, win) < 0.57 * lib.specdec_kv_bytes(ctypes.byref(d), L, B, cap)
     for bad in ((0, B, cap, win), (33, B, cap, win), (L, 0, cap, win), (L, B, 100, win), (L, B, cap, 64),
                 (L, B, cap, 100), (L, B, -64, win)):

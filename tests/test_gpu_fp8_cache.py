@@ -44,10 +44,14 @@ def _rows(rng, n, G, hd, spread=True):
     return _np(_bf16(x))
 
 
-def _cache(shape, B, cap, window=128, dirt=255):
-    kv = binding.Fp8KVCache(shape, B, cap, window)
-    kv.data.fill_(dirt)  # (stale contents: NaN codes, NaN scales and NaN rows)
+def _dirty(kv):
+    """Stale contents past the counters: NaN codes, NaN scales and NaN rows."""
+    kv.data[-(-kv.batch * kv.kv.n_kv_heads * 4 * kv.kv.window * 4 // 256) * 256:].fill_(255)
     return kv
+
+
+def _cache(shape, B, cap, window=128):
+    return _dirty(binding.Fp8KVCache(shape, B, cap, window))
 
 
 # ---------------------------------------------------------------- storage
@@ -440,7 +444,7 @@ def test_prefill_stores_the_rounded_rows(model, window, rows):
     n = 300
     tok = i32(synth.make_prompt(n, shape.vocab, batch=2))
     kv, kv16 = binding.Fp8KVCache(target, 2, 512, window), binding.KVCache(target, 2, 512)
-    kv.data.fill_(255)
+    _dirty(kv)
     binding.specdec_prefill(target, kv, tok)
     binding.specdec_prefill(target, kv16, tok)
     assert list(kv.read_state()["len"]) == [n - 1] * 2 and kv.read_state()["status"] == 0
@@ -470,8 +474,8 @@ def test_verify_draft_and_commit(model, fmt):
     B, g = 2, 4
     target, draft = binding.Model(dw, 2, max_rows=64, max_ctx=512), binding.Model(dw, 1, max_rows=64, max_ctx=512)
     kv_t, kv_d = binding.Fp8KVCache(target, B, 512, 128), binding.Fp8KVCache(draft, B, 512, 128)
-    kv_t.data.fill_(255)
-    kv_d.data.fill_(255)
+    _dirty(kv_t)
+    _dirty(kv_d)
     prompts = synth.make_prompt(188, shape.vocab, batch=B)
     binding.specdec_prefill(target, kv_t, i32(prompts))
     binding.specdec_prefill(draft, kv_d, i32(prompts))
@@ -526,6 +530,38 @@ def test_draft_step_logits(model):
     assert kv.read_state()["status"] == 0
 
 
+def test_long_drafts_and_invalid_rows(model):
+    """A draft of 64 tokens (its rows fill the ring past its block), and verify
+    passes with token ids outside the vocabulary: the valid rows are as without them."""
+    torch = torch_cuda()
+    shape, W, dw = model
+    draft = binding.Model(dw, 2, max_rows=128, max_ctx=512)
+    kv = binding.Fp8KVCache(draft, 1, 512, 192)
+    _dirty(kv)
+    L, g = 190, 64
+    binding.specdec_prefill(draft, kv, i32(synth.make_prompt(L + 1, shape.vocab)))
+    last = int(kv.read_state()["pending"][0, 1])
+    m, c = _oracle_on(shape, W, kv, 0, L)
+    d = torch.zeros((1, g), dtype=torch.int32, device="cuda")
+    lo = torch.zeros((1, shape.vocab), dtype=torch.float32, device="cuda")
+    for s in range(g):
+        binding.specdec_draft_step(draft, kv, g, s, 0.0, 0, 0, None, None, d, g, lo)
+        ref = m.forward_block([last if s == 0 else int(d[0, s - 1].item())], L + s, c)[-1]
+        assert np.abs(lo.cpu().numpy()[0] - ref).max() < 2e-2, s
+    assert kv.read_state()["status"] == 0
+    for bad in (4, 2):  # (the last row, one in the middle)
+        dd = i32(synth.make_prompt(5, shape.vocab, seed=3))
+        good = torch.empty((1, 6, shape.vocab), dtype=torch.float32, device="cuda")
+        lg = torch.empty_like(good)
+        binding.specdec_verify(draft, kv, 5, dd, 5, good)
+        dd[0, bad] = shape.vocab
+        binding.specdec_verify(draft, kv, 5, dd, 5, lg)
+        rows = list(range(bad + 1))
+        torch.testing.assert_close(lg[:, rows], good[:, rows], rtol=0, atol=1e-4)
+        assert kv.read_state()["status"] == -7
+        kv.set_state([L], [[0, last]], [1])
+
+
 def test_pass_refusals(model):
     torch = torch_cuda()
     shape, W, dw = model
@@ -537,6 +573,10 @@ def test_pass_refusals(model):
         binding.specdec_verify(target, kv, 65, d, 70, lg)  # 66 new rows: the ring takes 65
     assert e.value.status == -2
     binding.specdec_verify(target, kv, 64, d, 70, lg)
+    wide = binding.Fp8KVCache(target, 1, 512, 192)
+    with pytest.raises(binding.SpecdecError) as e:
+        binding.specdec_draft_step(target, wide, 65, 0, 0.0, 0, 0, None, None, d, 70)
+    assert e.value.status == -2
     other = binding.Fp8KVCache(dataclasses.replace(shape, n_kv_heads=8), 1, 512)
     with pytest.raises(binding.SpecdecError) as e:
         binding.specdec_verify(target, other, 4, d, 70, lg)
