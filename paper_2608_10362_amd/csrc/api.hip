@@ -766,7 +766,7 @@ specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* stream) {
 
 size_t specdec_attention_workspace_bytes(const specdec_kv* kv, int32_t n_heads, int32_t n) {
   if (check_attention(kv, n_heads, n) != SPECDEC_OK) return 0;
-  const size_t parts = (size_t)attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->capacity);
+  const size_t parts = (size_t)attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->head_dim, kv->capacity);
   const size_t slots = (size_t)kv->batch * n * n_heads * parts;
   return align_up(slots * kv->head_dim * 4) + align_up(slots * 2 * 4);
 }
@@ -789,7 +789,7 @@ specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_
   a.kv = kv_layout(kv);
   a.layer = layer;
   a.max_ctx = (int)kv->len_upper + n;
-  a.n_split = attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->capacity);
+  a.n_split = attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->head_dim, kv->capacity);
   a.o_part = (float*)workspace;
   a.ml_part = (float*)((char*)workspace + align_up((size_t)a.M * n_heads * a.n_split * kv->head_dim * 4));
   a.o = out;

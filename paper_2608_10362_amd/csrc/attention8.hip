@@ -14,7 +14,7 @@
 // left; two parts leave 2^-18, 3.5e-6 of the result over 2048 keys against 7e-7
 // for a float32 computation, one leaves 2^-9).
 //
-// Work: a line of sub-chunks of 32 keys, sequence by sequence, unit by unit (kv
+// Work: a line of chunks of 32 or 64 keys, sequence by sequence, unit by unit (kv
 // head, query tile); workgroup i takes the i-th `per` of them, so all stream the
 // same bytes whatever the lengths, and its NW waves take every NW-th.  Within a
 // unit's segment each wave keeps (max, sum, O), then they merge in LDS.  A unit
@@ -32,6 +32,10 @@ namespace specdec {
 namespace {
 
 constexpr int kPartsMax8 = 64;  // parts of one unit (one per lane of the combining wave)
+// Sub-chunks of 32 keys a wave takes at a time, its chunk: 8 KB of codes for 128
+// dims as for 64.
+__host__ __device__ constexpr int steps_of(int head_dim) { return head_dim == 128 ? 1 : 2; }
+__host__ __device__ constexpr int chunk_of(int head_dim) { return kF8Sub * steps_of(head_dim); }
 
 // v as a sum of three bf16 values, each of what the ones before leave.
 __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&part)[3]) {
@@ -60,12 +64,13 @@ __device__ __forceinline__ RowDesc row_of(const AttnArgs& a, int b, int i) {
   if (a.rows) return a.rows[b * a.rps + i];
   return RowDesc{b, a.f8.len[b] + i, 0, 1};
 }
-// Sub-chunks sequence b's rows see (its last row bounds them; the host's count
+// Chunks sequence b's rows see (its last row bounds them; the host's count
 // where that row is invalid).
-__device__ __forceinline__ int subs_of(const AttnArgs& a, int b) {
+template <int C>
+__device__ __forceinline__ int chunks_of(const AttnArgs& a, int b) {
   const RowDesc last = row_of(a, b, a.rps - 1);
-  const int most = (a.max_ctx + kF8Sub - 1) / kF8Sub;
-  return last.valid ? max(1, min(most, last.pos / kF8Sub + 1)) : most;
+  const int most = (a.max_ctx + C - 1) / C;
+  return last.valid ? max(1, min(most, last.pos / C + 1)) : most;
 }
 
 __device__ __forceinline__ int lane_sum(int v) {
@@ -101,19 +106,21 @@ __device__ __forceinline__ void finish_row(const AttnArgs& a, int b, int i, int 
 // is far from the next whole number compared with the product's rounding).
 __device__ __forceinline__ int div_small(int n, float inv) { return (int)(((float)n + 0.5f) * inv); }
 
-constexpr int kWaves8 = 8;  // per workgroup
+// Waves of a workgroup: with two query tiles a wave, two workgroups of 4 share a
+// CU, so that one's start and merge run under the other's products.
+__host__ __device__ constexpr int waves_of(int query_tiles) { return query_tiles == 1 ? 8 : 4; }
 
-// LDS: the queries' parts; then ring rows (a K fragment per tile and step, V's
-// fragments), one slot per sub-chunk in work, reused by the merge.  With one
-// query tile a wave (at most 64 rows, at most 65 of them not committed) at most
-// 4 sub-chunks of a sequence lie in the ring (63 + 65 rows from a multiple of
-// 64), sub-chunk j in slot j % 4; otherwise a slot per wave.
+// LDS: the queries' parts; then, one query tile a wave, ring rows (a K fragment
+// per tile and step, V's fragments), one slot per sub-chunk; reused by the
+// merge.  With at most 64 rows, at most 65 of them not committed, at most 4
+// sub-chunks of a sequence lie in the ring (63 + 65 rows from a multiple of
+// 64): sub-chunk j in slot j % 4.
 template <int HD, int QT>
 struct Lds8 {
-  static constexpr int KST = HD / 32, DT = HD / 16, OS = HD + 4, NW = kWaves8, NR = QT == 1 ? 4 : NW;
+  static constexpr int KST = HD / 32, DT = HD / 16, OS = HD + 4, NW = waves_of(QT);
   bf16x8 q[QT][KST][3][kWave];
   union {
-    u32x4 ring[NR][2 * KST + DT][kWave];
+    u32x4 ring[QT == 1 ? 4 : 1][2 * KST + DT][kWave];
     struct {
       float o[NW][16][OS];
       float ml[NW][16][2];
@@ -122,11 +129,11 @@ struct Lds8 {
   int last;
 };
 
-// Workgroups: LINE: the line of all units' sub-chunks, `per` to a workgroup (x);
+// Workgroups: LINE: the line of all units' chunks, `per` to a workgroup (x);
 // otherwise part x of unit y of sequence z, every part of a sequence `per` long.
-template <int HD, int QT, bool LINE>
-__global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(AttnArgs a, int n_tiles, int parts, int per0) {
-  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, RK = 2 * KST, NW = kWaves8;
+template <int HD, int QT, bool LINE, bool ONCE>
+__global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kernel(AttnArgs a, int n_tiles, int parts, int per0) {
+  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, RK = 2 * KST, NW = waves_of(QT), SP = steps_of(HD);
   __shared__ Lds8<HD, QT> sh;
   const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, nq = rps * group;
@@ -134,83 +141,149 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(Att
   const float qscale = 1.44269504088896341f / sqrtf((float)HD);  // (scores in powers of two)
   const float inv_group = 1.0f / (float)group;
 
-  // One segment: sub-chunks [k_lo, k_hi) of unit (b, g, tile), part `part` of its n.
+  // One segment: chunks [k_lo, k_hi) of unit (b, g, tile), part `part` of its n.
   auto segment = [&](int b, int g, int tile, int k_lo, int k_hi, int part, int n) {
     // (opaque: what a segment derives from it stays in the segment, not in registers across all of them)
     int lane = lane0;
     asm volatile("" : "+v"(lane));
     const int c16 = lane & 15, grp = lane >> 4;
-    const int sealed = (a.f8.len[b] + a.c0) / kF8Block * (kF8Block / kF8Sub);
-    if (QT == 1) k_hi = min(k_hi, sealed + 4);  // (no valid row is past it: the ring's slots)
+    // This wave's 32-dim steps of the query tiles, asked for before the length that
+    // everything else needs has arrived.
+    constexpr int QW = (QT * KST + NW - 1) / NW;
+    f32x4 qv[QW][2];
+#pragma unroll
+    for (int i = 0; i < QW; ++i) {
+      const int st = wave + i * NW, q = st / KST, s = st % KST;
+      const int qa = (tile * QT + q) * 16 + c16, qr = div_small(qa, inv_group);
+      const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
+      qv[i][0] = qv[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (st < QT * KST && qa < nq) {
+        const float* qp = a.qr + ((size_t)(b * rps + qr) * H + g * group + qa - qr * group) * HD + d;
+        qv[i][0] = *(const f32x4_a4*)qp;
+        qv[i][1] = *(const f32x4_a4*)(qp + 4);
+      }
+    }
+    // (the same in every lane; told so, the addresses that follow from it stay scalar)
+    const int sealed = __builtin_amdgcn_readfirstlane((a.f8.len[b] + a.c0) / kF8Block * (kF8Block / kF8Sub / SP));
+    if (QT == 1) k_hi = min(k_hi, sealed + 4 / SP);  // (no valid row is past it: the ring's slots)
 
     // Codes and scales through buffer descriptors that end with the sealed ones: a
     // wave's loads past its last sub-chunk read nothing, so none needs a branch
     // (with one, the compiler waits for every load at the loop's head).
     const int j_sealed = min(k_hi, sealed);
-    const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, b, g), (uint32_t)j_sealed * 2 * kF8Sub * HD);
-    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, b, g), (uint32_t)((j_sealed + 1) & ~1) * 4);
-    u32x4 kc[FS], vc[FS];
+    const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, b, g), (uint32_t)j_sealed * SP * 2 * kF8Sub * HD);
+    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, b, g), (uint32_t)((j_sealed * SP + 1) & ~1) * 4);
+    constexpr int kCodes = ONCE ? kNonTemporal : 0;
+    u32x4 kc[SP][FS], vc[SP][FS];
     float ks, vs;
     auto load_k = [&](int j) {
-      const uint32_t at = (uint32_t)j * 2 * kF8Sub * HD + lane * 16;
+      const uint32_t at = (uint32_t)j * SP * 2 * kF8Sub * HD + lane * 16;
 #pragma unroll
-      for (int f = 0; f < FS; ++f) kc[f] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + f * 1024, 0, 0));
-      ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j & ~1) * 4, 0, 0));
+      for (int i = 0; i < SP * FS; ++i)
+        kc[i / FS][i % FS] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i / FS * 2 * kF8Sub * HD + i % FS * 1024, 0, kCodes));
+      ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP & ~1) * 4, 0, 0));
     };
     auto load_v = [&](int j) {
-      const uint32_t at = (uint32_t)j * 2 * kF8Sub * HD + kF8Sub * HD + lane * 16;
+      const uint32_t at = (uint32_t)j * SP * 2 * kF8Sub * HD + kF8Sub * HD + lane * 16;
 #pragma unroll
-      for (int f = 0; f < FS; ++f) vc[f] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + f * 1024, 0, 0));
-      vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j | 1) * 4, 0, 0));
+      for (int i = 0; i < SP * FS; ++i)
+        vc[i / FS][i % FS] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i / FS * 2 * kF8Sub * HD + i % FS * 1024, 0, kCodes));
+      vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP | 1) * 4, 0, 0));
     };
-    // The ring's rows go to this wave's part of LDS without passing the registers.
+    // The ring's rows: with one query tile a wave they go to LDS without passing the
+    // registers, at the segment's start; with two, to registers, a step ahead.
     const uint16_t* ring = k_block<uint16_t>(a.f8.ring, a.layer, b, g);
-    auto slot_of = [&](int j) { return QT == 1 ? j & 3 : wave; };
-    auto load_ring = [&](int j) {
-      const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&sh.ring[slot_of(j)][0][0];
+    u32x4 rk[QT == 1 ? 1 : RK], rv[QT == 1 ? 1 : DT];
+    auto ring_k = [&](int sub) {  // (sub: the sub-chunk, in 32 positions)
       const __amdgpu_buffer_rsrc_t rr = make_rsrc(ring, (uint32_t)window * HD * 4u);
       int l = lane;
       asm volatile("" : "+v"(l));  // (addresses computed here, not kept)
-      const int w0 = j * kF8Sub % window, i = l & 15, c = l >> 4;
+      const int w0 = sub * kF8Sub % window, i = l & 15, c = l >> 4;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int s = 0; s < KST; ++s) {
           const int d = HD >= 64 ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 32 * s + 8 * c;
           const int pos = w0 + 8 * (i >> 2) + 4 * t + (i & 3);
-          load_lds16(lds0 + (t * KST + s) * 1024u, (uint32_t)KvIndex<uint16_t>::k(pos, d, HD, window) * 2u, rr);
+          const uint32_t at = (uint32_t)KvIndex<uint16_t>::k(pos, d, HD, window) * 2u;
+          if constexpr (QT == 1) {
+            const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&sh.ring[sub & 3][0][0];
+            load_lds16(lds0 + (t * KST + s) * 1024u, at, rr);
+          } else {
+            rk[t * KST + s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, at, 0, 0));
+          }
         }
+    };
+    auto ring_v = [&](int sub) {
+      const __amdgpu_buffer_rsrc_t rr = make_rsrc(ring, (uint32_t)window * HD * 4u);
+      int l = lane;
+      asm volatile("" : "+v"(l));
+      const int w0 = sub * kF8Sub % window, i = l & 15, c = l >> 4;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        load_lds16(lds0 + (RK + dt) * 1024u, (uint32_t)KvIndex<uint16_t>::v(w0 + 8 * c, 16 * dt + i, HD, window) * 2u, rr);
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint32_t at = (uint32_t)KvIndex<uint16_t>::v(w0 + 8 * c, 16 * dt + i, HD, window) * 2u;
+        if constexpr (QT == 1) {
+          const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&sh.ring[sub & 3][0][0];
+          load_lds16(lds0 + (RK + dt) * 1024u, at, rr);
+        } else {
+          rv[dt] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, at, 0, 0));
+        }
+      }
     };
 
-    // This wave's sub-chunks: j, j + NW, ...; the first codes, and the first ring
+    // This wave's chunks: j, j + NW, ...; the first codes, and the first ring
     // rows, are on their way while the queries are made ready.
     int j = k_lo + wave;
     int jr = max(j, j + (sealed - j + NW - 1) / NW * NW);  // the first of them in the ring
-    if (jr < k_hi) load_ring(jr);
+    // (one query tile: each wave has at most one chunk of the ring's)
+    const bool has_ring = jr < k_hi;
+    if (QT == 1 && has_ring) {
+#pragma unroll
+      for (int sp = 0; sp < SP; ++sp) {
+        ring_k(jr * SP + sp);
+        ring_v(jr * SP + sp);
+      }
+    }
     load_k(j);
     load_v(j);
+    // Where this wave has ring rows: this lane's query of each tile, its position; the tiles' range.
+    int qpos[QT], vis = 0, lowest = 0x7fffffff;
+    if (has_ring) {
+#pragma unroll
+      for (int q = 0; q < QT; ++q) {
+        const int qa = (tile * QT + q) * 16 + c16;
+        const RowDesc rd = row_of(a, b, qa < nq ? div_small(qa, inv_group) : 0);
+        qpos[q] = qa < nq && rd.valid ? rd.pos : -1;
+        if (qpos[q] >= 0) {
+          vis = max(vis, qpos[q] + 1);
+          lowest = min(lowest, qpos[q]);
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) {
+        vis = max(vis, __shfl_xor(vis, o, kWave));
+        lowest = min(lowest, __shfl_xor(lowest, o, kWave));
+      }
+      vis = __builtin_amdgcn_readfirstlane(vis);
+      lowest = __builtin_amdgcn_readfirstlane(lowest);
+    }
 
-    for (int i = wave; i < QT * KST; i += NW) {  // (wave-uniform) one 32-dim step of one tile
-      const int q = i / KST, s = i % KST, qa = (tile * QT + q) * 16 + c16;
-      const bool in = qa < nq;
-      const int qr = in ? div_small(qa, inv_group) : 0;
-      const int row = b * rps + qr, head = g * group + (in ? qa - qr * group : 0);
-      const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
-      const float* qp = a.qr + ((size_t)row * H + head) * HD + d;
-      const f32x4 v0 = *(const f32x4_a4*)qp, v1 = *(const f32x4_a4*)(qp + 4);
+#pragma unroll
+    for (int i = 0; i < QW; ++i) {
+      const int st = wave + i * NW;
+      if (st >= QT * KST) break;  // (wave-uniform)
       float v[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        v[e] = in ? v0[e] * qscale : 0.f;
-        v[4 + e] = in ? v1[e] * qscale : 0.f;
+        v[e] = qv[i][0][e] * qscale;
+        v[4 + e] = qv[i][1][e] * qscale;
       }
       bf16x8 p3[3];
       split8(v, p3);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) sh.q[q][s][k][lane] = p3[k];
+      for (int k = 0; k < 3; ++k) sh.q[st / KST][st % KST][k][lane] = p3[k];
     }
     __syncthreads();
 
@@ -242,9 +315,14 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(Att
           }
       }
     };
-    // The running maximum and sum of tile q over 8 new scores, which become probabilities relative to it.
-    auto softmax = [&](int q, float (&p)[8]) {
-      float m = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+    // The running maximum and sum of tile q over new scores, which become
+    // probabilities relative to it.  Masked: some may be -inf, all of them for a
+    // query that has seen no key yet (its maximum stays -inf).
+    auto softmax = [&](int q, auto& p, bool masked) {
+      constexpr int N = sizeof(p) / sizeof(float);
+      float m = fmaxf(p[0], p[1]);
+#pragma unroll
+      for (int e = 2; e < N; ++e) m = fmaxf(m, p[e]);
       m = groups_max(m);
       const float mnew = fmaxf(mx[q], m);
       if (__any(mnew > mx[q])) {  // (rescaled only where a maximum rose)
@@ -255,136 +333,143 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(Att
         mx[q] = mnew;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        // (a query that has seen no key yet keeps the maximum -inf)
-        p[e] = mx[q] == -INFINITY && p[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p[e] - mx[q]);
+      for (int e = 0; e < N; ++e) {
+        const float x = __builtin_amdgcn_exp2f(p[e] - mx[q]);
+        p[e] = masked && mx[q] == -INFINITY && p[e] == -INFINITY ? 0.f : x;
         sm[q] += p[e];
       }
     };
 
     for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
-      floatx4 acc[QT][2];
-      scores(
-          [&](int t, int s) {
-            const u32x4 w = HD >= 64 ? kc[t * (HD / 64) + s / 2] : kc[0];
-            const int h = HD >= 64 ? s & 1 : t;
-            return fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
-          },
-          acc);
+      float p[QT][8 * SP];
+#pragma unroll
+      for (int sp = 0; sp < SP; ++sp) {
+        floatx4 acc[QT][2];
+        scores(
+            [&](int t, int s) {
+              const u32x4 w = HD >= 64 ? kc[sp][t * (HD / 64) + s / 2] : kc[sp][0];
+              const int h = HD >= 64 ? s & 1 : t;
+              return fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
+            },
+            acc);
+#pragma unroll
+        for (int q = 0; q < QT; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
+      }
       // (a wave's next K is on its way through the softmax and P V, its next V through the next scores)
       load_k(j + NW);
-      bf16x8 pp[QT][3];
+      bf16x8 pp[QT][SP][3];
 #pragma unroll
       for (int q = 0; q < QT; ++q) {
-        float p[8];
+        softmax(q, p[q], false);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = acc[q][e >> 2][e & 3];
-        softmax(q, p);
-        split8(p, pp[q]);
+        for (int sp = 0; sp < SP; ++sp) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = p[q][8 * sp + e];
+          split8(v, pp[q][sp]);
+        }
       }
+      // (DG dimension tiles in turn: a product that waits for its accumulator would leave the matrix unit idle)
+      constexpr int DG = DT < 4 ? DT : 4;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const bf16x8 vv = fp8x8_to_bf16(vc[dt / 2][2 * (dt & 1)], vc[dt / 2][2 * (dt & 1) + 1], vs);
+      for (int sp = 0; sp < SP; ++sp)
 #pragma unroll
-        for (int k = 2; k >= 0; --k)
+        for (int d0 = 0; d0 < DT; d0 += DG) {
+          bf16x8 vv[DG];
 #pragma unroll
-          for (int q = 0; q < QT; ++q)
-            of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pp[q][k], of[q][dt], 0, 0, 0);
-      }
+          for (int i = 0; i < DG; ++i) {
+            const u32x4 w = vc[sp][(d0 + i) / 2];
+            vv[i] = fp8x8_to_bf16(w[2 * (i & 1)], w[2 * (i & 1) + 1], vs);
+          }
+#pragma unroll
+          for (int k = 2; k >= 0; --k)
+#pragma unroll
+            for (int i = 0; i < DG; ++i)
+#pragma unroll
+              for (int q = 0; q < QT; ++q)
+                of[q][d0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[i], pp[q][sp][k], of[q][d0 + i], 0, 0, 0);
+        }
       load_v(j + NW);
     }
 
-    if (jr < k_hi) {  // the ring
-      // This lane's query of each tile: its position; the tiles' range.
-      int qpos[QT], vis = 0, lowest = 0x7fffffff;
-#pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        const int qa = (tile * QT + q) * 16 + c16;
-        const RowDesc rd = row_of(a, b, qa < nq ? div_small(qa, inv_group) : 0);
-        qpos[q] = qa < nq && rd.valid ? rd.pos : -1;
-        if (qpos[q] >= 0) {
-          vis = max(vis, qpos[q] + 1);
-          lowest = min(lowest, qpos[q]);
-        }
+    if (has_ring) {
+      if (QT > 1) {
+        ring_k(jr * SP);
+        ring_v(jr * SP);
       }
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) {
-        vis = max(vis, __shfl_xor(vis, o, kWave));
-        lowest = min(lowest, __shfl_xor(lowest, o, kWave));
-      }
-      vis = __builtin_amdgcn_readfirstlane(vis);
-      lowest = __builtin_amdgcn_readfirstlane(lowest);
-      for (;;) {
-        const int k0 = jr * kF8Sub;
-        const u32x4(*rows)[kWave] = sh.ring[slot_of(jr)];
-        if (k0 >= vis) {
-          wait_vm<0>();  // (its rows' loads to LDS have ended)
-          break;
-        }
-        wait_vm<0>();
-        __builtin_amdgcn_wave_barrier();
-        floatx4 acc[QT][2];
-        scores([&](int t, int s) { return __builtin_bit_cast(bf16x8, rows[t * KST + s][lane]); }, acc);
-        bool odd = false;  // a NaN or infinity among the V entries seen
-        // Slots past the newest visible position hold stale values: their V entries
-        // are zeroed, never multiplied by a zero probability.
-        const int nvalid = vis - (k0 + 8 * grp);
-        auto v_of = [&](int dt, bool finite_only) {
-          u32x4 v = rows[RK + dt][lane];
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            if (2 * w >= nvalid) v[w] = 0u;
-            else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
-            const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
-            odd |= lo || up;
-            if (finite_only && lo) v[w] &= 0xffff0000u;
-            if (finite_only && up) v[w] &= 0xffffu;
+#pragma unroll 1
+      for (; jr < k_hi; jr += NW)
+#pragma unroll 1
+        for (int sp = 0; sp < SP; ++sp) {
+          const int sub = jr * SP + sp, k0 = sub * kF8Sub;
+          if (QT == 1) {
+            wait_vm<0>();  // (the rows are in LDS)
+            __builtin_amdgcn_wave_barrier();
           }
-          return v;
-        };
-        // A NaN or infinity that only later rows see must not reach the others
-        // through 0 * inf: where some query does not see all, such entries leave the
-        // product and are added by themselves to the queries that see them.
-        const bool diagonal = k0 + kF8Sub - 1 > lowest;
+          if (k0 >= vis) break;
+          const int next = sp + 1 < SP ? sub + 1 : (jr + NW) * SP;
+          const u32x4(*rows)[kWave] = sh.ring[QT == 1 ? sub & 3 : 0];
+          floatx4 acc[QT][2];
+          scores([&](int t, int s) { return __builtin_bit_cast(bf16x8, QT == 1 ? rows[t * KST + s][lane] : rk[QT == 1 ? 0 : t * KST + s]); }, acc);
+          if (QT > 1) ring_k(next);
+          // Where some query does not see all of them (uniform):
+          //  - slots past the newest visible position hold stale values: their V entries
+          //    are zeroed, never multiplied by a zero probability;
+          //  - a NaN or infinity that only later rows see must not reach the others through
+          //    0 * inf: such entries leave the product and are added by themselves to the
+          //    queries that see them.
+          const bool diagonal = k0 + kF8Sub - 1 > lowest;
+          const int nvalid = vis - (k0 + 8 * grp);
+          bool odd = false;
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-          float p[8];
+          for (int q = 0; q < QT; ++q) {
+            float p[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
-          softmax(q, p);
-          bf16x8 pp[3];
-          split8(p, pp);
+            for (int e = 0; e < 8; ++e) p[e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
+            softmax(q, p, true);
+            bf16x8 pp[3];
+            split8(p, pp);
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const bf16x8 vv = __builtin_bit_cast(bf16x8, v_of(dt, diagonal));
+            for (int dt = 0; dt < DT; ++dt) {
+              u32x4 v = QT == 1 ? rows[RK + dt][lane] : rv[QT == 1 ? 0 : dt];
+              if (diagonal) {
 #pragma unroll
-            for (int k = 2; k >= 0; --k)
-              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pp[k], of[q][dt], 0, 0, 0);
-          }
-          if (diagonal && __any(odd)) {
-            for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
-              float pi = 0.f;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) pi = (i & 7) == e ? p[e] : pi;
-              pi = __shfl(pi, 16 * (i >> 3) + c16, kWave);
-              // (V fragment dt: lane 16 (i / 8) + d, entry i % 8)
-              const uint16_t* vrow = (const uint16_t*)&rows[RK][16 * (i >> 3)] + (i & 7);
-#pragma unroll
-              for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  const float v = bf16_bits_to_f32(vrow[(size_t)dt * kWave * 8 + (4 * grp + r) * 8]);
-                  if (k0 + i <= qpos[q] && !isfinite(v)) of[q][dt][r] += pi * v;
+                for (int w = 0; w < 4; ++w) {
+                  if (2 * w >= nvalid) v[w] = 0u;
+                  else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
+                  const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
+                  odd |= lo || up;
+                  if (lo) v[w] &= 0xffff0000u;
+                  if (up) v[w] &= 0xffffu;
                 }
+              }
+#pragma unroll
+              for (int k = 2; k >= 0; --k)
+                of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pp[k], of[q][dt], 0, 0, 0);
+            }
+            if (diagonal && __any(odd)) {
+              for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
+                float pi = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pi = (i & 7) == e ? p[e] : pi;
+                pi = __shfl(pi, 16 * (i >> 3) + c16, kWave);
+                // (V fragment dt: lane 16 (i / 8) + d, entry i % 8)
+                const uint16_t* vrow = QT == 1 ? (const uint16_t*)&rows[RK][16 * (i >> 3)] + (i & 7)
+                                               : ring + KvIndex<uint16_t>::v(k0 % window + i, 0, HD, window);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                  for (int r = 0; r < 4; ++r) {
+                    const float v = bf16_bits_to_f32(vrow[(size_t)dt * kWave * 8 + (4 * grp + r) * 8]);
+                    if (k0 + i <= qpos[q] && !isfinite(v)) of[q][dt][r] += pi * v;
+                  }
+              }
             }
           }
+          if (QT > 1) ring_v(next);
         }
-        jr += NW;
-        if (jr >= k_hi) break;
-        __builtin_amdgcn_wave_barrier();  // (every lane is done with these rows)
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        load_ring(jr);
-      }
     }
 
     // Merge the waves of this segment in LDS, tile by tile (fixed order).
@@ -447,40 +532,65 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(Att
       }
       __syncthreads();
       if (sh.last) {
-        constexpr int LP = HD / 4, PI = kWave / LP, BT = 8;  // parts a load covers, loads in flight
-        const int n_rows = min(16 * QT, nq - tile * QT * 16);
-        for (int i = wave; i < n_rows; i += NW) {  // (wave-uniform)
-          const int qa = tile * QT * 16 + i, qr = div_small(qa, inv_group), head = g * group + qa - qr * group;
-          const size_t slot = ((size_t)(b * rps + qr) * H + head) * parts;
-          const float2 ml = lane < n ? get2(a.ml_part + 2 * (slot + lane)) : make_float2(-INFINITY, 0.f);
-          const int pg = lane / LP, d = lane % LP * 4;
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-          float wgt = 0.f, inv = 0.f;
-          for (int p0 = 0; p0 < n; p0 += BT * PI) {
-            float2 lo[BT], up[BT];
+        // (two rows a wave at once, their loads in one list: IT of them in flight)
+        constexpr int LP = HD / 4, PI = kWave / LP, RW = 2, IT = 12;
+        const int n_rows = min(16 * QT, nq - tile * QT * 16), pg = lane / LP, d = lane % LP * 4;
+        const int steps = (n + PI - 1) / PI;  // loads of one row
+        for (int i0 = wave; i0 < n_rows; i0 += NW * RW) {  // (wave-uniform)
+          const int here = i0 + NW < n_rows ? 2 : 1;
+          size_t slot[RW];
+          int qr[RW], head[RW];
+          float2 ml[RW];
+          f32x4 acc[RW];
+          float wgt[RW], inv[RW];
 #pragma unroll
-            for (int k = 0; k < BT; ++k) {
-              const float* src = a.o_part + (slot + min(p0 + k * PI + pg, n - 1)) * HD + d;
+          for (int r = 0; r < RW; ++r) {
+            const int qa = tile * QT * 16 + i0 + (r < here ? r * NW : 0);
+            qr[r] = div_small(qa, inv_group);
+            head[r] = g * group + qa - qr[r] * group;
+            slot[r] = ((size_t)(b * rps + qr[r]) * H + head[r]) * parts;
+            ml[r] = lane < n ? get2(a.ml_part + 2 * (slot[r] + lane)) : make_float2(-INFINITY, 0.f);
+            acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+          for (int t0 = 0; t0 < here * steps; t0 += IT) {
+            float2 lo[IT], up[IT];
+#pragma unroll
+            for (int k = 0; k < IT; ++k) {
+              const int t = t0 + k;
+              if (t >= here * steps) break;  // (uniform)
+              const int row1 = t >= steps, p = (t - (row1 ? steps : 0)) * PI + pg;
+              const float* src = a.o_part + ((row1 ? slot[1] : slot[0]) + min(p, n - 1)) * HD + d;
               lo[k] = get2(src);
               up[k] = get2(src + 2);
             }
-            if (p0 == 0) {
-              const float M = wave_max(ml.x);
-              wgt = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
-              inv = 1.0f / wave_sum(wgt * ml.y);
+            if (t0 == 0) {
+#pragma unroll
+              for (int r = 0; r < RW; ++r) {
+                const float M = wave_max(ml[r].x);
+                wgt[r] = ml[r].x == -INFINITY ? (ml[r].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[r].x - M);
+                inv[r] = 1.0f / wave_sum(wgt[r] * ml[r].y);
+              }
             }
 #pragma unroll
-            for (int k = 0; k < BT; ++k) {
-              const int p = p0 + k * PI + pg;
-              const float w = __shfl(wgt, p & 63, kWave);
-              if (p < n) acc += w * f32x4{lo[k].x, lo[k].y, up[k].x, up[k].y};
+            for (int k = 0; k < IT; ++k) {
+              const int t = t0 + k;
+              if (t >= here * steps) break;
+              const int row1 = t >= steps, p = (t - (row1 ? steps : 0)) * PI + pg;
+              const float wp = __shfl(row1 ? wgt[1] : wgt[0], p & 63, kWave), w = p < n ? wp : 0.f;  // (by every lane)
+              const f32x4 v = {lo[k].x, lo[k].y, up[k].x, up[k].y};
+              if (row1) acc[1] += w * v;
+              else acc[0] += w * v;
             }
           }
 #pragma unroll
-          for (int o = LP; o < kWave; o <<= 1)
+          for (int r = 0; r < RW; ++r) {
+            if (r >= here) break;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, kWave);
-          if (lane < LP) finish_row(a, b, qr, head, d, acc, inv);
+            for (int o = LP; o < kWave; o <<= 1)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[r][e] += __shfl_xor(acc[r][e], o, kWave);
+            if (lane < LP) finish_row(a, b, qr[r], head[r], d, acc[r], inv[r]);
+          }
         }
       }
     }
@@ -488,18 +598,18 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(Att
 
   if constexpr (!LINE) {
     const int b = blockIdx.z, u = blockIdx.y, part = blockIdx.x;
-    const int nb = subs_of(a, b), k_lo = part * per0;
+    const int nb = __builtin_amdgcn_readfirstlane(chunks_of<chunk_of(HD)>(a, b)), k_lo = part * per0;
     if (k_lo >= nb) return;  // (workgroup-uniform)
     const int g = u / n_tiles;
     segment(b, g, u - g * n_tiles, k_lo, min(nb, k_lo + per0), part, (nb + per0 - 1) / per0);
   } else {
     const int B = a.M / rps, U = G * n_tiles;
-    const int n0 = lane0 < B ? subs_of(a, lane0) : 0;  // (the first 64 sequences stay in a register)
+    const int n0 = lane0 < B ? chunks_of<chunk_of(HD)>(a, lane0) : 0;  // (the first 64 sequences stay in a register)
     int total = 0;
-    for (int c = 0; c < B; c += kWave) total += lane_sum(c == 0 ? n0 : (c + lane0 < B ? subs_of(a, c + lane0) : 0));
+    for (int c = 0; c < B; c += kWave) total += lane_sum(c == 0 ? n0 : (c + lane0 < B ? chunks_of<chunk_of(HD)>(a, c + lane0) : 0));
     total *= U;
     const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, per0);
-    auto subs = [&](int s) { return s < kWave ? __builtin_amdgcn_readlane(n0, s) : subs_of(a, s); };
+    auto subs = [&](int s) { return s < kWave ? __builtin_amdgcn_readlane(n0, s) : __builtin_amdgcn_readfirstlane(chunks_of<chunk_of(HD)>(a, s)); };
     int x = (int)blockIdx.x * per;
     const int hi = min(total, x + per);
     int b = 0, base = 0, nb = subs(0);  // the sequence that holds x; base: the line where it starts
@@ -521,16 +631,16 @@ __global__ __launch_bounds__(64 * kWaves8, QT > 1 ? 2 : 4) void attn8_kernel(Att
 struct Plan {
   int qt, n_tiles, line, nwg, per, parts;
 };
-Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int max_ctx) {
+Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
   Plan p;
   const int nq = rps * (n_heads / n_kv_heads);
   p.qt = nq <= 64 ? 1 : 2;
   p.n_tiles = (nq + 16 * p.qt - 1) / (16 * p.qt);
-  const long nb = (max_ctx + kF8Sub - 1) / kF8Sub, units = (long)n_kv_heads * p.n_tiles;
-  const long slots = (p.qt == 1 ? 2L : 1L) * device_compute_units();  // workgroups resident at once
+  const long nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim), units = (long)n_kv_heads * p.n_tiles;
+  const long slots = 2L * device_compute_units();  // workgroups resident at once
   const long per = std::max((nb * units * batch + slots - 1) / slots, (nb + kPartsMax8 - 3) / (kPartsMax8 - 2));
-  // Several sequences of unlike lengths and more than four sub-chunks a wave: the line.
-  p.line = batch > 1 && per > 4 * kWaves8;
+  // Several sequences of unlike lengths and more than four chunks a wave: the line.
+  p.line = batch > 1 && per > 4 * waves_of(p.qt);
   p.per = (int)(p.line ? (nb + kPartsMax8 - 3) / (kPartsMax8 - 2) : per);
   p.nwg = (int)(p.line ? slots : (nb + per - 1) / per);
   // Parts of a unit, at most: a workgroup takes at least nb * units / slots of the
@@ -542,23 +652,32 @@ Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int max_ctx) {
 
 }  // namespace
 
-int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int max_ctx) {
-  return plan_of(rps, batch, n_heads, n_kv_heads, max_ctx).parts;
+int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
+  return plan_of(rps, batch, n_heads, n_kv_heads, head_dim, max_ctx).parts;
 }
 
 hipError_t launch_attention8(const AttnArgs& a, hipStream_t s) {
   const int B = a.M / a.rps;
-  const Plan p = plan_of(a.rps, B, a.n_heads, a.n_kv_heads, a.max_ctx);
+  const Plan p = plan_of(a.rps, B, a.n_heads, a.n_kv_heads, a.head_dim, a.max_ctx);
   const long units = (long)a.n_kv_heads * p.n_tiles;
   if (p.parts > a.n_split || p.n_tiles > kF8TilesPerSlot * a.f8.ring.capacity || units > 65535 || B > 65535 ||
       (a.max_ctx + kF8Sub - 1L) / kF8Sub * units * B > 1L << 30)
     return hipErrorInvalidValue;
-  const dim3 grid = p.line ? dim3(p.nwg) : dim3(p.nwg, (unsigned)units, B), block(64 * kWaves8);
-#define SD_A8(HDV, QT)                                                                                         \
-  if (p.line) hipLaunchKernelGGL((attn8_kernel<HDV, QT, true>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per); \
-  else hipLaunchKernelGGL((attn8_kernel<HDV, QT, false>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per);
-#define SD_A8_HD(HDV) \
-  if (p.qt == 1) { SD_A8(HDV, 1) } else { SD_A8(HDV, 2) }
+  const dim3 grid = p.line ? dim3(p.nwg) : dim3(p.nwg, (unsigned)units, B), block(64 * waves_of(p.qt));
+  // (codes that one unit alone reads need not stay in a cache)
+#define SD_A8(HDV, QT, LINE, ONCE) \
+  hipLaunchKernelGGL((attn8_kernel<HDV, QT, LINE, ONCE>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per)
+#define SD_A8_HD(HDV)                                  \
+  if (p.qt == 2) {                                     \
+    if (p.line) SD_A8(HDV, 2, true, false);            \
+    else SD_A8(HDV, 2, false, false);                  \
+  } else if (p.n_tiles == 1) {                         \
+    if (p.line) SD_A8(HDV, 1, true, true);             \
+    else SD_A8(HDV, 1, false, true);                   \
+  } else {                                             \
+    if (p.line) SD_A8(HDV, 1, true, false);            \
+    else SD_A8(HDV, 1, false, false);                  \
+  }
   switch (a.head_dim) {
     case 32: SD_A8_HD(32) break;
     case 64: SD_A8_HD(64) break;

@@ -283,7 +283,7 @@ int device_compute_units();                    // CUs of the current device (cac
 hipError_t launch_rope_append(const AttnArgs& a, hipStream_t s);
 // FP8 caches (attention8.hip): parts of one (row, head) the launch may write
 // (o_part holds M * n_heads * parts * head_dim floats, ml_part 2 per part).
-int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int max_ctx);
+int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx);
 hipError_t launch_attention8(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
 
