@@ -117,6 +117,40 @@ def test_hard_rows(kind):
         _check_row(l, RULES[n], p[i], tok[i], words[i])
 
 
+@pytest.mark.parametrize("kind", ["sorted", "front_lowest", "front_inf", "every_fourth", "all_equal", "wide"])
+def test_order_of_the_vocabulary(kind):
+    """Rows whose likely tokens stand together, or in one place of every four, and a
+    vocabulary of 300001: the border does not depend on where they are, nor do the
+    tokens on whether probabilities are written (other launches draw then)."""
+    V, rng = (300001 if kind == "wide" else 40003), np.random.default_rng(21)
+    l = rng.normal(0, 2.5, V).astype(np.float32)
+    if kind == "sorted":
+        l = np.sort(l)[::-1].copy()
+    elif kind == "front_lowest":
+        l[600:] = np.finfo(np.float32).min
+    elif kind == "front_inf":
+        l[6000:] = -np.inf
+    elif kind == "every_fourth":
+        l[(np.arange(V) // 256) % 4 != 2] -= 40.0
+    elif kind == "all_equal":
+        l[:] = 0.5
+    names = list(RULES) + ["k5000"]
+    table = dict(RULES, k5000={"T": 0.9, "top_k": 5000, "top_p": 0.97})
+    logits = np.broadcast_to(l, (len(names), V)).copy()
+    words = synth.make_rand_u32(len(names), seed=9)
+    r = [table[n] for n in names]
+    sr = binding.SamplingRules(temperature=f32([x.get("T", 1.0) for x in r]), top_k=i32([x.get("top_k", 0) for x in r]),
+                               top_p=f32([x.get("top_p", 1.0) for x in r]), min_p=f32([x.get("min_p", 0.0) for x in r]))
+    log(f"vocabulary order {kind}")
+    p, tok, status = _run(logits, sr, words)
+    assert status == 0
+    for i in range(len(names)):
+        _check_row(l, r[i], p[i], tok[i], words[i])
+    _, alone, status = _run(logits, sr, words, with_probs=False)
+    assert status == 0
+    np.testing.assert_array_equal(alone, tok)
+
+
 def test_large_vocabulary_and_rows_of_one_sequence():
     V, B, R = 128256, 3, 4
     rng = np.random.default_rng(4)
