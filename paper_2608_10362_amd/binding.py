@@ -199,7 +199,7 @@ def _dev(t, name: str, dtype=None, numel: int = 0, optional: bool = False):
         if optional:
             return None
         raise ValueError(f"{name}: missing")
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: expected a device tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
@@ -212,9 +212,12 @@ def _dev(t, name: str, dtype=None, numel: int = 0, optional: bool = False):
 
 def _stream(stream) -> Optional[int]:
     import torch
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return stream.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    # the same handle without a Stream object: 0.2 us in place of 2.8 us a call
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def make_desc(shape) -> ModelDesc:
@@ -746,11 +749,11 @@ def specdec_sample_logits(logits, rules: Optional[SamplingRules] = None, rand=No
 def _on_current(t, name: str, dtype):
     """Check a tensor argument's type, and that it is on the current device (where the call launches)."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: expected a device tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 

@@ -83,9 +83,10 @@ __device__ __forceinline__ u32x2 codes8(u32x4 v, float inv) {
 }
 
 // One block's codes and scales (256 threads; waves 0 and 1 K, 2 and 3 V).
-// k8(pos, dim): 8 dims of one position; v8(pos, dim): 8 positions of one dim.
-template <int HD, typename KF, typename VF>
-__device__ __forceinline__ void quantize_block(KF k8, VF v8, unsigned char* codes, float* scales) {
+// k8(pos, dim): 8 dims of one position; v8(pos, dim): 8 positions of one dim, after
+// ready(), which every wave calls once K's loads are under way.
+template <int HD, typename KF, typename RF, typename VF>
+__device__ __forceinline__ void quantize_block(KF k8, RF ready, VF v8, unsigned char* codes, float* scales) {
   constexpr int F = HD / 16, FW = F / 2;  // fragments of K (as many of V), per wave
   __shared__ uint32_t red[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -93,21 +94,19 @@ __device__ __forceinline__ void quantize_block(KF k8, VF v8, unsigned char* code
   const bool is_v = wave >= 2;
   u32x4 x[FW][2];
   uint32_t m = 0;
+  auto load = [&](auto place, auto get) {
 #pragma unroll
-  for (int j = 0; j < FW; ++j) {
-    const int f = (wave & 1) * FW + j;
+    for (int j = 0; j < FW; ++j)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      int pos, dim;
-      if (is_v) {
-        v_place<HD>(f, c, i, e, pos, dim);
-        x[j][e] = v8(pos, dim);
-      } else {
-        k_place<HD>(f, c, i, e, pos, dim);
-        x[j][e] = k8(pos, dim);
+      for (int e = 0; e < 2; ++e) {
+        int pos, dim;
+        place((wave & 1) * FW + j, c, i, e, pos, dim);
+        x[j][e] = get(pos, dim);
       }
-    }
-  }
+  };
+  if (!is_v) load(k_place<HD>, k8);
+  ready();
+  if (is_v) load(v_place<HD>, v8);
 #pragma unroll
   for (int j = 0; j < FW; ++j)
 #pragma unroll
@@ -161,18 +160,25 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_write_kernel(Kv8Layout kv, i
   __shared__ uint16_t sv[kF8Block][HD + 2];
   const int blk = blockIdx.x / G, g = blockIdx.x % G;
   const size_t base = ((size_t)blk * kF8Block * G + g) * HD;
-  constexpr int RC = HD / 8;  // 16-byte pieces of a row
+  constexpr int RC = HD / 8, VL = kF8Block * RC / kCopyThreads;  // 16-byte pieces of a row, of a thread
+  u32x4 vr[VL];
 #pragma unroll
-  for (int j = 0; j < kF8Block * RC / kCopyThreads; ++j) {
+  for (int j = 0; j < VL; ++j) {
     const int t = threadIdx.x + j * kCopyThreads, r = t / RC, d = t % RC * 8;
-    const u32x4 x = *(const u32x4_a2*)(v + base + (size_t)r * G * HD + d);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) *(uint32_t*)&sv[r][d + 2 * q] = x[q];
+    vr[j] = *(const u32x4_a2*)(v + base + (size_t)r * G * HD + d);
   }
-  __syncthreads();
   const int at = pos0 / kF8Block + blk;
   quantize_block<HD>(
       [&](int pos, int dim) { return (u32x4) * (const u32x4_a2*)(k + base + (size_t)pos * G * HD + dim); },
+      [&] {
+#pragma unroll
+        for (int j = 0; j < VL; ++j) {
+          const int t = threadIdx.x + j * kCopyThreads, r = t / RC, d = t % RC * 8;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) *(uint32_t*)&sv[r][d + 2 * q] = vr[j][q];
+        }
+        __syncthreads();
+      },
       [&](int pos, int dim) {
         u32x4 x;
 #pragma unroll
@@ -282,6 +288,7 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_seal_kernel(Kv8Layout kv, in
           [&](int pos, int dim) {
             return *(const u32x4*)(src + KvIndex<uint16_t>::k(w0 + pos, dim, HD, kv.ring.capacity));
           },
+          [] {},
           [&](int pos, int dim) {
             return *(const u32x4*)(src + KvIndex<uint16_t>::v(w0 + pos, dim, HD, kv.ring.capacity));
           },

@@ -33,15 +33,18 @@
 // workgroup: slow, and right.
 //
 // What bounds it.  Few rows: launches and the chains inside them (loads of the words
-// before, one counter a row): 1 x 32000 top-k 20.9 us, 16 x 128256 top-p 40 us, in
-// kernels of 5 + 14 + 4 and 5 + 12 + 13 + 10 us.  Many rows: the exponentials of rows
-// without a top-k (64-bit, 25 instructions) and the bytes: 112 x 128256 with
-// probabilities 93 us, 115 MB there and back, 1.2 TB/s.  Four workgroups a CU beat
-// eight in the first scans (34 against 40 us at 112 rows) and lose as much in the
-// last; no kernel may spill, for one that uses scratch memory starts late (scan of
-// 16 x 128256: 22 us with 16 spilled registers, 12 us with none).  One workgroup of
-// 1024 threads a row, all in one launch, was 34 us on the first (one CU issues every
-// instruction of the row) and 194 us on the last.
+// before, one counter a row): 1 x 32000, top-k 50 17.6 us, 1000 31 us (a list past 256);
+// 16 x 128256, top-p 36 us, in kernels of 5 + 12 + 10 + 9 us.  Many rows: the
+// exponentials of rows without a top-k (64-bit, 25 instructions) and the bytes.
+// 112 x 128256 with probabilities (57 MB read once, 57 MB written): top-k and top-p
+// 70 us, 1.6 TB/s; neither 93 us (read three times); top-p 123 us.
+// Four workgroups a CU beat eight in the first scans (34 against 40 us at 112 mixed
+// rows) and lose as much in the last; no kernel may spill, for one that uses scratch
+// memory starts late (scan of 16 x 128256: 22 us with 16 spilled registers, 12 us with
+// none).  One workgroup of 1024 threads a row, all in one launch, was 34 us on
+// 1 x 32000 (one CU issues every instruction of the row) and 194 us on 112 x 128256.
+// A row's chunks have at least a quad a thread: half as much left half the groups
+// empty (top-k 1000 of 32000 listed 1800 entries, not 1330).
 #include <algorithm>
 
 #include "device_common.h"
@@ -56,6 +59,7 @@ constexpr int kThreads = 256;                   //
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBuckets = 2304;                  // of distances below 44 powers of two (no mass past them)
 constexpr int kList = 4096;                     // border candidates kept in LDS
+constexpr int kPairs = kList / 2;               // with their masses
 constexpr int kGroups = 4096;                   // group maxima of a row, at most
 constexpr int kGridTarget = 1024;               // workgroups: four a CU
 constexpr int kMaxChunks = 64;                  // per row (one per lane)
@@ -634,7 +638,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
     unsigned long long key[kList];
     unsigned long long mass[kBuckets];
     uint32_t hist[256];
-    ulonglong2 pair[kThreads];
+    ulonglong2 pair[kPairs];
   } sh;
   __shared__ Select sel;
   __shared__ Gather gather;
@@ -751,7 +755,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
   if (!last_here(&work->done, w.NC)) return;
 
   const uint32_t n = get(&work->listed);
-  const bool draw = a.out && !a.probs;
+  const bool draw = a.out && !a.probs && n <= (uint32_t)kThreads;  // (longer lists: as rows without one)
   unsigned long long mass = 0, key = ~0ull;
   if (n <= (uint32_t)kThreads) {
     const int parts = parts_of(n), at = threadIdx.x / parts;
@@ -793,15 +797,24 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
   } else {
     const bool listed = n <= (uint32_t)kList;
     // The candidates among them (those that fail min_p get the key 0): f(key, mass).
+    const bool paired = n <= (uint32_t)kPairs;
     if (listed)
       for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        const unsigned long long k = get(&list[i]);
+        unsigned long long k = get(&list[i]);
         const float l = logit_of((uint32_t)(k >> 32));
-        sh.key[i] = candidate(r, l, distance(r, m, l)) ? k : 0ull;
+        const double t = distance(r, m, l);
+        if (!candidate(r, l, t)) k = 0ull;
+        if (paired) sh.pair[i] = make_ulonglong2(k, mass_at(t));
+        else sh.key[i] = k;
       }
     __syncthreads();
     auto src = [&](auto f) {
-      if (listed) {
+      if (paired) {
+        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+          const ulonglong2 p = sh.pair[i];
+          if (p.x) f(p.x, p.y);
+        }
+      } else if (listed) {
         for (uint32_t i = threadIdx.x; i < n; i += kThreads)
           if (sh.key[i]) f(sh.key[i], mass_at(distance(r, m, logit_of((uint32_t)(sh.key[i] >> 32)))));
       } else {
@@ -813,22 +826,6 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
       }
     };
     border_k(r, src, key, mass, sel);
-    if (draw) {
-      const double scale = kTwo43 / (double)mass;
-      // (the lower index first: by the low words, which hold its complement)
-      auto drawn = [&](auto f) {
-        src([&](unsigned long long k, unsigned long long) {
-          const double t = distance(r, m, logit_of((uint32_t)(k >> 32)));
-          f(k & 0xffffffffull, k < key ? 0ull : (unsigned long long)fp_weight(prob_at(t, scale)));
-        });
-      };
-      unsigned long long S = 0;
-      drawn([&](unsigned long long, unsigned long long R) { S += R; });
-      S = block_total(S, sel.sum);
-      const unsigned long long t = scale_word(row_word(a, w), S);
-      const unsigned long long at = select_border(drawn, t + 1ull, true, sel);
-      if (threadIdx.x == 0) a.out[(size_t)w.r * a.ld_out] = (int32_t)~(uint32_t)at;
-    }
   }
   if (threadIdx.x == 0) {
     work->key = key;
@@ -841,7 +838,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
 __global__ __launch_bounds__(kThreads) void rules_pick_kernel(RulesArgs a) {
   __shared__ union {
     unsigned long long key[kList];
-    ulonglong2 pair[kThreads];
+    ulonglong2 pair[kPairs];
   } sh;
   __shared__ Select sel;
   __shared__ Gather gather;
@@ -888,11 +885,21 @@ __global__ __launch_bounds__(kThreads) void rules_pick_kernel(RulesArgs a) {
     mass = sel.hi[0];
   } else {
     const bool listed = n <= (uint32_t)kList;
+    const bool paired = n <= (uint32_t)kPairs;
     if (listed)
-      for (uint32_t i = threadIdx.x; i < n; i += kThreads) sh.key[i] = get(&list[i]);
+      for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+        const unsigned long long k = get(&list[i]);
+        if (paired) sh.pair[i] = make_ulonglong2(k, mass_at(distance(r, m, logit_of((uint32_t)(k >> 32)))));
+        else sh.key[i] = k;
+      }
     __syncthreads();
     auto src = [&](auto f) {
-      if (listed) {
+      if (paired) {
+        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+          const ulonglong2 p = sh.pair[i];
+          f(p.x, p.y);
+        }
+      } else if (listed) {
         for (uint32_t i = threadIdx.x; i < n; i += kThreads)
           f(sh.key[i], mass_at(distance(r, m, logit_of((uint32_t)(sh.key[i] >> 32)))));
       } else {
@@ -1021,8 +1028,8 @@ __global__ __launch_bounds__(kThreads) void rules_out_kernel(RulesArgs a) {
   }
 }
 
-// Chunks of a row: enough workgroups for the card, at least 512 entries each.
-int chunks_of(int rows, int V) { return std::max(1, std::min({kMaxChunks, (V + 511) / 512, (kGridTarget + rows - 1) / rows})); }
+// Chunks of a row: enough workgroups for the card, at least 1024 entries each (a quad a thread).
+int chunks_of(int rows, int V) { return std::max(1, std::min({kMaxChunks, (V + 1023) / 1024, (kGridTarget + rows - 1) / rows})); }
 
 }  // namespace
 
