@@ -8,11 +8,18 @@
 // query column, so a lane holds scores of one query, and with the K rows in the
 // cache's order lane group c holds positions 8c .. 8c+7 of 32, the k order of V:
 // the probabilities feed O^T = V^T P^T from the registers they were made in,
-// and no value crosses lanes but the row maximum.  Codes become bf16 by
-// v_cvt_scalef32_pk_bf16_fp8 (exact).  Queries and probabilities are float32:
-// each enters its product as three bf16 parts (8 significant bits each, 2^-27
-// left; two parts leave 2^-18, 3.5e-6 of the result over 2048 keys against 7e-7
-// for a float32 computation, one leaves 2^-9).
+// and no value crosses lanes but the row maximum.  Queries and probabilities are
+// float32 and enter their products in parts, so that the result is as good as a
+// float32 computation's (3e-7 of it against 1e-6 for the plain form, 7B-like):
+//  - one query tile a wave (at most 64 rows a kv head): codes as bf16, times their
+//    scale (exact), three bf16 parts (8 significant bits each, 2^-27 left; two leave
+//    2^-18, 3.5e-6 of the result over 2048 keys; one leaves 2^-9).  The products are
+//    few and the stream of codes is the bound;
+//  - two tiles: codes as fp16 (exact), two fp16 parts (11 bits each) of the query row
+//    times a power of two that brings its largest to 2^13 (parts far below lose bits
+//    no float32 sum holds), and of 2^15 p.  K's scale multiplies the scores, V's goes
+//    into the conversion where the values are fp16's and into the sums where not.
+//    56 -> 49 us against three bf16 parts, which the ring's rows, bf16 values, still take.
 //
 // Work: a line of chunks of 32 or 64 keys, sequence by sequence, unit by unit (kv
 // head, query tile); workgroup i takes the i-th `per` of them, so all stream the
@@ -20,6 +27,15 @@
 // unit's segment each wave keeps (max, sum, O), then they merge in LDS.  A unit
 // inside one workgroup is finished there; otherwise each stores its part and
 // the last to count itself adds the parts.
+//
+// Measured.  7B-like (32 kv heads of 128): one row over 2048 keys 10.0 us (a chain of
+// start 3, codes and products 3, merge 1.5, parts 2.5), 16 ragged rows over 1024 to
+// 8191 keys 117 us, 5.2 TB/s of codes (reads alone reach 5.6 at this size); 512 rows
+// over 2048 keys 44 us, 343 TFLOP/s of the operator's products, twice that in the matrix
+// unit (half the time is conversions and softmax, which its products do not hide, a
+// quarter the ring's rows).  1.1B-like (4 kv heads of 64, 8 query heads each): one
+// row over 131072 keys 20.6 us, 3.3 TB/s (14 us of stream; 61 parts of one unit by one
+// workgroup 5 us), 4 x 5 rows over 301 to 1028 keys 10.0 us.
 #include <algorithm>
 
 #include "device_common.h"
@@ -49,6 +65,27 @@ __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&part)[3]) {
     part[2][j] = (__bf16)(r - (float)m);
   }
 }
+
+// v as a sum of two fp16 values (11 significant bits each).
+__device__ __forceinline__ void split8(const float (&v)[8], f16x8 (&part)[2]) {
+  u32x4 h, l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    h[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * j], v[2 * j + 1]}, f16x2));
+    float r0, r1;  // v - h (exact) without a conversion of h
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r0) : "v"(h[j]), "v"(v[2 * j]));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r1) : "v"(h[j]), "v"(v[2 * j + 1]));
+    l[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{r0, r1}, f16x2));
+  }
+  part[0] = __builtin_bit_cast(f16x8, h);
+  part[1] = __builtin_bit_cast(f16x8, l);
+}
+
+// Exponent that brings a query row, whose largest |x| has the bits m, to [2^13, 2^14).
+__device__ __forceinline__ int row_shift(uint32_t m) {
+  return m == 0u || m >= 0x7f800000u ? 0 : min(100, 13 + 127 - (int)(m >> 23));
+}
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 // Maximum over the four lane groups of 16 (the same query).
 __device__ __forceinline__ float groups_max(float v) {
@@ -119,6 +156,8 @@ template <int HD, int QT>
 struct Lds8 {
   static constexpr int KST = HD / 32, DT = HD / 16, OS = HD + 4, NW = waves_of(QT);
   bf16x8 q[QT][KST][3][kWave];
+  f16x8 qh[QT > 1 ? QT : 1][QT > 1 ? KST : 1][2][QT > 1 ? kWave : 1];
+  uint32_t row_max[QT * 16];
   union {
     u32x4 ring[QT == 1 ? 4 : 1][2 * KST + DT][kWave];
     struct {
@@ -140,6 +179,8 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
   const int window = a.f8.ring.capacity;
   const float qscale = 1.44269504088896341f / sqrtf((float)HD);  // (scores in powers of two)
   const float inv_group = 1.0f / (float)group;
+  constexpr bool F16 = QT > 1;
+  constexpr float kLift = F16 ? 15.f : 0.f;  // (probabilities are held times 2^kLift: away from fp16's least values)
 
   // One segment: chunks [k_lo, k_hi) of unit (b, g, tile), part `part` of its n.
   auto segment = [&](int b, int g, int tile, int k_lo, int k_hi, int part, int n) {
@@ -147,6 +188,10 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
     int lane = lane0;
     asm volatile("" : "+v"(lane));
     const int c16 = lane & 15, grp = lane >> 4;
+    if (F16) {
+      if (threadIdx.x < 16 * QT) sh.row_max[threadIdx.x] = 0u;
+      __syncthreads();
+    }
     // This wave's 32-dim steps of the query tiles, asked for before the length that
     // everything else needs has arrived.
     constexpr int QW = (QT * KST + NW - 1) / NW;
@@ -284,8 +329,36 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       split8(v, p3);
 #pragma unroll
       for (int k = 0; k < 3; ++k) sh.q[st / KST][st % KST][k][lane] = p3[k];
+      if constexpr (F16) {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+        atomicMax(&sh.row_max[st / KST * 16 + c16], m);
+      }
     }
     __syncthreads();
+    float qinv[QT];  // (F16: what a row's products are multiplied by)
+    if constexpr (F16) {
+#pragma unroll
+      for (int i = 0; i < QW; ++i) {
+        const int st = wave + i * NW;
+        if (st >= QT * KST) break;
+        const float up = qscale * pow2i(row_shift(sh.row_max[st / KST * 16 + c16]));
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = qv[i][0][e] * up;
+          v[4 + e] = qv[i][1][e] * up;
+        }
+        f16x8 p2[2];
+        split8(v, p2);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sh.qh[st / KST][st % KST][k][lane] = p2[k];
+      }
+#pragma unroll
+      for (int q = 0; q < QT; ++q) qinv[q] = pow2i(-row_shift(sh.row_max[q * 16 + c16]));
+      __syncthreads();
+    }
 
     floatx4 of[QT][DT];
     float mx[QT], sm[QT];
@@ -315,15 +388,15 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
           }
       }
     };
-    // The running maximum and sum of tile q over new scores, which become
+    // The running maximum and sum of tile q over new scores p f, which become
     // probabilities relative to it.  Masked: some may be -inf, all of them for a
     // query that has seen no key yet (its maximum stays -inf).
-    auto softmax = [&](int q, auto& p, bool masked) {
+    auto softmax = [&](int q, auto& p, float f, bool masked) {
       constexpr int N = sizeof(p) / sizeof(float);
       float m = fmaxf(p[0], p[1]);
 #pragma unroll
       for (int e = 2; e < N; ++e) m = fmaxf(m, p[e]);
-      m = groups_max(m);
+      m = groups_max(m) * f;
       const float mnew = fmaxf(mx[q], m);
       if (__any(mnew > mx[q])) {  // (rescaled only where a maximum rose)
         const float alpha = mx[q] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx[q] - mnew);
@@ -334,64 +407,158 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float x = __builtin_amdgcn_exp2f(p[e] - mx[q]);
+        const float x = __builtin_amdgcn_exp2f(F16 ? __builtin_fmaf(p[e], f, kLift - mx[q]) : p[e] - mx[q]);
         p[e] = masked && mx[q] == -INFINITY && p[e] == -INFINITY ? 0.f : x;
         sm[q] += p[e];
       }
     };
 
-    for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
-      float p[QT][8 * SP];
+    if constexpr (F16) {
+      for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
+        float p[QT][8 * SP], f[QT];
 #pragma unroll
-      for (int sp = 0; sp < SP; ++sp) {
-        floatx4 acc[QT][2];
-        scores(
-            [&](int t, int s) {
-              const u32x4 w = HD >= 64 ? kc[sp][t * (HD / 64) + s / 2] : kc[sp][0];
-              const int h = HD >= 64 ? s & 1 : t;
-              return fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
-            },
-            acc);
-#pragma unroll
-        for (int q = 0; q < QT; ++q)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
-      }
-      // (a wave's next K is on its way through the softmax and P V, its next V through the next scores)
-      load_k(j + NW);
-      bf16x8 pp[QT][SP][3];
-#pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        softmax(q, p[q], false);
+        for (int q = 0; q < QT; ++q) f[q] = fminf(qinv[q] * ks, 3.4028235e38f);
+        int ql = lane;
+        asm volatile("" : "+v"(ql));
+        // (a wave at its products goes before one at its softmax: 51.5 -> 48.7 us, 512 rows over 2048)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int sp = 0; sp < SP; ++sp) {
-          float v[8];
+          floatx4 acc[QT][2];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = p[q][8 * sp + e];
-          split8(v, pp[q][sp]);
-        }
-      }
-      // (DG dimension tiles in turn: a product that waits for its accumulator would leave the matrix unit idle)
-      constexpr int DG = DT < 4 ? DT : 4;
+          for (int q = 0; q < QT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int sp = 0; sp < SP; ++sp)
+          for (int s = 0; s < KST; ++s) {
+            f16x8 kk[2];
 #pragma unroll
-        for (int d0 = 0; d0 < DT; d0 += DG) {
-          bf16x8 vv[DG];
+            for (int t = 0; t < 2; ++t) {
+              const u32x4 w = HD >= 64 ? kc[sp][t * (HD / 64) + s / 2] : kc[sp][0];
+              const int h = HD >= 64 ? s & 1 : t;
+              kk[t] = fp8x8_to_f16(w[2 * h], w[2 * h + 1], 1.0f);
+            }
 #pragma unroll
-          for (int i = 0; i < DG; ++i) {
-            const u32x4 w = vc[sp][(d0 + i) / 2];
-            vv[i] = fp8x8_to_bf16(w[2 * (i & 1)], w[2 * (i & 1) + 1], vs);
+            for (int k = 1; k >= 0; --k)  // (small parts first)
+#pragma unroll
+              for (int q = 0; q < QT; ++q) {
+                const f16x8 qq = sh.qh[q][s][k][ql];
+                acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk[0], qq, acc[q][0], 0, 0, 0);
+                acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk[1], qq, acc[q][1], 0, 0, 0);
+              }
           }
 #pragma unroll
-          for (int k = 2; k >= 0; --k)
+          for (int q = 0; q < QT; ++q)
 #pragma unroll
-            for (int i = 0; i < DG; ++i)
-#pragma unroll
-              for (int q = 0; q < QT; ++q)
-                of[q][d0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[i], pp[q][sp][k], of[q][d0 + i], 0, 0, 0);
+            for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
         }
-      load_v(j + NW);
+        __builtin_amdgcn_s_setprio(0);
+        load_k(j + NW);
+        f16x8 pp[QT][SP][2];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+          softmax(q, p[q], f[q], false);
+#pragma unroll
+          for (int sp = 0; sp < SP; ++sp) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = p[q][8 * sp + e];
+            split8(v, pp[q][sp]);
+          }
+        }
+        const int ve = __builtin_amdgcn_readfirstlane((int)__float_as_uint(vs) >> 23) - 127;
+        __builtin_amdgcn_s_setprio(1);
+        if (ve >= -15 && ve <= 7) {  // (V's values are fp16's)
+          constexpr int DG = DT < 4 ? DT : 4;
+#pragma unroll
+          for (int sp = 0; sp < SP; ++sp)
+#pragma unroll
+            for (int d0 = 0; d0 < DT; d0 += DG) {
+              f16x8 vv[DG];
+#pragma unroll
+              for (int i = 0; i < DG; ++i) {
+                const u32x4 w = vc[sp][(d0 + i) / 2];
+                vv[i] = fp8x8_to_f16(w[2 * (i & 1)], w[2 * (i & 1) + 1], vs);
+              }
+#pragma unroll
+              for (int k = 1; k >= 0; --k)
+#pragma unroll
+                for (int i = 0; i < DG; ++i)
+#pragma unroll
+                  for (int q = 0; q < QT; ++q)
+                    of[q][d0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv[i], pp[q][sp][k], of[q][d0 + i], 0, 0, 0);
+            }
+        } else {  // the codes' products, times the scale
+#pragma unroll
+          for (int sp = 0; sp < SP; ++sp)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+              const u32x4 w = vc[sp][dt / 2];
+              const f16x8 vv = fp8x8_to_f16(w[2 * (dt & 1)], w[2 * (dt & 1) + 1], 1.0f);
+#pragma unroll
+              for (int q = 0; q < QT; ++q) {
+                floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 1; k >= 0; --k) x = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp][k], x, 0, 0, 0);
+                of[q][dt] += x * vs;
+              }
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        load_v(j + NW);
+      }
+    } else {
+      for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
+        float p[QT][8 * SP];
+#pragma unroll
+        for (int sp = 0; sp < SP; ++sp) {
+          floatx4 acc[QT][2];
+          scores(
+              [&](int t, int s) {
+                const u32x4 w = HD >= 64 ? kc[sp][t * (HD / 64) + s / 2] : kc[sp][0];
+                const int h = HD >= 64 ? s & 1 : t;
+                return fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
+              },
+              acc);
+#pragma unroll
+          for (int q = 0; q < QT; ++q)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
+        }
+        // (a wave's next K is on its way through the softmax and P V, its next V through the next scores)
+        load_k(j + NW);
+        bf16x8 pp[QT][SP][3];
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+          softmax(q, p[q], 1.f, false);
+#pragma unroll
+          for (int sp = 0; sp < SP; ++sp) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = p[q][8 * sp + e];
+            split8(v, pp[q][sp]);
+          }
+        }
+        // (DG dimension tiles in turn: a product that waits for its accumulator would leave the matrix unit idle)
+        constexpr int DG = DT < 4 ? DT : 4;
+#pragma unroll
+        for (int sp = 0; sp < SP; ++sp)
+#pragma unroll
+          for (int d0 = 0; d0 < DT; d0 += DG) {
+            bf16x8 vv[DG];
+#pragma unroll
+            for (int i = 0; i < DG; ++i) {
+              const u32x4 w = vc[sp][(d0 + i) / 2];
+              vv[i] = fp8x8_to_bf16(w[2 * (i & 1)], w[2 * (i & 1) + 1], vs);
+            }
+#pragma unroll
+            for (int k = 2; k >= 0; --k)
+#pragma unroll
+              for (int i = 0; i < DG; ++i)
+#pragma unroll
+                for (int q = 0; q < QT; ++q)
+                  of[q][d0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[i], pp[q][sp][k], of[q][d0 + i], 0, 0, 0);
+          }
+        load_v(j + NW);
+      }
     }
 
     if (has_ring) {
@@ -428,26 +595,33 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
             float p[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
-            softmax(q, p, true);
+            softmax(q, p, 1.f, true);
             bf16x8 pp[3];
             split8(p, pp);
+            constexpr int DG = DT < 4 ? DT : 4;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              u32x4 v = QT == 1 ? rows[RK + dt][lane] : rv[QT == 1 ? 0 : dt];
-              if (diagonal) {
+            for (int d0 = 0; d0 < DT; d0 += DG) {
+              u32x4 v[DG];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  if (2 * w >= nvalid) v[w] = 0u;
-                  else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
-                  const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
-                  odd |= lo || up;
-                  if (lo) v[w] &= 0xffff0000u;
-                  if (up) v[w] &= 0xffffu;
+              for (int i = 0; i < DG; ++i) {
+                v[i] = QT == 1 ? rows[RK + d0 + i][lane] : rv[QT == 1 ? 0 : d0 + i];
+                if (diagonal) {
+#pragma unroll
+                  for (int w = 0; w < 4; ++w) {
+                    if (2 * w >= nvalid) v[i][w] = 0u;
+                    else if (2 * w + 1 >= nvalid) v[i][w] &= 0xffffu;
+                    const bool lo = (v[i][w] & 0x7f80u) == 0x7f80u, up = (v[i][w] & 0x7f800000u) == 0x7f800000u;
+                    odd |= lo || up;
+                    if (lo) v[i][w] &= 0xffff0000u;
+                    if (up) v[i][w] &= 0xffffu;
+                  }
                 }
               }
 #pragma unroll
               for (int k = 2; k >= 0; --k)
-                of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pp[k], of[q][dt], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < DG; ++i)
+                  of[q][d0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[i]), pp[k], of[q][d0 + i], 0, 0, 0);
             }
             if (diagonal && __any(odd)) {
               for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
@@ -600,8 +774,10 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
     const int b = blockIdx.z, u = blockIdx.y, part = blockIdx.x;
     const int nb = __builtin_amdgcn_readfirstlane(chunks_of<chunk_of(HD)>(a, b)), k_lo = part * per0;
     if (k_lo >= nb) return;  // (workgroup-uniform)
-    const int g = u / n_tiles;
-    segment(b, g, u - g * n_tiles, k_lo, min(nb, k_lo + per0), part, (nb + per0 - 1) / per0);
+    // (kv heads first, so that an XCD's workgroups read few of them; later tiles, which see
+    // more, beside earlier ones)
+    const int t = u / G, half = (n_tiles + 1) / 2;
+    segment(b, u - t * G, t < half ? n_tiles - 1 - t : t - half, k_lo, min(nb, k_lo + per0), part, (nb + per0 - 1) / per0);
   } else {
     const int B = a.M / rps, U = G * n_tiles;
     const int n0 = lane0 < B ? chunks_of<chunk_of(HD)>(a, lane0) : 0;  // (the first 64 sequences stay in a register)
@@ -638,7 +814,10 @@ Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int 
   p.n_tiles = (nq + 16 * p.qt - 1) / (16 * p.qt);
   const long nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim), units = (long)n_kv_heads * p.n_tiles;
   const long slots = 2L * device_compute_units();  // workgroups resident at once
-  const long per = std::max((nb * units * batch + slots - 1) / slots, (nb + kPartsMax8 - 3) / (kPartsMax8 - 2));
+  // (at least a chunk a wave: fewer parts to add.  Half a chunk was 12.9 us, one 10.4 us,
+  // two 11.4 us for a row over 2048 keys of 32 heads)
+  const long per = std::max({(nb * units * batch + slots - 1) / slots, (nb + kPartsMax8 - 3) / (kPartsMax8 - 2),
+                             (long)waves_of(p.qt)});
   // Several sequences of unlike lengths and more than four chunks a wave: the line.
   p.line = batch > 1 && per > 4 * waves_of(p.qt);
   p.per = (int)(p.line ? (nb + kPartsMax8 - 3) / (kPartsMax8 - 2) : per);

@@ -6,6 +6,9 @@
 namespace specdec {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));  // (callers' rows: bf16 alignment)
 
 // 8 e4m3 codes (four in each word, low byte first) times the power of two
@@ -17,6 +20,16 @@ __device__ __forceinline__ bf16x8 fp8x8_to_bf16(uint32_t lo, uint32_t hi, float 
   o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
   o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
   return __builtin_bit_cast(bf16x8, o);
+}
+
+// The same in fp16: exact where scale is 2^-15 .. 2^7 (codes: 0, 2^-9 .. 448).
+__device__ __forceinline__ f16x8 fp8x8_to_f16(uint32_t lo, uint32_t hi, float scale) {
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true));
+  return __builtin_bit_cast(f16x8, o);
 }
 
 }  // namespace specdec

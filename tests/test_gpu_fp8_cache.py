@@ -238,6 +238,64 @@ def test_attention(case):
     assert kv.read_state()["status"] == 0
 
 
+# Ragged batches whose keys make more than four chunks a wave: workgroups take
+# their share of all of them, not of one sequence's.
+LINES = [  # hd, H, G, lens, n, window
+    (32, 8, 8, [61000, 1, 30011], 1, 128),
+    (64, 8, 4, [0, 131000, 60000, 129], 2, 128),
+    (64, 32, 4, [40000, 40001, 63, 12345], 5, 128),
+    (128, 4, 4, [9000, 50, 4000], 80, 192),
+    (64, 4, 2, [20000, 0, 700], 70, 192),
+    (32, 4, 4, [20000, 3, 20001], 66, 192),
+]
+
+
+@pytest.mark.parametrize("case", LINES, ids=lambda c: f"hd{c[0]}-{c[1]}:{c[2]}-len{max(c[3])}-n{c[4]}")
+def test_attention_long_ragged_batches(case):
+    hd, H, G, lens, n, window = case
+    log(f"long ragged {case}")
+    rng = np.random.default_rng(sum(lens) + n + hd)
+    kv = _cache(_shape(hd, H, G, 1), len(lens), (max(lens) + n + 63) // 64 * 64, window)
+    kvs = _fill(kv, rng, lens, n, G, hd)
+    q = rng.normal(0, 1.5, (len(lens), n, H, hd)).astype(np.float32)
+    log(f"worst error {_check(_attend(kv, q), q, kvs, lens, sorted({0, n // 2, n - 1})):.3g}")
+    assert kv.read_state()["status"] == 0
+
+
+@pytest.mark.parametrize("hd,G", [(32, 2), (64, 1), (128, 2)])
+@pytest.mark.parametrize("k_mag,v_mag", [(0, 0), (0, -24), (0, 40), (60, 5), (-60, -100), (0, None)])
+def test_wide_calls_of_every_magnitude(hd, G, k_mag, v_mag):
+    """Many rows a kv head (their products are of fp16 parts): keys, values and queries
+    far from 1, values that change their scale from block to block (None), queries of
+    zero and of unlike magnitudes in one tile."""
+    rng = np.random.default_rng(hd + G)
+    L, n, H, window = 333, 70, 2 * G, 192
+    kv = _cache(_shape(hd, H, G, 1), 1, 448, window)
+    k = _np(_bf16(rng.normal(0, 1.3, (L + n, G, hd)) * 2.0 ** k_mag))
+    v = rng.normal(0, 1.3, (L + n, G, hd))
+    v *= 2.0 ** rng.integers(-20, 20, (-(-(L + n) // 64), 1, 1)).repeat(64, 0)[:L + n] if v_mag is None else 2.0 ** v_mag
+    v = _np(_bf16(v))
+    kv.write_context(0, 0, 0, _bf16(k[:L]), _bf16(v[:L]))
+    kv.set_state([L], [[0, 1]], [1])
+    binding.specdec_kv_append(kv, 0, _bf16(k[None, L:]), _bf16(v[None, L:]))
+    kvs = [[fp8.stored(k, L // 64 * 64), fp8.stored(v, L // 64 * 64)]]
+    q = rng.normal(0, 1.5, (1, n, H, hd)) * 2.0 ** -k_mag
+    q[0, 3] = 0
+    q[0, 4] *= 2.0 ** -40
+    q[0, 5] *= 2.0 ** 6
+    q = q.astype(np.float32)
+    log(f"magnitudes hd={hd} k 2^{k_mag} v 2^{v_mag}")
+    got = _attend(kv, q)
+    log(f"worst error {_check(got, q, kvs, [L]):.3g}")
+    # a row that is not finite is its own affair
+    q[0, 6, 0, 1] = np.inf
+    q[0, 7, 1, 2] = np.nan
+    again = _attend(kv, q)
+    assert not np.isfinite(again[0, 6, 0]).any() and np.isnan(again[0, 7, 1]).all()
+    again[0, 6, 0], again[0, 7, 1] = got[0, 6, 0], got[0, 7, 1]
+    np.testing.assert_array_equal(again, got)
+
+
 def test_attention_many_sequences():
     """More sequences than a wave has lanes, of lengths that share workgroups."""
     rng = np.random.default_rng(11)
