@@ -33,13 +33,13 @@
 // workgroup: slow, and right.
 //
 // What bounds it.  Few rows: launches and the chains inside them (loads of the words
-// before, one counter a row): 1 x 32000, top-k 50 17.6 us, 1000 31 us (a list past 256);
-// 16 x 128256, top-p 36 us, in kernels of 5 + 12 + 10 + 9 us.  Many rows: the
+// before, one counter a row): 1 x 32000, top-k 50 17.4 us, 1000 30 us (a list past 256);
+// 16 x 128256, top-p 35 us, in kernels of 5 + 12 + 10 + 9 us.  Many rows: the
 // exponentials of rows without a top-k (64-bit, 25 instructions) and the bytes.
 // 112 x 128256 with probabilities (57 MB read once, 57 MB written): top-k and top-p
-// 70 us, 1.6 TB/s; neither 93 us (read three times); top-p 123 us.
-// Four workgroups a CU beat eight in the first scans (34 against 40 us at 112 mixed
-// rows) and lose as much in the last; no kernel may spill, for one that uses scratch
+// 62 us, 1.9 TB/s; neither 87 us (read three times); top-p 116 us.
+// Six workgroups a CU (kGridTarget): with four the scan of 112 mixed rows is 32 us, not
+// 35, but the last launch 33, not 28.  No kernel may spill, for one that uses scratch
 // memory starts late (scan of 16 x 128256: 22 us with 16 spilled registers, 12 us with
 // none).  One workgroup of 1024 threads a row, all in one launch, was 34 us on
 // 1 x 32000 (one CU issues every instruction of the row) and 194 us on 112 x 128256.
@@ -61,7 +61,7 @@ constexpr int kBuckets = 2304;                  // of distances below 44 powers 
 constexpr int kList = 4096;                     // border candidates kept in LDS
 constexpr int kPairs = kList / 2;               // with their masses
 constexpr int kGroups = 4096;                   // group maxima of a row, at most
-constexpr int kGridTarget = 1024;               // workgroups: four a CU
+constexpr int kGridTarget = 1536;               // workgroups: six a CU
 constexpr int kMaxChunks = 64;                  // per row (one per lane)
 constexpr int kSegments = kRulesMaxVocab / 256 + 2 * kMaxChunks;  // of a row (a chunk's last may be short)
 constexpr double kTwo43 = 8796093022208.0;
@@ -325,12 +325,14 @@ __device__ __forceinline__ uint32_t wave_bound(const uint32_t (&v)[E], int k) {
 }
 
 // ---------------------------------------------------------------- max
-// Lanes to a group of a row with a top-k: at most kGroups groups, and not many
-// more than 4 k (G groups leave G ln(G / (G - k)) entries above their k-th largest
-// maximum where the logits' order is random: 1.15 k at G = 4 k).
+// Groups of a row with a top-k, at most: one, four or sixteen maxima a thread of the
+// scan.  (G groups leave G ln(G / (G - k)) entries above their k-th largest maximum
+// where the logits' order is random: 1.15 k at G = 4 k, 1.4 k at 2 k.)
+__host__ __device__ __forceinline__ int group_limit(int k) { return k <= 64 ? kThreads : k <= 256 ? 4 * kThreads : kGroups; }
+// Lanes to a group.
 __host__ __device__ __forceinline__ int group_lanes(int NC, int k) {
   int n = 1;
-  while (n < kWave && (NC * kThreads / n > kGroups || NC * kThreads / (2 * n) >= max(4 * k, 256))) n *= 2;
+  while (n < kWave && NC * kThreads / n > group_limit(k)) n *= 2;
   return n;
 }
 __global__ __launch_bounds__(kThreads) void rules_max_kernel(RulesArgs a) {
@@ -395,8 +397,9 @@ __device__ __forceinline__ ChunkMax row_max(const ChunkMax* parts, int NC) {
 }
 
 // ---------------------------------------------------------------- selection
+constexpr int kFew = 128;
 struct Select {
-  unsigned long long hist_m[256];
+  alignas(16) unsigned long long hist_m[2 * kFew];
   uint32_t hist_c[256];
   unsigned long long sum[kWaves], lo[kWaves], hi[kWaves];
   int digit;
@@ -424,10 +427,37 @@ __device__ __forceinline__ void block_extremes(unsigned long long& lo, unsigned 
   }
 }
 
+// At most a workgroup's width of entries, by 1, 2 or 4 threads an entry (`parts`;
+// thread t: entry t / parts): how many of them come before `key`, and their mass.
+// pair: {key, mass}, zeros behind the last up to a multiple of 8.
+__device__ __forceinline__ int parts_of(int n) { return 4 * n <= kThreads ? 4 : 2 * n <= kThreads ? 2 : 1; }
+__device__ __forceinline__ int rank_pairs(const ulonglong2* pair, int n, int parts, unsigned long long key,
+                                          unsigned long long& before) {
+  int rank = 0;
+  before = 0;
+  for (int i = 8 * (threadIdx.x & (parts - 1)); i < n; i += 8 * parts) {
+    ulonglong2 p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = pair[i + e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool first = p[e].x > key;
+      rank += first;
+      before += first ? p[e].y : 0ull;
+    }
+  }
+  for (int o = 1; o < parts; o <<= 1) {
+    rank += __shfl_xor(rank, o, kWave);
+    before += (unsigned long long)__shfl_xor(before, o, kWave);
+  }
+  return rank;
+}
+
 // The key of the last kept when the first `rest` of src's entries (by_mass: the
 // fewest whose mass reaches `rest`) are kept, larger keys first.  src(f):
 // f(key, mass) for every entry, keys distinct.  Radix selection from the highest bit
-// in which the keys differ, 8 bits a pass, until one entry is left.
+// in which the keys differ, 8 bits a pass, until few entries share the prefix: these
+// are ranked.
 template <typename SRC>
 __device__ __forceinline__ unsigned long long select_border(SRC src, unsigned long long rest, bool by_mass, Select& sh) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -482,12 +512,22 @@ __device__ __forceinline__ unsigned long long select_border(SRC src, unsigned lo
     rest -= sh.before;
     prefix |= (unsigned long long)sh.digit << shift;
     top = shift;
-    if (sh.left == 1u) break;
+    if (sh.left <= (uint32_t)kFew) break;
   }
-  // the one entry that is left
-  src([&](unsigned long long key, unsigned long long) {
-    if (top >= 64 || (key >> top) == (prefix >> top)) sh.result = key;
+  // the entries that share the prefix, in the histogram's place
+  ulonglong2* few = (ulonglong2*)sh.hist_m;
+  if (threadIdx.x < kFew) few[threadIdx.x] = make_ulonglong2(0ull, 0ull);
+  if (threadIdx.x == 0) sh.left = 0u;
+  __syncthreads();
+  src([&](unsigned long long key, unsigned long long m) {
+    if (top >= 64 || (key >> top) == (prefix >> top)) few[atomicAdd(&sh.left, 1u)] = make_ulonglong2(key, by_mass ? m : 1ull);
   });
+  __syncthreads();
+  const int n = (int)sh.left, parts = parts_of(n), at = threadIdx.x / parts;
+  const ulonglong2 own = at < n ? few[at] : make_ulonglong2(0ull, 0ull);
+  unsigned long long before;
+  rank_pairs(few, n, parts, own.x, before);
+  if (before < rest && rest <= before + own.y) sh.result = own.x;  // (one entry)
   __syncthreads();
   return sh.result;
 }
@@ -587,32 +627,6 @@ __device__ __forceinline__ void store4(float* p, int j, int end, const float (&v
     for (int e = 0; j + e < end; ++e) p[j + e] = v[e];
 }
 
-// The same without passes for at most a workgroup's width of entries, by 1, 2 or 4
-// threads an entry (`parts`; thread t: entry t / parts): how many of them come before
-// `key`, and their mass.  pair: {key, mass}, kThreads of them, zeros behind the last.
-__device__ __forceinline__ int parts_of(int n) { return 4 * n <= kThreads ? 4 : 2 * n <= kThreads ? 2 : 1; }
-__device__ __forceinline__ int rank_pairs(const ulonglong2* pair, int n, int parts, unsigned long long key,
-                                          unsigned long long& before) {
-  int rank = 0;
-  before = 0;
-  for (int i = 8 * (threadIdx.x & (parts - 1)); i < n; i += 8 * parts) {
-    ulonglong2 p[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = pair[i + e];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool first = p[e].x > key;
-      rank += first;
-      before += first ? p[e].y : 0ull;
-    }
-  }
-  for (int o = 1; o < parts; o <<= 1) {
-    rank += __shfl_xor(rank, o, kWave);
-    before += (unsigned long long)__shfl_xor(before, o, kWave);
-  }
-  return rank;
-}
-
 // A row's list.  Entries go to the workgroup's own first (LDS), then with one
 // reservation to the row's.
 struct Gather {
@@ -630,6 +644,20 @@ __device__ __forceinline__ void gather_flush(Gather& g, const unsigned long long
   __syncthreads();
   const uint32_t at = g.at;
   for (uint32_t i = threadIdx.x; i < min(n, (uint32_t)kList) && at + i < (uint32_t)kList; i += kThreads) put(&list[at + i], keys[i]);
+}
+
+// f(i, key) for the row's list, its loads in flight eight at a time.
+template <typename F>
+__device__ __forceinline__ void read_list(const unsigned long long* list, uint32_t n, F f) {
+  constexpr int E = 8;
+  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += E * kThreads) {
+    unsigned long long k[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) k[e] = get(&list[min(i0 + e * kThreads, n - 1)]);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (i0 + e * kThreads < n) f(i0 + e * kThreads, k[e]);
+  }
 }
 
 // ---------------------------------------------------------------- scan
@@ -662,19 +690,15 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
     // every fourth group maximum, and the least of these (fewer groups than k: none).
     const int n = w.NC * kThreads / group_lanes(w.NC, r.k), k = (r.k + kWaves - 1) / kWaves, at0 = lane * kWaves + wv;
     uint32_t bound = 0u;
-    if (n < r.k + kWaves) {
-    } else if (n <= kThreads) {
-      const uint32_t v[1] = {at0 < n ? first : 0u};
-      bound = wave_bound(v, k);
-    } else {
-      uint32_t v[kGroups / kThreads];
+    auto of = [&](auto& v) {
+      constexpr int E = sizeof(v) / sizeof(uint32_t);
+      v[0] = at0 < n ? first : 0u;
 #pragma unroll
-      for (int i = 0; i < kGroups / kThreads; ++i) {
-        const int at = i * kThreads + at0;
-        v[i] = at < n ? group[at] : 0u;
-      }
-      bound = wave_bound(v, k);
-    }
+      for (int i = 1; i < E; ++i) v[i] = i * kThreads + at0 < n ? group[i * kThreads + at0] : 0u;
+      return wave_bound(v, k);
+    };
+    uint32_t v1[1], v4[4], v16[kGroups / kThreads];
+    if (n >= r.k + kWaves) bound = n <= kThreads ? of(v1) : n <= 4 * kThreads ? of(v4) : of(v16);
     if (lane == 0) s_row.bound[wv] = bound;
   }
   if (wv == 0) {
@@ -799,14 +823,13 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
     // The candidates among them (those that fail min_p get the key 0): f(key, mass).
     const bool paired = n <= (uint32_t)kPairs;
     if (listed)
-      for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        unsigned long long k = get(&list[i]);
+      read_list(list, n, [&](uint32_t i, unsigned long long k) {
         const float l = logit_of((uint32_t)(k >> 32));
         const double t = distance(r, m, l);
         if (!candidate(r, l, t)) k = 0ull;
         if (paired) sh.pair[i] = make_ulonglong2(k, mass_at(t));
         else sh.key[i] = k;
-      }
+      });
     __syncthreads();
     auto src = [&](auto f) {
       if (paired) {
@@ -887,11 +910,10 @@ __global__ __launch_bounds__(kThreads) void rules_pick_kernel(RulesArgs a) {
     const bool listed = n <= (uint32_t)kList;
     const bool paired = n <= (uint32_t)kPairs;
     if (listed)
-      for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        const unsigned long long k = get(&list[i]);
+      read_list(list, n, [&](uint32_t i, unsigned long long k) {
         if (paired) sh.pair[i] = make_ulonglong2(k, mass_at(distance(r, m, logit_of((uint32_t)(k >> 32)))));
         else sh.key[i] = k;
-      }
+      });
     __syncthreads();
     auto src = [&](auto f) {
       if (paired) {
