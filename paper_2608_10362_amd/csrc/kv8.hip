@@ -4,7 +4,12 @@
 //
 // All are copies: the bound is the stream of bytes.  A block of 64 positions of
 // one kv head is one workgroup's: its K and V pass through registers once
-// (their maximum, then the codes).
+// (their maximum, then the codes).  V changes from rows to operand order in LDS,
+// K's operand order is that of its rows' pieces; the write asks for K before it
+// waits for V (16.0 -> 15.0 us at 2048 positions of 32 heads of 128).
+// 32745 positions of that shape: write 190 us, read 185 us, 805 MB each, 4.3 TB/s
+// (a copy of that size: 5.2).  Nontemporal rows in: write 165 us, the read after it
+// 195; nontemporal rows out: read 296 us; so all accesses are plain ones.
 #include <algorithm>
 
 #include "device_common.h"
