@@ -290,11 +290,13 @@ SPECDEC_API specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* s
  * row i of sequence b at position len[b] + i, seeing keys 0 .. len[b]+i (the
  * last ones appended, not committed); query head h reads kv head
  * h / (n_heads / n_kv_heads).  out, same shape, float32:
- * softmax(q k^T / sqrt(head_dim)) v, the sums in float32.  A key or value row
- * with a NaN or infinity affects the rows that see it and no others.
+ * softmax(q k^T / sqrt(head_dim)) v, the sums in float32; out may be q.  A key or
+ * value row with a NaN or infinity affects the rows that see it and no others.
  * workspace: specdec_attention_workspace_bytes bytes (0 for arguments the call
  * rejects), 256-byte aligned, dead after the call; calls that share one must be
- * ordered on one stream (graphs captured with one, replayed in order).
+ * ordered on one stream (graphs captured with one, replayed in order).  So must
+ * calls on one cache, whatever their workspaces: the count of finished parts is
+ * kept in its data.
  * Graph capture: sized from kv->len_upper, as the passes are (see above).
  * Asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (other caches), SHAPE
  * (n_heads not a multiple of n_kv_heads or above 128 times it, n > window -

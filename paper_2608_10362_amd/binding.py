@@ -428,6 +428,7 @@ class Fp8KVCache(KVCache):
         if nbytes == 0:
             raise SpecdecError(-2, "specdec_kv_bytes_fp8")
         self.data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _on_current(self.data, "device", torch.uint8)
         self.state = torch.zeros(lib().specdec_kv_state_count(batch), dtype=torch.int32, device=device)
         self.kv = KV()
         _check(lib().specdec_kv_init_fp8(ctypes.byref(self.kv), ctypes.byref(desc), n_layers, batch, capacity, window,
@@ -522,6 +523,7 @@ def specdec_kv_append(kv: KVCache, layer: int, k, v, stream=None):
     shp = (kv.batch, k.shape[1] if k.dim() == 4 else 0, kv.kv.n_kv_heads, kv.kv.head_dim)
     for name, t in (("k", k), ("v", v)):
         _on_current(t, name, torch.bfloat16)
+        _same_device(kv.data, "kv", t)
         if tuple(t.shape) != shp or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous [batch, n, {shp[2]}, {shp[3]}] tensor of one shape")
     _check(lib().specdec_kv_append(ctypes.byref(kv.kv), layer, shp[1], k.data_ptr(), v.data_ptr(), _stream(stream)),
@@ -542,8 +544,9 @@ def attention_workspace(kv: KVCache, n_heads: int, n: int):
 
 
 def specdec_attention(kv: KVCache, layer: int, q, out, workspace=None, stream=None):
-    """q, out: device float32 [batch, n, n_heads, head_dim].  `workspace` (from
-    attention_workspace) is allocated per call when not given."""
+    """q, out: device float32 [batch, n, n_heads, head_dim] (out may be q).
+    `workspace` (from attention_workspace) is allocated per call when not given.
+    Calls on one cache must be ordered on one stream."""
     import torch
     if q.dim() != 4 or q.shape[0] != kv.batch or q.shape[3] != kv.kv.head_dim or out.shape != q.shape:
         raise ValueError("q, out: expected [batch, n, n_heads, head_dim]")
@@ -551,6 +554,7 @@ def specdec_attention(kv: KVCache, layer: int, q, out, workspace=None, stream=No
         _on_current(t, name, torch.float32)
         if not t.is_contiguous():
             raise ValueError(f"{name}: must be contiguous")
+    _same_device(kv.data, "kv", q)
     n, n_heads = q.shape[1], q.shape[2]
     if workspace is None:
         workspace = attention_workspace(kv, n_heads, n)

@@ -780,12 +780,19 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
     segment(b, u - t * G, t < half ? n_tiles - 1 - t : t - half, k_lo, min(nb, k_lo + per0), part, (nb + per0 - 1) / per0);
   } else {
     const int B = a.M / rps, U = G * n_tiles;
-    const int n0 = lane0 < B ? chunks_of<chunk_of(HD)>(a, lane0) : 0;  // (the first 64 sequences stay in a register)
-    int total = 0;
-    for (int c = 0; c < B; c += kWave) total += lane_sum(c == 0 ? n0 : (c + lane0 < B ? chunks_of<chunk_of(HD)>(a, c + lane0) : 0));
+    // (64 sequences' chunks at a time in a register)
+    auto some = [&](int c) { return c + lane0 < B ? chunks_of<chunk_of(HD)>(a, c + lane0) : 0; };
+    int n64 = some(0), at64 = 0, total = lane_sum(n64);
+    for (int c = kWave; c < B; c += kWave) total += lane_sum(some(c));
     total *= U;
     const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, per0);
-    auto subs = [&](int s) { return s < kWave ? __builtin_amdgcn_readlane(n0, s) : __builtin_amdgcn_readfirstlane(chunks_of<chunk_of(HD)>(a, s)); };
+    auto subs = [&](int s) {
+      if ((s & ~(kWave - 1)) != at64) {
+        at64 = s & ~(kWave - 1);
+        n64 = some(at64);
+      }
+      return __builtin_amdgcn_readlane(n64, s & (kWave - 1));
+    };
     int x = (int)blockIdx.x * per;
     const int hi = min(total, x + per);
     int b = 0, base = 0, nb = subs(0);  // the sequence that holds x; base: the line where it starts

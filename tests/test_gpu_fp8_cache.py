@@ -247,6 +247,7 @@ LINES = [  # hd, H, G, lens, n, window
     (128, 4, 4, [9000, 50, 4000], 80, 192),
     (64, 4, 2, [20000, 0, 700], 70, 192),
     (32, 4, 4, [20000, 3, 20001], 66, 192),
+    (32, 2, 2, [(977 * i) % 8000 for i in range(150)], 1, 128),
 ]
 
 
@@ -260,6 +261,21 @@ def test_attention_long_ragged_batches(case):
     q = rng.normal(0, 1.5, (len(lens), n, H, hd)).astype(np.float32)
     log(f"worst error {_check(_attend(kv, q), q, kvs, lens, sorted({0, n // 2, n - 1})):.3g}")
     assert kv.read_state()["status"] == 0
+
+
+@pytest.mark.parametrize("n", [1, 5, 100])
+def test_attention_in_place(n):
+    """out may be q: a unit's rows are stored when all its parts have read them."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(n)
+    lens = [3000, 40]
+    kv = _cache(_shape(64, 8, 2, 1), 2, 3136, 192)
+    _fill(kv, rng, lens, n, 2, 64)
+    q = rng.normal(0, 1.5, (2, n, 8, 64)).astype(np.float32)
+    want = _attend(kv, q)
+    x = torch.from_numpy(q).cuda()
+    binding.specdec_attention(kv, 0, x, x)
+    np.testing.assert_array_equal(x.cpu().numpy(), want)
 
 
 @pytest.mark.parametrize("hd,G", [(32, 2), (64, 1), (128, 2)])
