@@ -1167,7 +1167,7 @@ specdec_status specdec_sample(int32_t batch, int32_t vocab, const float* probs, 
 
 size_t specdec_sample_logits_workspace_bytes(int32_t batch, int32_t rows, int32_t vocab) {
   if (check_rules(batch, rows, vocab) != SPECDEC_OK) return 0;
-  return rules_scratch_bytes(batch * rows);
+  return rules_scratch_bytes(batch * rows, vocab);
 }
 
 specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab, const float* logits, int64_t ld,
@@ -1179,7 +1179,7 @@ specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab,
   if (st != SPECDEC_OK) return st;
   if (!logits || ld < vocab || (!probs && !out) || (probs && ld_probs < vocab) || (out && ld_out < 1) ||
       misaligned8(step_dev) || purpose < 0 || purpose > 0xffff || index < 0 || index > 0xffff - (rows - 1) ||
-      !workspace || (uintptr_t)workspace % kAlign || workspace_bytes < rules_scratch_bytes(batch * rows))
+      !workspace || (uintptr_t)workspace % kAlign || workspace_bytes < rules_scratch_bytes(batch * rows, vocab))
     return SPECDEC_ERR_INVALID_ARG;
   if (probs) {  // (the draw reads logits again after other workgroups have stored probabilities)
     const int64_t n = (int64_t)batch * rows - 1;

@@ -355,7 +355,7 @@ hipError_t launch_commit(const CommitArgs& a, hipStream_t s);
 
 // Sampling rules (rules.hip).
 constexpr int kRulesMaxVocab = 1 << 20;  // (integer masses of 43 bits: their sums stay below 2^63)
-size_t rules_scratch_bytes(int n_rows);
+size_t rules_scratch_bytes(int n_rows, int V);
 struct RulesArgs {
   int B, rows, V;
   const float* logits;
@@ -373,7 +373,7 @@ struct RulesArgs {
   int32_t* out;              // or null
   int64_t ld_out;
   int32_t* status;
-  void* scratch;             // rules_scratch_bytes(B * rows)
+  void* scratch;             // rules_scratch_bytes(B * rows, V)
 };
 hipError_t launch_rules(const RulesArgs& a, hipStream_t s);
 

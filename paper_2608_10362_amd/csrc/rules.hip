@@ -63,7 +63,6 @@ constexpr int kPairs = kList / 2;               // with their masses
 constexpr int kGroups = 4096;                   // group maxima of a row, at most
 constexpr int kGridTarget = 1536;               // workgroups: six a CU
 constexpr int kMaxChunks = 64;                  // per row (one per lane)
-constexpr int kSegments = kRulesMaxVocab / 256 + 2 * kMaxChunks;  // of a row (a chunk's last may be short)
 constexpr double kTwo43 = 8796093022208.0;
 
 enum { ROW_GREEDY = 1, ROW_BAD = 2, ROW_ALL = 3, ROW_K = 4, ROW_P = 5 };
@@ -100,27 +99,44 @@ struct RowWork {
 };
 static_assert(sizeof(RowWork) == 256, "two lines a row");
 
+// Buckets to a power of two over the first 16 of them, 8 to one from there: few,
+// for each workgroup adds all of its own to the row's; enough that the border's,
+// 0.4 V ln 2 / rate entries where the logits are normal and T is their deviation,
+// goes into the list.
+__host__ __device__ __forceinline__ int bucket_rate(int V) { return V <= 262144 ? 32 : 128; }
+__host__ __device__ __forceinline__ int buckets_of(int rate) { return 16 * rate + 28 * 8; }
+static_assert(16 * 128 + 28 * 8 <= kBuckets, "every rate's buckets");
+
+// Rows' arrays, strides by the call's rows, vocabulary and chunks a row (NC).
 struct RuleScratch {
-  ChunkMax* cmax;              // [rows][kMaxChunks]
-  unsigned long long* draw;    // [rows][kSegments] weights of the draw in 256 consecutive entries of a chunk
+  ChunkMax* cmax;              // [rows][NC]
+  unsigned long long* draw;    // [rows][segments_of(V)] weights of the draw in 256 consecutive entries of a chunk
   RowWork* work;               // [rows]
-  unsigned long long* mass;    // [rows][kBuckets]
-  uint32_t* group;             // [rows][kGroups] ordered group maxima
-  float* top;                  // [rows][kMaxChunks][kThreads] maximum of each thread's entries
-  unsigned long long* list;    // [rows][kList]
+  unsigned long long* mass;    // [rows][buckets_of(V's rate)]
+  uint32_t* group;             // [rows][groups_of(NC)] ordered group maxima
+  float* top;                  // [rows][NC][kThreads] maximum of each thread's entries
+  unsigned long long* list;    // [rows][list_of(V)]
 };
+// (a chunk's last segment may be short)
+__host__ __device__ __forceinline__ int segments_of(int V) { return (V + 255) / 256 + 2 * kMaxChunks; }
+__host__ __device__ __forceinline__ int groups_of(int NC) { return NC * kThreads < kGroups ? NC * kThreads : kGroups; }
+__host__ __device__ __forceinline__ int list_of(int V) { return V < kList ? V : kList; }
 __host__ __device__ inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-__host__ __device__ inline size_t carve_rules(void* base, size_t rows, RuleScratch* s) {
+// Grows with rows and V: a workspace of the largest call holds every call's.
+__host__ __device__ inline size_t carve_rules(void* base, size_t rows, int V, RuleScratch* s) {
   size_t off = 0;
   char* p = (char*)base;
   auto take = [&](size_t n) { const size_t at = off; off = up256(off + n); return p + at; };
-  s->cmax = (ChunkMax*)take(rows * kMaxChunks * sizeof(ChunkMax));
-  s->draw = (unsigned long long*)take(rows * kSegments * 8);
+  // (chunks of all rows together: rows * ceil(kGridTarget / rows) at most)
+  const size_t most = rows + kGridTarget - 1, chunks = rows * kMaxChunks < most ? rows * kMaxChunks : most;
+  const size_t groups = rows * kGroups < chunks * kThreads ? rows * kGroups : chunks * kThreads;
+  s->cmax = (ChunkMax*)take(chunks * sizeof(ChunkMax));
+  s->draw = (unsigned long long*)take(rows * segments_of(V) * 8);
   s->work = (RowWork*)take(rows * sizeof(RowWork));
-  s->mass = (unsigned long long*)take(rows * kBuckets * 8);
-  s->group = (uint32_t*)take(rows * kGroups * 4);
-  s->top = (float*)take(rows * kMaxChunks * kThreads * 4);
-  s->list = (unsigned long long*)take(rows * kList * 8);
+  s->mass = (unsigned long long*)take(rows * buckets_of(bucket_rate(V)) * 8);
+  s->group = (uint32_t*)take(groups * 4);
+  s->top = (float*)take(chunks * kThreads * 4);
+  s->list = (unsigned long long*)take(rows * list_of(V) * 8);
   return off;
 }
 
@@ -187,13 +203,6 @@ __device__ __forceinline__ unsigned long long mass_at(double t) {
   const double x = floor(pow2_neg(t) * kTwo43) + 4503599627370496.0;
   return (unsigned long long)__double_as_longlong(x) & 0xfffffffffffffull;
 }
-// Buckets to a power of two over the first 16 of them, 8 to one from there: few,
-// for each workgroup adds all of its own to the row's; enough that the border's,
-// 0.4 V ln 2 / rate entries where the logits are normal and T is their deviation,
-// goes into the list.
-__host__ __device__ __forceinline__ int bucket_rate(int V) { return V <= 262144 ? 32 : 128; }
-__host__ __device__ __forceinline__ int buckets_of(int rate) { return 16 * rate + 28 * 8; }
-static_assert(16 * 128 + 28 * 8 <= kBuckets, "every rate's buckets");
 __device__ __forceinline__ int bucket_of(double t, int rate) {  // (rounding keeps the order; t < 44)
   const float x = (float)t;
   return x < 16.f ? (int)(x * (float)rate) : min(16 * rate + (int)((x - 16.f) * 8.f), buckets_of(rate) - 1);
@@ -339,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void rules_max_kernel(RulesArgs a) {
   __shared__ float sm[kWaves];
   __shared__ int si[kWaves], sb[kWaves];
   RuleScratch sc;
-  carve_rules(a.scratch, (size_t)a.B * a.rows, &sc);
+  carve_rules(a.scratch, (size_t)a.B * a.rows, a.V, &sc);
   const Where w = where(a);
   const int kind = kind_of(a, w.b);
   float m = -INFINITY;
@@ -348,14 +357,14 @@ __global__ __launch_bounds__(kThreads) void rules_max_kernel(RulesArgs a) {
     bad |= !(l < INFINITY);  // (NaN or +inf)
     if (l > m) { m = l; at = j; }
   });
-  sc.top[((size_t)w.r * kMaxChunks + w.c) * kThreads + threadIdx.x] = m;
+  sc.top[((size_t)w.r * w.NC + w.c) * kThreads + threadIdx.x] = m;
   if (kind == ROW_K) {
     const int gl = group_lanes(w.NC, a.top_k[w.b]);
     float gm = m;
     for (int o = 1; o < gl; o <<= 1) gm = fmaxf(gm, __shfl_xor(gm, o, kWave));
-    if (threadIdx.x % gl == 0) sc.group[(size_t)w.r * kGroups + (w.c * kThreads + threadIdx.x) / gl] = ordered(gm);
+    if (threadIdx.x % gl == 0) sc.group[(size_t)w.r * groups_of(w.NC) + (w.c * kThreads + threadIdx.x) / gl] = ordered(gm);
   } else if (kind == ROW_P) {
-    for (int i = w.c * kThreads + threadIdx.x; i < buckets_of(bucket_rate(a.V)); i += w.NC * kThreads) sc.mass[(size_t)w.r * kBuckets + i] = 0ull;
+    for (int i = w.c * kThreads + threadIdx.x; i < buckets_of(bucket_rate(a.V)); i += w.NC * kThreads) sc.mass[(size_t)w.r * buckets_of(bucket_rate(a.V)) + i] = 0ull;
   }
   const float wm = wave_max(m);
   at = m == wm ? at : 0x7fffffff;
@@ -374,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void rules_max_kernel(RulesArgs a) {
       if (sm[k] > t.m || (sm[k] == t.m && si[k] < t.i)) { t.m = sm[k]; t.i = si[k]; }
       t.bad |= sb[k];
     }
-    sc.cmax[(size_t)w.r * kMaxChunks + w.c] = t;
+    sc.cmax[(size_t)w.r * w.NC + w.c] = t;
     if (w.c == 0) {
       sc.work[w.r].done = 0u;
       sc.work[w.r].listed = 0u;
@@ -677,14 +686,14 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
     uint32_t bound[kWaves];
   } s_row;
   RuleScratch sc;
-  carve_rules(a.scratch, (size_t)a.B * a.rows, &sc);
+  carve_rules(a.scratch, (size_t)a.B * a.rows, a.V, &sc);
   const Where w = where(a);
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const uint32_t* group = sc.group + (size_t)w.r * kGroups;
+  const uint32_t* group = sc.group + (size_t)w.r * groups_of(w.NC);
   const uint32_t first = group[lane * kWaves + wv];  // (of use where the row has a top-k)
   const Rules r = sc.work[w.r].rules;
   RowWork* work = sc.work + w.r;
-  const float top = sc.top[((size_t)w.r * kMaxChunks + w.c) * kThreads + threadIdx.x];
+  const float top = sc.top[((size_t)w.r * w.NC + w.c) * kThreads + threadIdx.x];
   if (r.kind == ROW_K) {
     // A lower bound of the k-th largest logit: each wave's of the (k / 4)-th largest of
     // every fourth group maximum, and the least of these (fewer groups than k: none).
@@ -702,7 +711,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
     if (lane == 0) s_row.bound[wv] = bound;
   }
   if (wv == 0) {
-    const ChunkMax mx = row_max(sc.cmax + (size_t)w.r * kMaxChunks, w.NC);
+    const ChunkMax mx = row_max(sc.cmax + (size_t)w.r * w.NC, w.NC);
     const int kind = mx.bad || mx.m == -INFINITY ? ROW_BAD : r.kind;
     if (lane == 0) {
       s_row.m = mx.m;
@@ -728,7 +737,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
       if (candidate(r, l, t)) sum += mass_at(t);
     });
     sum = block_total(sum, sel.sum);
-    unsigned long long* parts = sc.draw + (size_t)w.r * kSegments;
+    unsigned long long* parts = sc.draw + (size_t)w.r * segments_of(a.V);
     if (threadIdx.x == 0) put(&parts[w.c], sum);
     if (!last_here(&work->done, w.NC)) return;
     const unsigned long long all = wave_sum_u64(lane < w.NC ? get(&parts[lane]) : 0ull);
@@ -750,7 +759,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
       if (W) atomicAdd(&sh.mass[bucket_of(t, rate)], W);
     });
     __syncthreads();
-    unsigned long long* mass = sc.mass + (size_t)w.r * kBuckets;
+    unsigned long long* mass = sc.mass + (size_t)w.r * buckets_of(bucket_rate(a.V));
     for (int i = threadIdx.x; i < nb; i += kThreads)
       if (sh.mass[i]) __hip_atomic_fetch_add(&mass[i], sh.mass[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (!last_here(&work->done, w.NC)) return;
@@ -768,7 +777,7 @@ __global__ __launch_bounds__(kThreads, 4) void rules_scan_kernel(RulesArgs a) {
   uint32_t bound = s_row.bound[0];
 #pragma unroll
   for (int i = 1; i < kWaves; ++i) bound = min(bound, s_row.bound[i]);
-  unsigned long long* list = sc.list + (size_t)w.r * kList;
+  unsigned long long* list = sc.list + (size_t)w.r * list_of(a.V);
   // (nor are those whose probability is 0: a mask of the lowest value fills no list)
   const float low = (float)((double)m - 151.0 / r.c);
   if (ordered(top) >= bound && top >= low)  // (few of the threads have anything to read)
@@ -866,17 +875,17 @@ __global__ __launch_bounds__(kThreads) void rules_pick_kernel(RulesArgs a) {
   __shared__ Select sel;
   __shared__ Gather gather;
   RuleScratch sc;
-  carve_rules(a.scratch, (size_t)a.B * a.rows, &sc);
+  carve_rules(a.scratch, (size_t)a.B * a.rows, a.V, &sc);
   const Where w = where(a);
   RowWork* work = sc.work + w.r;
   if (work->kind != ROW_P) return;  // (workgroup-uniform, as all that follows from the row's words)
   const Rules r = work->rules;
   const float m = work->m;
   const Inside inside(r, m, work->bucket, bucket_rate(a.V));
-  unsigned long long* list = sc.list + (size_t)w.r * kList;
+  unsigned long long* list = sc.list + (size_t)w.r * list_of(a.V);
   if (threadIdx.x == 0) gather.n = 0u;
   __syncthreads();
-  if (sc.top[((size_t)w.r * kMaxChunks + w.c) * kThreads + threadIdx.x] >= inside.lo)
+  if (sc.top[((size_t)w.r * w.NC + w.c) * kThreads + threadIdx.x] >= inside.lo)
     each(w.row, w.j0, w.j1, [&](int j, float l) {
       double t;
       if (inside(r, m, l, t)) gather_add(gather, sh.key, key_of(l, j));
@@ -946,7 +955,7 @@ __global__ __launch_bounds__(kThreads) void rules_out_kernel(RulesArgs a) {
   __shared__ int s_segment;
   __shared__ unsigned long long s_t;
   RuleScratch sc;
-  carve_rules(a.scratch, (size_t)a.B * a.rows, &sc);
+  carve_rules(a.scratch, (size_t)a.B * a.rows, a.V, &sc);
   const Where w = where(a);
   RowWork* work = sc.work + w.r;
   float* probs = a.probs ? a.probs + (size_t)w.r * a.ld_probs : nullptr;
@@ -969,10 +978,10 @@ __global__ __launch_bounds__(kThreads) void rules_out_kernel(RulesArgs a) {
   const Kept prob(work->key, work->mass);
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int spc = (chunk_of(a.V, w.NC) + 255) / 256;  // segments of a chunk
-  unsigned long long* parts = sc.draw + (size_t)w.r * kSegments;
+  unsigned long long* parts = sc.draw + (size_t)w.r * segments_of(a.V);
   constexpr int Q = 2;
   // (a thread whose entries all lie below the border reads nothing)
-  const bool any = sc.top[((size_t)w.r * kMaxChunks + w.c) * kThreads + threadIdx.x] >= prob.edge;
+  const bool any = sc.top[((size_t)w.r * w.NC + w.c) * kThreads + threadIdx.x] >= prob.edge;
   for (int base = w.j0; base < w.j1; base += 4 * Q * kThreads) {
     float v[Q][4];
 #pragma unroll
@@ -1055,9 +1064,9 @@ int chunks_of(int rows, int V) { return std::max(1, std::min({kMaxChunks, (V + 1
 
 }  // namespace
 
-size_t rules_scratch_bytes(int n_rows) {
+size_t rules_scratch_bytes(int n_rows, int V) {
   RuleScratch s;
-  return carve_rules(nullptr, (size_t)n_rows, &s);
+  return carve_rules(nullptr, (size_t)n_rows, V, &s);
 }
 
 hipError_t launch_rules(const RulesArgs& a, hipStream_t s) {

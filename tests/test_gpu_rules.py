@@ -258,6 +258,30 @@ def test_graph_replays_and_a_shared_workspace():
             np.testing.assert_array_equal(bo.cpu().numpy(), tok)
 
 
+@pytest.mark.parametrize("B,R,V", [(1, 1, 50000), (700, 3, 1500), (5, 2, 20000)])
+def test_workspaces_need_no_contents(B, R, V):
+    """One workspace that holds anything, then the leavings of calls of other shapes."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(V)
+    names = (list(RULES) * B)[:B] if B > 1 else ["kpm"]
+    logits = rng.normal(0, 2, (B, R, V)).astype(np.float32)
+    words = synth.make_rand_u32((B, R), seed=V)
+    ws = torch.full((binding.sample_workspace(700, 3, 50000).numel(),), 255, dtype=torch.uint8, device="cuda")
+    log(f"workspace {B} x {R} x {V}")
+    p, tok, status = _run(logits, _device_rules(names), words, workspace=ws)
+    assert status == 0
+    for b in range(0, B, max(1, B // 40)):
+        for i in range(R):
+            _check_row(logits[b, i], RULES[names[b]], p[b, i], tok[b, i], words[b, i])
+    _run(rng.normal(0, 2, (9, 2, 40000)).astype(np.float32), _device_rules((["p", "k", "off"] * 3)), words=synth.make_rand_u32((9, 2), seed=1),
+         workspace=ws)
+    p2, tok2, _ = _run(logits, _device_rules(names), words, workspace=ws)
+    np.testing.assert_array_equal(p2, p)
+    np.testing.assert_array_equal(tok2, tok)
+    _, alone, _ = _run(logits, _device_rules(names), words, with_probs=False, workspace=ws)
+    np.testing.assert_array_equal(alone, tok)
+
+
 def test_refusals():
     torch = torch_cuda()
     lg = torch.zeros((2, 3, 100), device="cuda")
