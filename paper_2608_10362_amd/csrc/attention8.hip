@@ -590,6 +590,21 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
           const bool diagonal = k0 + kF8Sub - 1 > lowest;
           const int nvalid = vis - (k0 + 8 * grp);
           bool odd = false;
+          auto strip = [&](u32x4& v) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              if (2 * w >= nvalid) v[w] = 0u;
+              else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
+              const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
+              odd |= lo || up;
+              if (lo) v[w] &= 0xffff0000u;
+              if (up) v[w] &= 0xffffu;
+            }
+          };
+          if (QT > 1 && diagonal) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) strip(rv[QT == 1 ? 0 : dt]);
+          }
 #pragma unroll
           for (int q = 0; q < QT; ++q) {
             float p[8];
@@ -605,17 +620,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
 #pragma unroll
               for (int i = 0; i < DG; ++i) {
                 v[i] = QT == 1 ? rows[RK + d0 + i][lane] : rv[QT == 1 ? 0 : d0 + i];
-                if (diagonal) {
-#pragma unroll
-                  for (int w = 0; w < 4; ++w) {
-                    if (2 * w >= nvalid) v[i][w] = 0u;
-                    else if (2 * w + 1 >= nvalid) v[i][w] &= 0xffffu;
-                    const bool lo = (v[i][w] & 0x7f80u) == 0x7f80u, up = (v[i][w] & 0x7f800000u) == 0x7f800000u;
-                    odd |= lo || up;
-                    if (lo) v[i][w] &= 0xffff0000u;
-                    if (up) v[i][w] &= 0xffffu;
-                  }
-                }
+                if (QT == 1 && diagonal) strip(v[i]);
               }
 #pragma unroll
               for (int k = 2; k >= 0; --k)
