@@ -198,6 +198,7 @@ template <int HD>
 __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, int layer, int b, int pos0, int n,
                                                                 uint16_t* k, uint16_t* v) {
   __shared__ uint16_t sv[kF8Block][HD + 2];
+  __shared__ alignas(16) uint16_t sk[kF8Block][HD + 8];
   constexpr int F = HD / 16, FW = F / 4 > 0 ? F / 4 : 1;  // fragments per wave
   const int G = kv.ring.n_kv_heads, g = blockIdx.y;
   const int blk = pos0 / kF8Block + blockIdx.x, p0 = blk * kF8Block;
@@ -225,8 +226,7 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, in
       for (int e = 0; e < 2; ++e) {
         int pos, dim;
         k_place<HD>(f, c, i, e, pos, dim);
-        const u32x4 x = __builtin_bit_cast(u32x4, fp8x8_to_bf16(kc[j][2 * e], kc[j][2 * e + 1], ks));
-        if (in(pos)) *(u32x4_a2*)(k + at(pos) + dim) = x;
+        *(u32x4*)&sk[pos][dim] = __builtin_bit_cast(u32x4, fp8x8_to_bf16(kc[j][2 * e], kc[j][2 * e + 1], ks));
         const u32x4 y = __builtin_bit_cast(u32x4, fp8x8_to_bf16(vc[j][2 * e], vc[j][2 * e + 1], vs));
         v_place<HD>(f, c, i, e, pos, dim);
 #pragma unroll
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, in
     const int w0 = p0 % kv.ring.capacity;
     for (int t = threadIdx.x; t < kF8Block * HD / 8; t += kCopyThreads) {
       const int r = t / (HD / 8), d = t % (HD / 8) * 8;
-      if (in(r)) *(u32x4_a2*)(k + at(r) + d) = *(const u32x4*)(src + KvIndex<uint16_t>::k(w0 + r, d, HD, kv.ring.capacity));
+      *(u32x4*)&sk[r][d] = *(const u32x4*)(src + KvIndex<uint16_t>::k(w0 + r, d, HD, kv.ring.capacity));
       const int dim = t % HD, pos = t / HD * 8;
       const u32x4 y = *(const u32x4*)(src + KvIndex<uint16_t>::v(w0 + pos, dim, HD, kv.ring.capacity));
 #pragma unroll
@@ -255,6 +255,7 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, in
   for (int t = threadIdx.x; t < kF8Block * HD / 8; t += kCopyThreads) {
     const int r = t / (HD / 8), d = t % (HD / 8) * 8;
     if (!in(r)) continue;
+    *(u32x4_a2*)(k + at(r) + d) = *(const u32x4*)&sk[r][d];
     u32x4 x;
 #pragma unroll
     for (int q = 0; q < 4; ++q) x[q] = *(const uint32_t*)&sv[r][d + 2 * q];
