@@ -31,10 +31,10 @@
 // Measured.  7B-like (32 kv heads of 128): one row over 2048 keys 10.0 us (a chain of
 // start 3, codes and products 3, merge 1.5, parts 2.5), 16 ragged rows over 1024 to
 // 8191 keys 117 us, 5.2 TB/s of codes (reads alone reach 5.6 at this size); 512 rows
-// over 2048 keys 44 us, 343 TFLOP/s of the operator's products, twice that in the matrix
+// over 2048 keys 43 us, 351 TFLOP/s of the operator's products, twice that in the matrix
 // unit (half the time is conversions and softmax, which its products do not hide, a
 // quarter the ring's rows).  1.1B-like (4 kv heads of 64, 8 query heads each): one
-// row over 131072 keys 20.6 us, 3.3 TB/s (14 us of stream; 61 parts of one unit by one
+// row over 131072 keys 20.9 us, 3.2 TB/s (14 us of stream; 61 parts of one unit by one
 // workgroup 5 us), 4 x 5 rows over 301 to 1028 keys 10.0 us.
 #include <algorithm>
 

@@ -7,9 +7,10 @@
 // (their maximum, then the codes).  V changes from rows to operand order in LDS,
 // K's operand order is that of its rows' pieces; the write asks for K before it
 // waits for V (16.0 -> 15.0 us at 2048 positions of 32 heads of 128).
-// 32745 positions of that shape: write 190 us, read 185 us, 805 MB each, 4.3 TB/s
-// (a copy of that size: 5.2).  Nontemporal rows in: write 165 us, the read after it
-// 195; nontemporal rows out: read 296 us; so all accesses are plain ones.
+// 32745 positions of that shape: write 173 us, read 136 us, 805 MB each, 4.7 and
+// 5.9 TB/s (a copy of that size: 5.2).  Read back, K goes through LDS too: stored from
+// operand order, in pieces of 16 bytes, 643 MB were written for 537 (194 against
+// 160 us).  Nontemporal rows out: 100 us more; so all accesses are plain ones.
 #include <algorithm>
 
 #include "device_common.h"
@@ -193,15 +194,17 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_write_kernel(Kv8Layout kv, i
       kv.code_base(layer, b, g) + (size_t)at * 2 * kF8Block * HD, kv.scale_base(layer, b, g) + 2 * (size_t)at);
 }
 
-// Grid (blocks that [pos0, pos0 + n) touches, G): the block's values as rows.
+// Grid: G times the blocks that [pos0, pos0 + n) touches; the block's values as rows.  (Heads
+// first, so that whole positions are stored at about the same time: 160 -> 136 us for
+// 32745 positions of 32 heads, and 194 -> 171 us for the write of them before it.)
 template <int HD>
 __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, int layer, int b, int pos0, int n,
                                                                 uint16_t* k, uint16_t* v) {
   __shared__ uint16_t sv[kF8Block][HD + 2];
   __shared__ alignas(16) uint16_t sk[kF8Block][HD + 8];
   constexpr int F = HD / 16, FW = F / 4 > 0 ? F / 4 : 1;  // fragments per wave
-  const int G = kv.ring.n_kv_heads, g = blockIdx.y;
-  const int blk = pos0 / kF8Block + blockIdx.x, p0 = blk * kF8Block;
+  const int G = kv.ring.n_kv_heads, g = blockIdx.x % G;
+  const int blk = pos0 / kF8Block + blockIdx.x / G, p0 = blk * kF8Block;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 4, i = lane & 15;
   auto at = [&](int pos) { return ((size_t)(p0 + pos - pos0) * G + g) * HD; };
   auto in = [&](int pos) { return p0 + pos >= pos0 && p0 + pos < pos0 + n; };
@@ -363,7 +366,7 @@ hipError_t launch_kv8_write(const Kv8Layout& kv, int layer, int b, int pos0, int
 
 hipError_t launch_kv8_read(const Kv8Layout& kv, int layer, int b, int pos0, int n, void* k, void* v, hipStream_t s) {
   if (n <= 0) return hipSuccess;
-  const dim3 grid((pos0 + n - 1) / kF8Block - pos0 / kF8Block + 1, kv.ring.n_kv_heads);
+  const dim3 grid(((pos0 + n - 1) / kF8Block - pos0 / kF8Block + 1) * kv.ring.n_kv_heads);
 #define SD_R(HD)                                                                                                   \
   hipLaunchKernelGGL((kv8_read_kernel<HD>), grid, dim3(kCopyThreads), 0, s, kv, layer, b, pos0, n, (uint16_t*)k, \
                      (uint16_t*)v)
