@@ -21,20 +21,22 @@
 //    into the conversion where the values are fp16's and into the sums where not.
 //    56 -> 49 us against three bf16 parts, which the ring's rows, bf16 values, still take.
 //
-// Work: a line of chunks of 32 or 64 keys, sequence by sequence, unit by unit (kv
-// head, query tile); workgroup i takes the i-th `per` of them, so all stream the
-// same bytes whatever the lengths, and its NW waves take every NW-th.  Within a
-// unit's segment each wave keeps (max, sum, O), then they merge in LDS.  A unit
-// inside one workgroup is finished there; otherwise each stores its part and
-// the last to count itself adds the parts.
+// Work: a unit is a kv head and a query tile of a sequence; its keys come in chunks of
+// 32 or 64, and a workgroup takes a range of them, its NW waves every NW-th.  Each
+// wave keeps (max, sum, O) of its own, then they merge in LDS.  A unit inside one
+// workgroup is finished there; otherwise each stores its part and the last to count
+// itself adds the parts.  Ragged batches with more than four chunks a wave put all
+// units' chunks on a line, and workgroup i takes the i-th `per` of them: all stream
+// the same bytes whatever the lengths.  Other calls have a workgroup per range.
 //
 // Measured.  7B-like (32 kv heads of 128): one row over 2048 keys 10.0 us (a chain of
-// start 3, codes and products 3, merge 1.5, parts 2.5), 16 ragged rows over 1024 to
-// 8191 keys 117 us, 5.2 TB/s of codes (reads alone reach 5.6 at this size); 512 rows
-// over 2048 keys 43 us, 351 TFLOP/s of the operator's products, twice that in the matrix
-// unit (half the time is conversions and softmax, which its products do not hide, a
-// quarter the ring's rows).  1.1B-like (4 kv heads of 64, 8 query heads each): one
-// row over 131072 keys 20.9 us, 3.2 TB/s (14 us of stream; 61 parts of one unit by one
+// start 3, codes and products 3, merge 1.5, parts 2.5); 16 ragged rows over 1024 to
+// 8191 keys 114 us, 5.3 TB/s of codes (99 us, 6.1 TB/s, where all are 4607 long and
+// no unit is cut; reads alone reach 5.6 to 6.5); 512 rows over 2048 keys 43 us,
+// 351 TFLOP/s of the operator's products, twice that in the matrix unit (half the
+// time is conversions and softmax, which its products do not hide, a quarter the
+// ring's rows).  1.1B-like (4 kv heads of 64, 8 query heads each): one row over
+// 131072 keys 20.9 us, 3.2 TB/s (14 us of stream; 61 parts of one unit by one
 // workgroup 5 us), 4 x 5 rows over 301 to 1028 keys 10.0 us.
 #include <algorithm>
 
@@ -790,7 +792,8 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
     int n64 = some(0), at64 = 0, total = lane_sum(n64);
     for (int c = kWave; c < B; c += kWave) total += lane_sum(some(c));
     total *= U;
-    const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, per0);
+    // (four chunks a wave at least: a cut moves by less than half of that)
+    const int per = max(max((total + (int)gridDim.x - 1) / (int)gridDim.x, per0), 4 * NW);
     auto subs = [&](int s) {
       if ((s & ~(kWave - 1)) != at64) {
         at64 = s & ~(kWave - 1);
@@ -798,19 +801,47 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       }
       return __builtin_amdgcn_readlane(n64, s & (kWave - 1));
     };
-    int x = (int)blockIdx.x * per;
-    const int hi = min(total, x + per);
-    int b = 0, base = 0, nb = subs(0);  // the sequence that holds x; base: the line where it starts
-    while (x < hi) {
-      while (x >= base + nb * U) {
-        base += nb * U;
-        ++b;
-        nb = subs(b);
+    // Where a unit of n chunks is cut that a border meets d chunks in: after whole rounds
+    // of all waves, and not at all where a round or less would be cut off (16 ragged rows
+    // over 1024 to 8191 keys 114.5 us, 118 us with cuts where they fall).
+    auto snap = [](int d, int n) {
+      const int r = (d + NW / 2) / NW * NW;
+      return r <= NW ? 0 : n - r <= NW ? n : r;
+    };
+    struct At {
+      int b, base, nb;  // a sequence, the line where it starts, the chunks of its units
+    };
+    auto walk = [&](At& at, int x) {  // to the sequence that holds x
+      while (x >= at.base + at.nb * U) {
+        at.base += at.nb * U;
+        ++at.b;
+        at.nb = subs(at.b);
       }
-      const int u = (x - base) / nb, unit0 = base + u * nb;  // unit0: the line where the unit starts
-      const int k_lo = x - unit0, k_hi = min(nb, k_lo + (hi - x)), first = unit0 / per, g = u / n_tiles;
-      x += k_hi - k_lo;
-      segment(b, g, u - g * n_tiles, k_lo, k_hi, (int)blockIdx.x - first, (unit0 + nb - 1) / per - first + 1);
+      return at.base + (x - at.base) / at.nb * at.nb;  // the line where x's unit starts
+    };
+    int x = (int)blockIdx.x * per, hi = x + per;
+    if (x >= total) return;
+    At at{0, 0, subs(0)};
+    int unit0 = walk(at, x);
+    x = unit0 + snap(x - unit0, at.nb);
+    if (hi < total) {
+      At end = at;
+      unit0 = walk(end, hi);
+      hi = unit0 + snap(hi - unit0, end.nb);
+    } else {
+      hi = total;
+    }
+    while (x < hi) {
+      unit0 = walk(at, x);
+      const int nb = at.nb, u = (unit0 - at.base) / nb, g = u / n_tiles, k_lo = x - unit0, k_hi = min(nb, hi - unit0);
+      // the first and the last workgroup with a part of the unit: the borders before its
+      // start and its end, but for one that was moved across
+      int first = unit0 / per, last = (unit0 + nb - 1) / per;
+      const int y0 = (first + 1) * per - unit0, y1 = last * per - unit0;
+      if (y0 < nb && snap(y0, nb) == 0) ++first;
+      if (y1 >= 0 && snap(y1, nb) == nb) --last;
+      x = unit0 + k_hi;
+      segment(at.b, g, u - g * n_tiles, k_lo, k_hi, (int)blockIdx.x - first, last - first + 1);
       __syncthreads();  // (LDS is free for the next segment)
     }
   }
