@@ -25,8 +25,8 @@
 // 32 or 64, and a workgroup takes a range of them, its NW waves every NW-th.  Each
 // wave keeps (max, sum, O) of its own, then they merge in LDS.  A unit inside one
 // workgroup is finished there; otherwise each stores its part and the last to count
-// itself adds the parts.  Ragged batches with more than four chunks a wave put all
-// units' chunks on a line, and workgroup i takes the i-th `per` of them: all stream
+// itself adds the parts.  Ragged batches of few rows, with more than four chunks a wave,
+// put all units' chunks on a line, and workgroup i takes the i-th `per` of them: all stream
 // the same bytes whatever the lengths.  Other calls have a workgroup per range.
 //
 // Measured.  7B-like (32 kv heads of 128): one row over 2048 keys 10.0 us (a chain of
@@ -857,13 +857,22 @@ Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int 
   p.n_tiles = (nq + 16 * p.qt - 1) / (16 * p.qt);
   const long nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim), units = (long)n_kv_heads * p.n_tiles;
   const long slots = 2L * device_compute_units();  // workgroups resident at once
-  // (at least a chunk a wave: fewer parts to add.  Half a chunk was 12.9 us, one 10.4 us,
-  // two 11.4 us for a row over 2048 keys of 32 heads)
-  const long per = std::max({(nb * units * batch + slots - 1) / slots, (nb + kPartsMax8 - 3) / (kPartsMax8 - 2),
-                             (long)waves_of(p.qt)});
-  // Several sequences of unlike lengths and more than four chunks a wave: the line.
-  p.line = batch > 1 && per > 4 * waves_of(p.qt);
-  p.per = (int)(p.line ? (nb + kPartsMax8 - 3) / (kPartsMax8 - 2) : per);
+  // Several sequences of unlike lengths, one query tile, more than four chunks a wave:
+  // the line.  (Two tiles cost a cut more than it gives: 4 x 70 rows over 500 to 6000 keys
+  // 106 us on the line, 93 us not; over 100, 60000, 100 and 50 keys 437 and 97 us.)
+  const long least = (nb + kPartsMax8 - 3) / (kPartsMax8 - 2);
+  p.line = p.qt == 1 && batch > 1 && (nb * units * batch + slots - 1) / slots > 4 * waves_of(p.qt);
+  // Otherwise as many parts of a unit as let all workgroups be resident (200 rows over
+  // 1736 keys, 224 units: 2 parts 36 us, 3, of equal chunks and a rest, 45 us); more where
+  // one sequence of a batch may be far longer than the others, 128 chunks to a part, but
+  // no more than it would have alone (one of 60000 keys in four: 97 us, without 299 us;
+  // 64 chunks to a part make 4 x 70 rows over 4000 keys 101 us, not 80); and at least a
+  // chunk a wave: fewer parts to add.  (Half a chunk was 12.9 us, one 10.4 us, two 11.4 us
+  // for a row over 2048 keys of 32 heads.)
+  const long all = std::max(1L, slots / (units * batch)), alone = std::max(1L, slots / units);
+  const long share = std::min((nb + all - 1) / all, batch > 1 ? 128L : nb);
+  const long per = std::max({share, (nb + alone - 1) / alone, least, (long)waves_of(p.qt)});
+  p.per = (int)(p.line ? least : per);
   p.nwg = (int)(p.line ? slots : (nb + per - 1) / per);
   // Parts of a unit, at most: a workgroup takes at least nb * units / slots of the
   // longest sequence's line, whatever the other lengths.  (Grows with max_ctx:
@@ -891,8 +900,7 @@ hipError_t launch_attention8(const AttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((attn8_kernel<HDV, QT, LINE, ONCE>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per)
 #define SD_A8_HD(HDV)                                  \
   if (p.qt == 2) {                                     \
-    if (p.line) SD_A8(HDV, 2, true, false);            \
-    else SD_A8(HDV, 2, false, false);                  \
+    SD_A8(HDV, 2, false, false);                       \
   } else if (p.n_tiles == 1) {                         \
     if (p.line) SD_A8(HDV, 1, true, true);             \
     else SD_A8(HDV, 1, false, true);                   \

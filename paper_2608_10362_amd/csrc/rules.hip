@@ -55,7 +55,7 @@ namespace specdec {
 
 namespace {
 
-constexpr int kThreads = 256;                   // 
+constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBuckets = 2304;                  // of distances below 44 powers of two (no mass past them)
 constexpr int kList = 4096;                     // border candidates kept in LDS

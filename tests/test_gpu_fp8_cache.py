@@ -238,8 +238,8 @@ def test_attention(case):
     assert kv.read_state()["status"] == 0
 
 
-# Ragged batches whose keys make more than four chunks a wave: workgroups take
-# their share of all of them, not of one sequence's.
+# Ragged batches whose keys make more than four chunks a wave: where the rows are few,
+# workgroups take their share of all of them, not of one sequence's.
 LINES = [  # hd, H, G, lens, n, window
     (32, 8, 8, [61000, 1, 30011], 1, 128),
     (64, 8, 4, [0, 131000, 60000, 129], 2, 128),
