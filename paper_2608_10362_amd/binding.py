@@ -10,6 +10,7 @@ fails loudly otherwise -- there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional
@@ -220,6 +221,14 @@ def _stream(stream) -> Optional[int]:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _memory_of(stream):
+    """Context in which a call launched on `stream` allocates: what is allocated for the
+    current stream goes, once dropped, to that stream's next allocation, which
+    does not wait for `stream`."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def make_desc(shape) -> ModelDesc:
     return ModelDesc(shape.n_layers, shape.d_model, shape.n_heads, shape.n_kv_heads, shape.head_dim, shape.ffn_dim,
                      shape.vocab, shape.rms_eps, shape.rope_base,
@@ -369,10 +378,16 @@ class KVCache:
                                               v.data_ptr(), _stream(stream)), "specdec_kv_write_context")
 
     def read_context(self, layer: int, b: int, pos0: int, n: int, stream=None):
+        """The rows as new tensors, valid once `stream` has run the copy; they may be
+        dropped while the stream that was current at the call still reads them."""
         import torch
         shp = (n, self.kv.n_kv_heads, self.kv.head_dim)
-        k = torch.empty(shp, dtype=self.storage_dtype(), device=self.data.device)
-        v = torch.empty_like(k)
+        with _memory_of(stream):
+            k = torch.empty(shp, dtype=self.storage_dtype(), device=self.data.device)
+            v = torch.empty_like(k)
+        if stream is not None:
+            for t in (k, v):
+                t.record_stream(torch.cuda.current_stream())
         _check(lib().specdec_kv_read_context(ctypes.byref(self.kv), layer, b, pos0, n, k.data_ptr(), v.data_ptr(),
                                              _stream(stream)), "specdec_kv_read_context")
         return k, v
@@ -545,7 +560,8 @@ def attention_workspace(kv: KVCache, n_heads: int, n: int):
 
 def specdec_attention(kv: KVCache, layer: int, q, out, workspace=None, stream=None):
     """q, out: device float32 [batch, n, n_heads, head_dim] (out may be q).
-    `workspace` (from attention_workspace) is allocated per call when not given.
+    `workspace` (from attention_workspace) is allocated per call, on the call's stream, when
+    not given.
     Calls on one cache must be ordered on one stream."""
     import torch
     if q.dim() != 4 or q.shape[0] != kv.batch or q.shape[3] != kv.kv.head_dim or out.shape != q.shape:
@@ -557,7 +573,8 @@ def specdec_attention(kv: KVCache, layer: int, q, out, workspace=None, stream=No
     _same_device(kv.data, "kv", q)
     n, n_heads = q.shape[1], q.shape[2]
     if workspace is None:
-        workspace = attention_workspace(kv, n_heads, n)
+        with _memory_of(stream):
+            workspace = attention_workspace(kv, n_heads, n)
     _dev(workspace, "workspace", torch.uint8, 1)
     _same_device(workspace, "workspace", q)
     _check(lib().specdec_attention(ctypes.byref(kv.kv), layer, n_heads, n, q.data_ptr(), out.data_ptr(),
@@ -608,7 +625,7 @@ def specdec_accept(batch: int, gamma: int, vocab: int, input_kind: int, temperat
                    rand, seed: int, step: int, n_accepted, next_token, status=None, workspace=None, stream=None,
                    step_dev=None):
     """Accept / resample.  `workspace` (uint8 device tensor) is allocated per
-    call when not given; pass one from accept_workspace() in loops.  step_dev:
+    call, on the call's stream, when not given; pass one from accept_workspace() in loops.  step_dev:
     as for specdec_draft_step."""
     import torch
     _dev(p, "p", torch.float32, batch * (gamma + 1) * vocab)
@@ -622,7 +639,8 @@ def specdec_accept(batch: int, gamma: int, vocab: int, input_kind: int, temperat
     _dev(next_token, "next_token", torch.int32, batch)
     _dev(status, "status", torch.int32, 1, optional=True)
     if workspace is None:
-        workspace = accept_workspace(batch, gamma, vocab, p.device)
+        with _memory_of(stream):
+            workspace = accept_workspace(batch, gamma, vocab, p.device)
     _dev(workspace, "workspace", torch.uint8, 1)
     _check(lib().specdec_accept(batch, gamma, vocab, input_kind, temperature, p.data_ptr(), _ptr(q), _ptr(d), ld_d,
                                 _ptr(rand), seed, step, step_dev, n_accepted.data_ptr(), next_token.data_ptr(),
@@ -707,7 +725,7 @@ def specdec_sample_logits(logits, rules: Optional[SamplingRules] = None, rand=No
     """logits [batch, rows, vocab] or [batch, vocab] float32; probs: the same
     shape; out: int32 [batch, rows].  probs and out may be strided over their
     leading dimensions (a slot of a larger buffer) if one stride covers them.
-    `workspace` is allocated per call when not given."""
+    `workspace` is allocated per call, on the call's stream, when not given."""
     import torch
     _on_current(logits, "logits", torch.float32)
     if logits.dim() not in (2, 3):
@@ -740,7 +758,8 @@ def specdec_sample_logits(logits, rules: Optional[SamplingRules] = None, rand=No
         _dev(status, "status", torch.int32, 1)
         _same_device(status, "status", logits)
     if workspace is None:
-        workspace = sample_workspace(batch, rows, vocab, logits.device)
+        with _memory_of(stream):
+            workspace = sample_workspace(batch, rows, vocab, logits.device)
     _dev(workspace, "workspace", torch.uint8, 1)
     _same_device(workspace, "workspace", logits)
     _check(lib().specdec_sample_logits(batch, rows, vocab, logits.data_ptr(), ld,
