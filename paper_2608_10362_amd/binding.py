@@ -229,6 +229,14 @@ def _memory_of(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _after_current(stream):
+    """`stream` waits for the current stream, on which a constructor has just allocated
+    (and zeroed) what it now sets up on `stream`."""
+    import torch
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+
+
 def make_desc(shape) -> ModelDesc:
     return ModelDesc(shape.n_layers, shape.d_model, shape.n_heads, shape.n_kv_heads, shape.head_dim, shape.ffn_dim,
                      shape.vocab, shape.rms_eps, shape.rope_base,
@@ -288,6 +296,7 @@ class DeviceWeights:
                 raise SpecdecError(-2, "specdec_packed_bytes_fmt")
             self.packed = torch.empty(nbytes, dtype=torch.uint8, device=self.t["embed"].device)
             w, keep = self.c_struct(self.n_layers)
+            _after_current(stream)
             _check(lib().specdec_pack_weights_fmt(ctypes.byref(desc), ctypes.byref(w), self.n_layers, fmt,
                                                   self.packed.data_ptr(), nbytes, _stream(stream)),
                    "specdec_pack_weights_fmt")
@@ -358,6 +367,7 @@ class KVCache:
         self.data = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         self.state = torch.zeros(lib().specdec_kv_state_count(batch), dtype=torch.int32, device=dev)
         self.kv = KV()
+        _after_current(stream)
         _check(lib().specdec_kv_init(ctypes.byref(self.kv), model.handle, batch, capacity, self.data.data_ptr(),
                                      nbytes, self.state.data_ptr(), _stream(stream)), "specdec_kv_init")
 
@@ -446,6 +456,7 @@ class Fp8KVCache(KVCache):
         _on_current(self.data, "device", torch.uint8)
         self.state = torch.zeros(lib().specdec_kv_state_count(batch), dtype=torch.int32, device=device)
         self.kv = KV()
+        _after_current(stream)
         _check(lib().specdec_kv_init_fp8(ctypes.byref(self.kv), ctypes.byref(desc), n_layers, batch, capacity, window,
                                          self.data.data_ptr(), nbytes, self.state.data_ptr(), _stream(stream)),
                "specdec_kv_init_fp8")

@@ -14,7 +14,10 @@ CURRENT, SIDE = 1, 2  # stream handles
 
 class Stream:
     def __init__(self, handle):
-        self.cuda_stream = handle
+        self.cuda_stream, self.waited = handle, []
+
+    def wait_stream(self, other):
+        self.waited.append(other.cuda_stream)
 
 
 class Memory:
@@ -101,3 +104,35 @@ def test_a_calls_own_memory_belongs_to_its_stream(stand_in, call, stream, handle
     assert Memory.made and all(m.of == handle for m in Memory.made)
     if call == "read_context":  # (what goes back to the caller is kept for the caller's stream too)
         assert all(m.recorded >= {CURRENT} or m.of == CURRENT for m in Memory.made)
+
+
+class Waits(Library):
+    """Keeps what the launch stream had waited for at each launch."""
+    def __init__(self, stream):
+        super().__init__()
+        self.stream, self.before = stream, []
+
+    def __getattr__(self, name):
+        call = super().__getattr__(name)
+
+        def noted(*args):
+            if not name.endswith("_bytes"):
+                self.before.append((name, list(self.stream.waited)))
+            return call(*args)
+        return noted
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["KVCache", "Fp8KVCache"])
+def test_a_caches_set_up_waits_for_what_made_its_memory(stand_in, monkeypatch, fp8):
+    """The buffers are the current stream's (which may still have work in memory it hands
+    out again, and zeroes the state): a set-up on another stream comes after that."""
+    side = Stream(SIDE)
+    lib = Waits(side)
+    monkeypatch.setattr(binding, "lib", lambda: lib)
+    model = binding.Model.__new__(binding.Model)
+    model.workspace, model.n_layers, model.handle, model.max_rows = torch.ones(1), 1, 0, 16
+    model.desc = binding.ModelDesc()
+    (binding.Fp8KVCache if fp8 else binding.KVCache)(model, 1, 64, stream=side)
+    init = [w for name, w in lib.before if name.startswith("specdec_kv_init")]
+    assert init == [[CURRENT]]
+    assert all(m.of == CURRENT for m in Memory.made)
