@@ -557,6 +557,8 @@ def specdec_kv_append(kv: KVCache, layer: int, k, v, stream=None):
 
 
 def specdec_kv_advance(kv: KVCache, n: int, stream=None):
+    import torch
+    _on_current(kv.data, "kv", torch.uint8)
     _check(lib().specdec_kv_advance(ctypes.byref(kv.kv), n, _stream(stream)), "specdec_kv_advance")
 
 
