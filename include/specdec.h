@@ -290,8 +290,9 @@ SPECDEC_API specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* s
  * row i of sequence b at position len[b] + i, seeing keys 0 .. len[b]+i (the
  * last ones appended, not committed); query head h reads kv head
  * h / (n_heads / n_kv_heads).  out, same shape, float32:
- * softmax(q k^T / sqrt(head_dim)) v, the sums in float32; out may be q.  A key or
- * value row with a NaN or infinity affects the rows that see it and no others.
+ * softmax(q k^T / sqrt(head_dim)) v, the sums in float32; out may be q, but may
+ * not overlap it otherwise.  A key or value row with a NaN or infinity affects
+ * the rows that see it and no others.
  * workspace: specdec_attention_workspace_bytes bytes (0 for arguments the call
  * rejects), 256-byte aligned, dead after the call; calls that share one must be
  * ordered on one stream (graphs captured with one, replayed in order).  So must

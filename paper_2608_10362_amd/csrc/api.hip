@@ -778,6 +778,10 @@ specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_
   if (!q || !out || layer < 0 || layer >= kv->n_layers || !workspace || (uintptr_t)workspace % kAlign ||
       workspace_bytes < specdec_attention_workspace_bytes(kv, n_heads, n))
     return SPECDEC_ERR_INVALID_ARG;
+  // (a unit's rows are stored when all of its parts have read theirs, and no other's)
+  const size_t bytes = (size_t)kv->batch * n * n_heads * kv->head_dim * 4;
+  if (out != q && (uintptr_t)out < (uintptr_t)q + bytes && (uintptr_t)q < (uintptr_t)out + bytes)
+    return SPECDEC_ERR_INVALID_ARG;
   if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
   AttnArgs a{};
   a.M = kv->batch * n;

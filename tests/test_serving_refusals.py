@@ -30,3 +30,20 @@ def test_an_advance_takes_a_cache_on_the_current_device(monkeypatch):
     with pytest.raises(ValueError):
         binding.specdec_kv_advance(_Cache("cpu"), 1)
     assert not called
+
+
+FAKE = 1 << 20  # never dereferenced: the calls fail first
+
+
+def _attention(lib, q, out, batch=2, n_kv_heads=4, head_dim=64, n_heads=8, n=2, window=128, capacity=256):
+    kv = binding.KV()
+    kv.data, kv.state, kv.batch, kv.capacity, kv.n_layers, kv.len_upper = FAKE, FAKE, batch, capacity, 3, 100
+    kv.n_kv_heads, kv.head_dim, kv.dtype, kv.window = n_kv_heads, head_dim, binding.SPECDEC_FP8, window
+    return lib.specdec_attention(ctypes.byref(kv), 0, n_heads, n, q, out, FAKE, 1 << 60, None)
+
+
+def test_attention_refuses_an_out_that_is_part_of_q(lib):
+    nbytes = 2 * 2 * 8 * 64 * 4
+    for off in (4, 256, nbytes - 4):
+        assert _attention(lib, FAKE, FAKE + off) == -1
+        assert _attention(lib, FAKE + off, FAKE) == -1
