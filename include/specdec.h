@@ -239,7 +239,9 @@ SPECDEC_API specdec_status specdec_kv_init(specdec_kv* kv, const specdec_model* 
  *    prefill runs in chunks of at most window - 64 tokens per sequence.
  *  capacity: a multiple of 64.  data: 256-byte aligned device memory, at least
  *    specdec_kv_bytes_fp8 bytes (the call zeroes a region of counters in it, the
- *    rest needs no contents).  At most 128 query heads per kv head.
+ *    rest needs no contents).  At most 128 query heads per kv head and 65535
+ *    sequences; a pass needs kv heads times query tiles of a sequence (16 query
+ *    rows of a kv head up to 64 of them, 32 above) up to 65535 (SHAPE).
  *  specdec_kv_set_state may set any length whose last len % 64 positions are
  *    still in the ring: the last `window` positions written (by
  *    specdec_kv_write_context, an append or a pass), less what was written
@@ -301,7 +303,8 @@ SPECDEC_API specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* s
  * Graph capture: sized from kv->len_upper, as the passes are (see above).
  * Asynchronous.  Errors: INVALID_ARG, UNSUPPORTED (other caches), SHAPE
  * (n_heads not a multiple of n_kv_heads or above 128 times it, n > window -
- * 63), KV_CAPACITY. */
+ * 63, more kv heads times query tiles than specdec_kv_init_fp8 names),
+ * KV_CAPACITY. */
 SPECDEC_API size_t specdec_attention_workspace_bytes(const specdec_kv* kv, int32_t n_heads, int32_t n);
 SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_heads, int32_t n,
                                              const float* q, float* out, void* workspace, size_t workspace_bytes,

@@ -268,7 +268,7 @@ specdec_status check_fp8(const specdec_model_desc* d, int n_layers, int batch, i
     return SPECDEC_ERR_INVALID_ARG;
   if (d->dtype != SPECDEC_BF16) return SPECDEC_ERR_UNSUPPORTED;
   if (capacity % kF8Block || window % kF8Block || window < 2 * kF8Block) return SPECDEC_ERR_SHAPE;
-  if (d->n_heads / d->n_kv_heads > kF8MaxGroup) return SPECDEC_ERR_SHAPE;
+  if (d->n_heads / d->n_kv_heads > kF8MaxGroup || batch > kF8MaxBatch) return SPECDEC_ERR_SHAPE;
   // (a unit's codes are addressed by 32 bits)
   if (((size_t)capacity + 1024) * 2 * d->head_dim >= (size_t)1 << 32) return SPECDEC_ERR_UNSUPPORTED;
   return SPECDEC_OK;
@@ -277,7 +277,8 @@ specdec_status check_fp8(const specdec_model_desc* d, int n_layers, int batch, i
 specdec_status check_attention(const specdec_kv* kv, int n_heads, int n) {
   if (!kv || !kv->data || !kv->state || n_heads <= 0 || n <= 0) return SPECDEC_ERR_INVALID_ARG;
   if (!is_fp8(kv)) return SPECDEC_ERR_UNSUPPORTED;
-  if (n_heads % kv->n_kv_heads || n_heads / kv->n_kv_heads > kF8MaxGroup || !ring_holds(kv, n) || n > kv->capacity)
+  if (n_heads % kv->n_kv_heads || n_heads / kv->n_kv_heads > kF8MaxGroup || !ring_holds(kv, n) || n > kv->capacity ||
+      !attention8_fits(n, kv->batch, n_heads, kv->n_kv_heads))
     return SPECDEC_ERR_SHAPE;
   return SPECDEC_OK;
 }
@@ -317,7 +318,7 @@ specdec_status forward(const specdec_model* m, specdec_kv* kv, RowsArgs ra, int 
   const specdec_model_desc& d = m->desc;
   const int M = ra.M, dt = d.dtype;
   const int H = d.n_heads, G = d.n_kv_heads, hd = d.head_dim;
-  if (M > m->max_rows) return SPECDEC_ERR_SHAPE;
+  if (M > m->max_rows || (is_fp8(kv) && !attention8_fits(ra.rps, M / ra.rps, H, G))) return SPECDEC_ERR_SHAPE;
   ctx_bound = std::min(ctx_bound, kv->capacity);
   const int n_split = (ctx_bound + m->chunk - 1) / m->chunk;
   if (n_split > m->n_split_max) return SPECDEC_ERR_SHAPE;

@@ -850,18 +850,22 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
 struct Plan {
   int qt, n_tiles, line, nwg, per, parts;
 };
+int tiles_a_wave(int nq) { return nq <= 64 ? 1 : 2; }
+int tiles_of(int nq) { return (nq + 16 * tiles_a_wave(nq) - 1) / (16 * tiles_a_wave(nq)); }
 Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
   Plan p;
   const int nq = rps * (n_heads / n_kv_heads);
-  p.qt = nq <= 64 ? 1 : 2;
-  p.n_tiles = (nq + 16 * p.qt - 1) / (16 * p.qt);
+  p.qt = tiles_a_wave(nq);
+  p.n_tiles = tiles_of(nq);
   const long nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim), units = (long)n_kv_heads * p.n_tiles;
   const long slots = 2L * device_compute_units();  // workgroups resident at once
   // Several sequences of unlike lengths, one query tile, more than four chunks a wave:
   // the line.  (Two tiles cost a cut more than it gives: 4 x 70 rows over 500 to 6000 keys
   // 106 us on the line, 93 us not; over 100, 60000, 100 and 50 keys 437 and 97 us.)
   const long least = (nb + kPartsMax8 - 3) / (kPartsMax8 - 2);
-  p.line = p.qt == 1 && batch > 1 && (nb * units * batch + slots - 1) / slots > 4 * waves_of(p.qt);
+  // (The line is counted in 32 bits.)
+  const long most = nb * units * batch;
+  p.line = p.qt == 1 && batch > 1 && (most + slots - 1) / slots > 4 * waves_of(p.qt) && most <= 1L << 30;
   // Otherwise as many parts of a unit as let all workgroups be resident (200 rows over
   // 1736 keys, 224 units: 2 parts 36 us, 3, of equal chunks and a rest, 45 us); more where
   // one sequence of a batch may be far longer than the others, 128 chunks to a part, but
@@ -883,6 +887,10 @@ Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int 
 
 }  // namespace
 
+bool attention8_fits(int rps, int batch, int n_heads, int n_kv_heads) {
+  return batch <= kF8MaxBatch && (long)n_kv_heads * tiles_of(rps * (n_heads / n_kv_heads)) <= kF8MaxUnits;
+}
+
 int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
   return plan_of(rps, batch, n_heads, n_kv_heads, head_dim, max_ctx).parts;
 }
@@ -890,11 +898,11 @@ int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int head_d
 hipError_t launch_attention8(const AttnArgs& a, hipStream_t s) {
   const int B = a.M / a.rps;
   const Plan p = plan_of(a.rps, B, a.n_heads, a.n_kv_heads, a.head_dim, a.max_ctx);
-  const long units = (long)a.n_kv_heads * p.n_tiles;
-  if (p.parts > a.n_split || p.n_tiles > kF8TilesPerSlot * a.f8.ring.capacity || units > 65535 || B > 65535 ||
-      (a.max_ctx + kF8Sub - 1L) / kF8Sub * units * B > 1L << 30)
-    return hipErrorInvalidValue;
-  const dim3 grid = p.line ? dim3(p.nwg) : dim3(p.nwg, (unsigned)units, B), block(64 * waves_of(p.qt));
+  if (p.parts > a.n_split || p.n_tiles > kF8TilesPerSlot * a.f8.ring.capacity ||
+      !attention8_fits(a.rps, B, a.n_heads, a.n_kv_heads))
+    return hipErrorInvalidValue;  // (the callers have checked)
+  const dim3 grid = p.line ? dim3(p.nwg) : dim3(p.nwg, (unsigned)(a.n_kv_heads * p.n_tiles), B);
+  const dim3 block(64 * waves_of(p.qt));
   // (codes that one unit alone reads need not stay in a cache)
 #define SD_A8(HDV, QT, LINE, ONCE) \
   hipLaunchKernelGGL((attn8_kernel<HDV, QT, LINE, ONCE>), grid, block, 0, s, a, p.n_tiles, p.parts, p.per)

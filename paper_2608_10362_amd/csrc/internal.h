@@ -79,6 +79,8 @@ constexpr int kF8MinExp = -100;
 constexpr int kF8Sub = 32;            // positions an attention wave takes at a time
 constexpr int kF8TilesPerSlot = 4;    // query tiles of a (sequence, kv head), per ring position
 constexpr int kF8MaxGroup = 128;      // query heads per kv head (32 queries a tile: 4 tiles a row at most)
+constexpr int kF8MaxBatch = 65535;    // sequences of a cache (a grid dimension of its launches)
+constexpr int kF8MaxUnits = 65535;    // kv heads times query tiles of a sequence (the same)
 constexpr int kF8MaxDraft = 64;       // drafted tokens of a draft step's iteration (its one-row passes see them in the ring)
 struct Kv8Layout {
   unsigned char* codes;
@@ -284,6 +286,8 @@ hipError_t launch_rope_append(const AttnArgs& a, hipStream_t s);
 // FP8 caches (attention8.hip): parts of one (row, head) the launch may write
 // (o_part holds M * n_heads * parts * head_dim floats, ml_part 2 per part).
 int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx);
+// Whether a launch of rps rows a sequence has a grid (checked before a call launches anything).
+bool attention8_fits(int rps, int batch, int n_heads, int n_kv_heads);
 hipError_t launch_attention8(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
 
