@@ -518,7 +518,8 @@ typedef struct {
  *    max(1, ceil(top_p * mass of the top_k)).
  * probs (optional, row (b, i) at probs + (b*rows + i)*ld_probs):
  *   fl32(e_j 2^43 / mass of the kept) for kept tokens, 0 elsewhere (greedy: 1
- *   for the argmax).  May not overlap logits.
+ *   for the argmax).  May not overlap logits; rows of both that alternate in
+ *   one buffer need one stride.
  * out (optional, entry (b, i) at out + (b*rows + i)*ld_out): the fixed-point
  *   draw of specdec_sample from those probabilities with the 32-bit word
  *   rand[b*rows + i], or, rand == NULL, Philox(seed, b, step, purpose, index + i)

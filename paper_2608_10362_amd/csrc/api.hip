@@ -1055,6 +1055,18 @@ specdec_status check_accept(int32_t batch, int32_t gamma, int32_t vocab, int32_t
   return SPECDEC_OK;
 }
 
+// Whether n rows of `width` floats at a (stride ld_a) and as many at b may share
+// memory: by their extents, but for rows of one stride that lie between each
+// other's (two slots of one buffer).
+bool rows_overlap(const float* a, int64_t ld_a, const float* b, int64_t ld_b, int64_t n, int64_t width) {
+  const intptr_t a0 = (intptr_t)a, b0 = (intptr_t)b;
+  const intptr_t a1 = a0 + 4 * ((n - 1) * ld_a + width), b1 = b0 + 4 * ((n - 1) * ld_b + width);
+  if (b0 >= a1 || a0 >= b1) return false;
+  if (ld_a != ld_b) return true;
+  const intptr_t period = 4 * ld_a, at = ((b0 - a0) % period + period) % period;
+  return at < 4 * width || at + 4 * width > period;
+}
+
 specdec_status check_rules(int32_t batch, int32_t rows, int32_t vocab) {
   if (batch <= 0 || rows <= 0 || vocab <= 0) return SPECDEC_ERR_INVALID_ARG;
   if (vocab > kRulesMaxVocab || (int64_t)batch * rows > 65535) return SPECDEC_ERR_UNSUPPORTED;
@@ -1186,12 +1198,8 @@ specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab,
       misaligned8(step_dev) || purpose < 0 || purpose > 0xffff || index < 0 || index > 0xffff - (rows - 1) ||
       !workspace || (uintptr_t)workspace % kAlign || workspace_bytes < rules_scratch_bytes(batch * rows, vocab))
     return SPECDEC_ERR_INVALID_ARG;
-  if (probs) {  // (the draw reads logits again after other workgroups have stored probabilities)
-    const int64_t n = (int64_t)batch * rows - 1;
-    const char *p0 = (const char*)probs, *p1 = (const char*)(probs + n * ld_probs + vocab);
-    const char *l0 = (const char*)logits, *l1 = (const char*)(logits + n * ld + vocab);
-    if (p0 < l1 && l0 < p1) return SPECDEC_ERR_INVALID_ARG;
-  }
+  // (the draw reads logits again after other workgroups have stored probabilities)
+  if (probs && rows_overlap(logits, ld, probs, ld_probs, (int64_t)batch * rows, vocab)) return SPECDEC_ERR_INVALID_ARG;
   RulesArgs a{};
   a.B = batch;
   a.rows = rows;

@@ -85,3 +85,15 @@ def test_passes_past_the_attentions_grid_launch_nothing(lib):
     # (a prompt's chunks hold window - 64 tokens: 64, 16 tiles in each of 8192 kv heads)
     assert lib.specdec_prefill(m, ctypes.byref(kv), 80, FAKE, None) == -2
     lib.specdec_model_destroy(m)
+
+
+def test_probabilities_over_the_logits_are_refused(lib):
+    ws = lib.specdec_sample_logits_workspace_bytes(2, 3, 1000)
+
+    def call(probs, ld=2000, ld_probs=2000):
+        return lib.specdec_sample_logits(2, 3, 1000, FAKE, ld, None, None, 0, 0, None, 2, 0, probs, ld_probs, None, 0,
+                                         None, FAKE, ws, None)
+    for at in (0, 4, 3996, 4004, 8000, 8000 * 5 + 3996, -3996, -8000 * 5 - 3996):  # (a row ends at 4000, the next starts at 8000)
+        assert call(FAKE + at) == -1, at
+    for at in (4000, 8000, -4000):  # other strides
+        assert call(FAKE + at, ld_probs=1000) == -1 and call(FAKE + at, ld=1000) == -1
