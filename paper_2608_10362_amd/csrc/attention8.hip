@@ -49,6 +49,7 @@ namespace specdec {
 
 namespace {
 
+constexpr float kLeast = -3.4028234663852886e38f;  // the least finite float32
 constexpr int kPartsMax8 = 64;  // parts of one unit (one per lane of the combining wave)
 // Sub-chunks of 32 keys a wave takes at a time, its chunk: 8 KB of codes for 128
 // dims as for 64.
@@ -366,7 +367,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
     float mx[QT], sm[QT];
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
-      mx[q] = -INFINITY;
+      mx[q] = kLeast;
       sm[q] = 0.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) of[q][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -391,9 +392,10 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       }
     };
     // The running maximum and sum of tile q over new scores p f, which become
-    // probabilities relative to it.  Masked: some may be -inf, all of them for a
-    // query that has seen no key yet (its maximum stays -inf).
-    auto softmax = [&](int q, auto& p, float f, bool masked) {
+    // probabilities relative to it.  Scores may be -inf, masked or below float32's
+    // range: the maximum starts at the least finite value, so they weigh 0 even where
+    // a query has seen no others yet.
+    auto softmax = [&](int q, auto& p, float f) {
       constexpr int N = sizeof(p) / sizeof(float);
       float m = fmaxf(p[0], p[1]);
 #pragma unroll
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       m = groups_max(m) * f;
       const float mnew = fmaxf(mx[q], m);
       if (__any(mnew > mx[q])) {  // (rescaled only where a maximum rose)
-        const float alpha = mx[q] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx[q] - mnew);
+        const float alpha = __builtin_amdgcn_exp2f(mx[q] - mnew);
         sm[q] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) of[q][dt] *= alpha;
@@ -409,8 +411,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float x = __builtin_amdgcn_exp2f(F16 ? __builtin_fmaf(p[e], f, kLift - mx[q]) : p[e] - mx[q]);
-        p[e] = masked && mx[q] == -INFINITY && p[e] == -INFINITY ? 0.f : x;
+        p[e] = __builtin_amdgcn_exp2f(F16 ? __builtin_fmaf(p[e], f, kLift - mx[q]) : p[e] - mx[q]);
         sm[q] += p[e];
       }
     };
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
         f16x8 pp[QT][SP][2];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-          softmax(q, p[q], f[q], false);
+          softmax(q, p[q], f[q]);
 #pragma unroll
           for (int sp = 0; sp < SP; ++sp) {
             float v[8];
@@ -530,7 +531,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
         bf16x8 pp[QT][SP][3];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-          softmax(q, p[q], 1.f, false);
+          softmax(q, p[q], 1.f);
 #pragma unroll
           for (int sp = 0; sp < SP; ++sp) {
             float v[8];
@@ -612,7 +613,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
             float p[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
-            softmax(q, p, 1.f, true);
+            softmax(q, p, 1.f);
             bf16x8 pp[3];
             split8(p, pp);
             constexpr int DG = DT < 4 ? DT : 4;
@@ -675,16 +676,15 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
       __syncthreads();
       const int d = threadIdx.x % (HD / 4) * 4;
       for (int i = threadIdx.x / (HD / 4); i < n_here; i += 64 * NW / (HD / 4)) {
-        float M = -INFINITY, L = 0.f;
+        float M = kLeast, L = 0.f;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) M = fmaxf(M, sh.m.ml[w][i][0]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          // (a wave without keys: maximum -inf, sum and outputs 0; NaN scores alone: maximum -inf, a NaN sum)
-          const float m = sh.m.ml[w][i][0], l = sh.m.ml[w][i][1];
-          const float e = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - M);
-          L += e * l;
+          // (a wave without keys: the least maximum, sum and outputs 0; NaN scores alone: that and a NaN sum)
+          const float e = __builtin_amdgcn_exp2f(sh.m.ml[w][i][0] - M);
+          L += e * sh.m.ml[w][i][1];
           o += e * *(const f32x4*)&sh.m.o[w][i][d];
         }
         const int qa = (tile * QT + q) * 16 + i, qr = div_small(qa, inv_group);
@@ -730,7 +730,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
             qr[r] = div_small(qa, inv_group);
             head[r] = g * group + qa - qr[r] * group;
             slot[r] = ((size_t)(b * rps + qr[r]) * H + head[r]) * parts;
-            ml[r] = lane < n ? get2(a.ml_part + 2 * (slot[r] + lane)) : make_float2(-INFINITY, 0.f);
+            ml[r] = lane < n ? get2(a.ml_part + 2 * (slot[r] + lane)) : make_float2(kLeast, 0.f);
             acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
           }
           for (int t0 = 0; t0 < here * steps; t0 += IT) {
@@ -748,7 +748,7 @@ __global__ __launch_bounds__(64 * waves_of(QT), QT > 1 ? 2 : 4) void attn8_kerne
 #pragma unroll
               for (int r = 0; r < RW; ++r) {
                 const float M = wave_max(ml[r].x);
-                wgt[r] = ml[r].x == -INFINITY ? (ml[r].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[r].x - M);
+                wgt[r] = __builtin_amdgcn_exp2f(ml[r].x - M);
                 inv[r] = 1.0f / wave_sum(wgt[r] * ml[r].y);
               }
             }
