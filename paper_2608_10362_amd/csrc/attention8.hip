@@ -12,12 +12,12 @@
 // float32 and enter their products in parts, so that the result is as good as a
 // float32 computation's (3e-7 of it against 1e-6 for the plain form, 7B-like):
 //  - one query tile a wave (at most 64 rows a kv head): codes as bf16, times their
-//    scale (exact), three bf16 parts (8 significant bits each, 2^-27 left; two leave
-//    2^-18, 3.5e-6 of the result over 2048 keys; one leaves 2^-9).  The products are
-//    few and the stream of codes is the bound;
-//  - two tiles: codes as fp16 (exact), two fp16 parts (11 bits each) of the query row
-//    times a power of two that brings its largest to 2^13 (parts far below lose bits
-//    no float32 sum holds), and of 2^15 p.  K's scale multiplies the scores, V's goes
+//    scale (exact), three bf16 parts, which hold a float32 whole (two leave up to
+//    2^-17 of it, 3.5e-6 of the result over 2048 keys; one up to 2^-8).  The products
+//    are few and the stream of codes is the bound;
+//  - two tiles: codes as fp16 (exact), two fp16 parts (up to 2^-23 left) of the query
+//    row times a power of two that brings its largest to 2^13 (parts far below lose
+//    bits no float32 sum holds), and of 2^15 p.  K's scale multiplies the scores, V's goes
 //    into the conversion where the values are fp16's and into the sums where not.
 //    56 -> 49 us against three bf16 parts, which the ring's rows, bf16 values, still take.
 //
@@ -56,7 +56,8 @@ constexpr int kPartsMax8 = 64;  // parts of one unit (one per lane of the combin
 __host__ __device__ constexpr int steps_of(int head_dim) { return head_dim == 128 ? 1 : 2; }
 __host__ __device__ constexpr int chunk_of(int head_dim) { return kF8Sub * steps_of(head_dim); }
 
-// v as a sum of three bf16 values, each of what the ones before leave.
+// v as a sum of three bf16 values, each of what the ones before leave (exact: 24 bits
+// in three times 8 and two signs).
 __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&part)[3]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -69,7 +70,7 @@ __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&part)[3]) {
   }
 }
 
-// v as a sum of two fp16 values (11 significant bits each).
+// v as a sum of two fp16 values (of 24 bits the last may be off: 11 each and a sign).
 __device__ __forceinline__ void split8(const float (&v)[8], f16x8 (&part)[2]) {
   u32x4 h, l;
 #pragma unroll
