@@ -294,7 +294,8 @@ SPECDEC_API specdec_status specdec_kv_advance(specdec_kv* kv, int32_t n, void* s
  * h / (n_heads / n_kv_heads).  out, same shape, float32:
  * softmax(q k^T / sqrt(head_dim)) v, the sums in float32; out may be q, but may
  * not overlap it otherwise.  A key or value row with a NaN or infinity affects
- * the rows that see it and no others.
+ * the rows that see it and no others (they get NaN, or where a value is infinite
+ * that infinity or NaN, as it becomes NaN when its block is rounded).
  * workspace: specdec_attention_workspace_bytes bytes (0 for arguments the call
  * rejects), 256-byte aligned, dead after the call; calls that share one must be
  * ordered on one stream (graphs captured with one, replayed in order).  So must

@@ -59,3 +59,54 @@ def test_parts_of_queries_and_probabilities(hd, kind, L, n, H):
     err = np.abs(got - ref[..., None]).max(-1)
     log(f"parts {kind} hd={hd} L={L} n={n}: worst {err.max():.3g}, {(err / tol).max():.3g} of the bound")
     assert (err <= tol).all()
+
+
+def _bad_rows(kv, rng, L, n, G, hd, rows):
+    """Appends n rows, some with a NaN or infinity: rows[r] = (kind, kv head) of row L + r."""
+    k, v = (_np(_bf16(rng.normal(0, 1.3, (n, G, hd)))) for _ in range(2))
+    kb, vb = k.copy(), v.copy()
+    for r, (kind, g) in rows.items():
+        if kind == "k":
+            kb[r, g, 2] = np.nan
+        else:
+            vb[r, g, 5], vb[r, g, 6] = (np.nan, -np.inf) if kind == "nan" else (np.inf, -np.inf)
+    binding.specdec_kv_append(kv, 0, _bf16(kb[None]), _bf16(vb[None]))
+    return k, v
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("n,H,L", [(70, 4, 150), (100, 2, 407), (66, 8, 63), (129, 2, 0)])
+def test_many_rows_and_rows_that_are_not_seen(hd, n, H, L):
+    """More than 64 query rows a kv head (two tiles a wave): NaN and infinities in K and V
+    rows of the ring, which wraps, affect the queries that see them and no others, in
+    every sub-chunk; slots past the newest row hold NaN."""
+    rng = np.random.default_rng(hd + n + L)
+    G, group = 2, H // 2
+    assert n * group > 64
+    window = (63 + n + 63) // 64 * 64
+    kv = _cache(_shape(hd, H, G, 1), 1, (L + n + 63) // 64 * 64 + 64, window)
+    ck, cv = (_np(_bf16(rng.normal(0, 1.3, (L, G, hd)))) for _ in range(2))
+    if L:
+        kv.write_context(0, 0, 0, _bf16(ck), _bf16(cv))
+    kv.set_state([L], [[0, 1]], [1])
+    # kv head 0: values; kv head 1: a key
+    first, last, key = n // 7, n - 2, n // 2
+    rows = {first: ("inf", 0), n // 3: ("nan", 0), (2 * n) // 3: ("inf", 0), last: ("nan", 0), key: ("k", 1)}
+    k, v = _bad_rows(kv, rng, L, n, G, hd, rows)
+    log(f"rows not seen: hd={hd} n={n} L={L} ring of {window}, bad rows {sorted(rows)}")
+    q = rng.normal(0, 1, (1, n, H, hd)).astype(np.float32)
+    got = _attend(kv, q)
+    sealed = L // 64 * 64
+    keys = np.concatenate([fp8.stored(ck, sealed), k]) if L else k.astype(np.float64)
+    values = np.concatenate([fp8.stored(cv, sealed), v]) if L else v.astype(np.float64)
+    h0, h1 = slice(0, group), slice(group, H)
+    one = lambda x, g: x[:, g:g + 1]  # noqa: E731
+    # rows before the first bad value, all dims; every row, the dims without one
+    _check(got[:, :, h0], q[:, :, h0], [[one(keys, 0), one(values, 0)]], [L], rows=range(first))
+    assert not np.isfinite(got[0, first:, h0, 5]).any() and not np.isfinite(got[0, first:, h0, 6]).any()
+    clean, cut = got[:, :, h0].copy(), one(values, 0).copy()
+    clean[..., 5:7], cut[..., 5:7] = 0, 0
+    _check(clean, q[:, :, h0], [[one(keys, 0), cut]], [L])
+    _check(got[:, :, h1], q[:, :, h1], [[one(keys, 1), one(values, 1)]], [L], rows=range(key))
+    assert np.isnan(got[0, key:, h1]).all()
+    assert kv.read_state()["status"] == 0
