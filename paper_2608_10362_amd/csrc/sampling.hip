@@ -628,14 +628,12 @@ __global__ void commit_kernel(CommitArgs a) {
     const int A = a.n_accepted[b], g = a.gamma;
     if (A < 0 || A > g) continue;
     const int nxt = a.next_token[b];
+    a.len[b] += commit_step(a, b);  // (by the pending count before this commit's)
     if (a.role == SPECDEC_ROLE_TARGET) {
-      a.len[b] += A + 1;
       a.pending[2 * b] = 0;
       a.pending[2 * b + 1] = nxt;
       a.n_pending[b] = 1;
     } else {
-      const int np = a.n_pending[b];
-      a.len[b] += np + min(A, g - 1);
       if (A == g) {
         a.pending[2 * b] = a.d[(size_t)b * a.ld_d + g - 1];
         a.n_pending[b] = 2;
