@@ -221,8 +221,10 @@ SPECDEC_API int32_t specdec_kv_state_count(int32_t batch);
 SPECDEC_API specdec_status specdec_kv_init(specdec_kv* kv, const specdec_model* model, int32_t batch, int32_t capacity,
                                void* data, size_t data_bytes, int32_t* state, void* stream);
 
-/* The same for an 8-bit cache of a bf16 model (dtype SPECDEC_FP8): about half
- * the bytes per position.  Every call that takes a specdec_kv takes one.
+/* The same for an 8-bit cache of a bf16 model (dtype SPECDEC_FP8): half the
+ * bytes per position, a scale per block (1 / (16 head_dim) of that again), and
+ * window / capacity of a bf16 cache for the ring.  Every call that takes a
+ * specdec_kv takes one.
  * Positions lie in blocks of 64.  The whole blocks a sequence has committed
  * (positions below len / 64 * 64) are held as e4m3 codes with one scale 2^e
  * per (layer, sequence, kv head, block, K or V), e the smallest integer with

@@ -429,12 +429,25 @@ class KVCache:
         return int(self.state[4 * B + 2:4 * B + 4].cpu().numpy().view(np.uint64)[0])
 
 
+def default_window(max_rows: int, batch: int, capacity: int) -> int:
+    """The window of an Fp8KVCache for a handle of ``max_rows`` rows (0: none): what a
+    prompt's chunk of these rows needs, at most a quarter of the capacity, at least 128.
+
+    A prompt runs in chunks of window - 64 tokens per sequence, so a wide ring makes prefill
+    faster, and is most of the cache where contexts are short.  Past 1024 rows a pass it
+    brings nothing: 4096 tokens, 7B-like, four layers, 11.4 ms at a window of 2112 (as
+    over a bf16 cache), 11.3 at 1088, 12.3 at 576, 20 at 256, 30 at 128."""
+    need = (min(max_rows, 1024) // batch + 64 + 63) // 64 * 64
+    return max(128, min(need, capacity // 4 // 64 * 64))
+
+
 class Fp8KVCache(KVCache):
     """An 8-bit cache (see specdec_kv_init_fp8): takes the place of a KVCache of
     a bf16 model in every call, or serves a caller's own model through
     specdec_kv_append, specdec_attention and specdec_kv_advance.  ``of``: the
     Model that uses it, or a model shape (then ``n_layers`` of it).  ``window``:
-    positions of the bf16 ring, by default 128 and what the handle's rows fill."""
+    positions of the bf16 ring, default_window's if not given.  Bytes, as a share of a
+    bf16 cache's: 0.5 and a little, and window / capacity."""
 
     def __init__(self, of, batch: int, capacity: int, window: Optional[int] = None, n_layers: Optional[int] = None,
                  device="cuda", stream=None):
@@ -447,8 +460,7 @@ class Fp8KVCache(KVCache):
             desc = make_desc(of)
             n_layers = of.n_layers if n_layers is None else n_layers
         if window is None:
-            rows = of.max_rows // batch if self.model is not None else 0
-            window = max(128, (rows + 64 + 63) // 64 * 64)
+            window = default_window(0 if self.model is None else of.max_rows, batch, capacity)
         nbytes = lib().specdec_kv_bytes_fp8(ctypes.byref(desc), n_layers, batch, capacity, window)
         if nbytes == 0:
             raise SpecdecError(-2, "specdec_kv_bytes_fp8")
