@@ -5,8 +5,8 @@ import pytest
 from oracle import fp8
 from paper_2608_10362_amd import binding
 from tests import fp8_parts
-from tests.gpu_util import log
-from tests.test_gpu_fp8_cache import _attend, _bf16, _cache, _check, _np, _shape
+from tests.gpu_util import log, torch_cuda
+from tests.test_gpu_fp8_cache import _attend, _bf16, _cache, _check, _fill, _np, _shape
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,82 @@ def test_many_rows_and_rows_that_are_not_seen(hd, n, H, L):
     _check(got[:, :, h1], q[:, :, h1], [[one(keys, 1), one(values, 1)]], [L], rows=range(key))
     assert np.isnan(got[0, key:, h1]).all()
     assert kv.read_state()["status"] == 0
+
+
+@pytest.mark.parametrize("case", [
+    (128, 7, 1, [333], 1), (64, 71, 1, [200], 1), (32, 128, 1, [700], 1), (64, 128, 1, [90, 4000], 2),
+    (128, 142, 2, [130], 3), (32, 34, 17, [64, 0, 65], 7)], ids=lambda c: f"hd{c[0]}-{c[1]}:{c[2]}-n{c[4]}")
+def test_odd_groups_and_the_largest(case):
+    """Query heads per kv head of 3 to 128, the last length up to the capacity, the second of two layers."""
+    hd, H, G, lens, n = case
+    rng = np.random.default_rng(H + n)
+    cap = (max(lens) + n + 63) // 64 * 64
+    lens = [cap - n if x == max(lens) else x for x in lens]  # (the longest fills the cache)
+    kv = _cache(_shape(hd, H, G, 2), len(lens), cap, 128)
+    _fill(kv, rng, lens, n, G, hd, layer=0)
+    kvs = _fill(kv, rng, lens, n, G, hd, layer=1)
+    q = rng.normal(0, 1.5, (len(lens), n, H, hd)).astype(np.float32)
+    log(f"groups {case}: worst error {_check(_attend(kv, q, 1), q, kvs, lens):.3g}")
+    binding.specdec_kv_advance(kv, n)
+    assert kv.read_state()["status"] == 0
+
+
+def test_two_caches_on_two_streams():
+    """Calls at once on two caches, with workspaces of their own, eager and captured."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(3)
+    hd, H, G, n = 64, 8, 1, 2
+    lens = [[5000, 17], [333, 2048]]
+    kvs = [_cache(_shape(hd, H, G, 1), 2, 5056, 128) for _ in lens]
+    held = [_fill(kv, rng, L, n, G, hd) for kv, L in zip(kvs, lens)]
+    q = [torch.from_numpy(rng.normal(0, 1.5, (2, n, H, hd)).astype(np.float32)).cuda() for _ in lens]
+    out = [torch.empty_like(x) for x in q]
+    ws = [binding.attention_workspace(kv, H, n) for kv in kvs]
+    streams, graphs = [torch.cuda.Stream() for _ in lens], []
+    torch.cuda.synchronize()
+    for j in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=streams[j]):
+            binding.specdec_attention(kvs[j], 0, q[j], out[j], ws[j])
+        graphs.append(g)
+    for rep in range(4):
+        for o in out:
+            o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        log(f"two caches at once, {rep}")
+        for i in range(5):
+            for j in range(2):
+                if rep % 2:
+                    binding.specdec_attention(kvs[j], 0, q[j], out[j], ws[j], stream=streams[j])
+                else:
+                    with torch.cuda.stream(streams[j]):
+                        graphs[j].replay()
+        torch.cuda.synchronize()
+        for j in range(2):
+            _check(out[j].cpu().numpy(), q[j].cpu().numpy(), held[j], lens[j])
+
+
+def test_lengths_set_back_and_grown_again():
+    """A length set back (drafted text thrown away) and grown by other rows: codes of blocks that are
+    completed anew, the ring's of those that are not, for a ring that has wrapped."""
+    rng = np.random.default_rng(9)
+    hd, H, G, window, cap = 64, 4, 2, 192, 640
+    kv = _cache(_shape(hd, H, G, 1), 1, cap, window)
+    k, v = (rng.normal(0, 1.3, (cap, G, hd)) for _ in range(2))
+    k, v = _np(_bf16(k)), _np(_bf16(v))
+    L = 500
+    kv.write_context(0, 0, 0, _bf16(k[:L]), _bf16(v[:L]))
+    for back in (500, 449, 447, 400, 380):
+        kv.set_state([back], [[0, 1]], [1])
+        n = 5
+        k2, v2 = (_np(_bf16(rng.normal(0, 1.3, (n, G, hd)))) for _ in range(2))
+        binding.specdec_kv_append(kv, 0, _bf16(k2[None]), _bf16(v2[None]))
+        k[back:back + n], v[back:back + n] = k2, v2
+        q = rng.normal(0, 1.5, (1, n, H, hd)).astype(np.float32)
+        sealed = back // 64 * 64
+        log(f"set back to {back}")
+        _check(_attend(kv, q), q, [[fp8.stored(k[:back + n], sealed), fp8.stored(v[:back + n], sealed)]], [back])
+        binding.specdec_kv_advance(kv, n)
+        now = (back + n) // 64 * 64
+        for got, x in zip(kv.read_context(0, 0, 0, back + n), (k, v)):
+            np.testing.assert_array_equal(_np(got), fp8.stored(x[:back + n], now))
