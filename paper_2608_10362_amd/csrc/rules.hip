@@ -412,7 +412,7 @@ struct Select {
   uint32_t hist_c[256];
   unsigned long long sum[kWaves], lo[kWaves], hi[kWaves];
   int digit;
-  uint32_t left;
+  uint32_t left, n_few;
   unsigned long long before, result;
 };
 
@@ -526,13 +526,13 @@ __device__ __forceinline__ unsigned long long select_border(SRC src, unsigned lo
   // the entries that share the prefix, in the histogram's place
   ulonglong2* few = (ulonglong2*)sh.hist_m;
   if (threadIdx.x < kFew) few[threadIdx.x] = make_ulonglong2(0ull, 0ull);
-  if (threadIdx.x == 0) sh.left = 0u;
+  if (threadIdx.x == 0) sh.n_few = 0u;  // (not `left`, which other waves may not have read yet)
   __syncthreads();
   src([&](unsigned long long key, unsigned long long m) {
-    if (top >= 64 || (key >> top) == (prefix >> top)) few[atomicAdd(&sh.left, 1u)] = make_ulonglong2(key, by_mass ? m : 1ull);
+    if (top >= 64 || (key >> top) == (prefix >> top)) few[atomicAdd(&sh.n_few, 1u)] = make_ulonglong2(key, by_mass ? m : 1ull);
   });
   __syncthreads();
-  const int n = (int)sh.left, parts = parts_of(n), at = threadIdx.x / parts;
+  const int n = (int)sh.n_few, parts = parts_of(n), at = threadIdx.x / parts;
   const ulonglong2 own = at < n ? few[at] : make_ulonglong2(0ull, 0ull);
   unsigned long long before;
   rank_pairs(few, n, parts, own.x, before);
