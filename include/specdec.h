@@ -266,7 +266,10 @@ SPECDEC_API specdec_status specdec_kv_init_fp8(specdec_kv* kv, const specdec_mod
  * FP8 caches: k, v are bf16; pos0 must be a multiple of 64 (SHAPE otherwise).
  * The blocks that end inside the range are quantized, and its last `window`
  * rows go to the ring as well, so a following specdec_kv_set_state may set
- * len to pos0 + n (or up to window - 63 positions less). */
+ * len to pos0 + n (or up to window - 63 positions less).  In the ring they take
+ * the places (position mod window) of the rows that were there: a context is
+ * written in order, and after a write behind a sequence's newest positions
+ * (below len - window) those from len / 64 * 64 on are written again. */
 SPECDEC_API specdec_status specdec_kv_write_context(specdec_kv* kv, int32_t layer, int32_t b, int32_t pos0, int32_t n,
                                         const void* k, const void* v, void* stream);
 /* Copy K and V rows back out (same layout as specdec_kv_write_context).  FP8

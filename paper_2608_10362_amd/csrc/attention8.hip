@@ -29,15 +29,16 @@
 // put all units' chunks on a line, and workgroup i takes the i-th `per` of them: all stream
 // the same bytes whatever the lengths.  Other calls have a workgroup per range.
 //
-// Measured.  7B-like (32 kv heads of 128): one row over 2048 keys 10.0 us (a chain of
+// Measured.  7B-like (32 kv heads of 128): one row over 2048 keys 9.8 us (a chain of
 // start 3, codes and products 3, merge 1.5, parts 2.5); 16 ragged rows over 1024 to
-// 8191 keys 114 us, 5.3 TB/s of codes (99 us, 6.1 TB/s, where all are 4607 long and
-// no unit is cut; reads alone reach 5.6 to 6.5); 512 rows over 2048 keys 43 us,
-// 351 TFLOP/s of the operator's products, twice that in the matrix unit (half the
+// 8191 keys 112 us, 5.4 TB/s of codes (99 us, 6.1 TB/s, where all are 4607 long and
+// no unit is cut; a read of as many bytes takes 94); 512 rows over 2048 keys 42 us,
+// 358 TFLOP/s of the operator's products, twice that in the matrix unit (half the
 // time is conversions and softmax, which its products do not hide, a quarter the
 // ring's rows).  1.1B-like (4 kv heads of 64, 8 query heads each): one row over
-// 131072 keys 20.9 us, 3.2 TB/s (14 us of stream; 61 parts of one unit by one
-// workgroup 5 us), 4 x 5 rows over 301 to 1028 keys 10.0 us.
+// 131072 keys 20.7 us, 3.2 TB/s (14 us of stream; 61 parts of one unit by one
+// workgroup 5 us), 4 x 5 rows over 301 to 1028 keys 9.8 us, 8 x 5 rows over 8192
+// keys 23 us, 1.4 TB/s (each of a kv head's three query tiles reads its codes).
 #include <algorithm>
 
 #include "device_common.h"

@@ -266,7 +266,8 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_read_kernel(Kv8Layout kv, in
   }
 }
 
-// Grid (n, batch).
+// Grid (n, batch).  7B-like (32 kv heads of 128): 1 row 4.8 us (7 with the host's call),
+// 512 rows 17 us, 2048 rows 52 us, 1.3 TB/s: V goes out two bytes at a time, 16 apart.
 __global__ __launch_bounds__(kCopyThreads) void kv8_append_kernel(Kv8Layout kv, int layer, int n, const uint16_t* k,
                                                                   const uint16_t* v, int32_t* status, int pos_limit) {
   const int b = blockIdx.y, i = blockIdx.x, pos = kv.len[b] + i;
@@ -279,7 +280,11 @@ __global__ __launch_bounds__(kCopyThreads) void kv8_append_kernel(Kv8Layout kv, 
 }
 
 // Grid (kv heads / kSealHeads, layers, batch).  Most calls complete no block of
-// most sequences: such a workgroup ends after reading two words.
+// most sequences: such a workgroup ends after reading two words.  A commit over 8 layers,
+// 7B-like, takes 3 us longer than over a bf16 cache where no block is completed, 8 where
+// one sequence completes one, 30 where 16 do.  Blocks of one call are taken in turn:
+// advances by 512 and 2048 rows (8 and 32 blocks, 8 layers) take 82 and 362 us,
+// 1.2 and 1.1 TB/s.
 constexpr int kSealHeads = 4;
 template <int HD>
 __global__ __launch_bounds__(kCopyThreads) void kv8_seal_kernel(Kv8Layout kv, int c0, int n, int is_commit,

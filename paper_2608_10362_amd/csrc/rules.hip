@@ -29,15 +29,18 @@
 // From scan on, threads whose maximum lies below the border (the bound) read nothing:
 // a row with a border is read once or twice, not four times.  Lists of at most 256
 // are ranked by comparing all pairs, longer ones by digits; a list that overflows
-// (thousands of equal logits) is replaced by passes over the row itself, by one
-// workgroup: slow, and right.
+// is replaced by passes over the row itself, by one workgroup: slow, and right.  That
+// takes thousands of equal logits; or a top-k past about 2400 (1 x 32000: 40 us at 2300,
+// 157 at 2500); or one near the row's groups, 256 a chunk, or above, where there are
+// so many rows that each has few chunks (640 rows of 32000, three chunks each: 117 us at
+// 500, 507 at 760; 1536 rows, one each: 181 us at 200, 556 at 250).
 //
 // What bounds it.  Few rows: launches and the chains inside them (loads of the words
-// before, one counter a row): 1 x 32000, top-k 50 17.4 us, 1000 30 us (a list past 256);
-// 16 x 128256, top-p 35 us, in kernels of 5 + 12 + 10 + 9 us.  Many rows: the
+// before, one counter a row): 1 x 32000, top-k 50 17.5 us, 1000 31 us (a list past 256);
+// 16 x 128256, top-p 37 to 42 us, in kernels of 6 + 13 + 13 + 11 us.  Many rows: the
 // exponentials of rows without a top-k (64-bit, 25 instructions) and the bytes.
-// 112 x 128256 with probabilities (57 MB read once, 57 MB written): top-k and top-p
-// 62 us, 1.9 TB/s; neither 87 us (read three times); top-p 116 us.
+// 112 x 128256 with probabilities (57 MB read once, 57 MB written): top-k 50 62 us,
+// 1.9 TB/s; top-k 1000 94 us; neither 96 us (read three times); top-p 105 us; greedy 31 us.
 // Six workgroups a CU (kGridTarget): with four the scan of 112 mixed rows is 32 us, not
 // 35, but the last launch 33, not 28.  No kernel may spill, for one that uses scratch
 // memory starts late (scan of 16 x 128256: 22 us with 16 spilled registers, 12 us with
