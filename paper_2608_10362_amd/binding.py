@@ -437,7 +437,7 @@ def default_window(max_rows: int, batch: int, capacity: int) -> int:
     faster, and is most of the cache where contexts are short.  Past 1024 rows a pass it
     brings nothing: 4096 tokens, 7B-like, four layers, 11.4 ms at a window of 2112 (as
     over a bf16 cache), 11.3 at 1088, 12.3 at 576, 20 at 256, 30 at 128."""
-    need = (min(max_rows, 1024) // batch + 64 + 63) // 64 * 64
+    need = (min(max_rows, 1024) // max(batch, 1) + 64 + 63) // 64 * 64
     return max(128, min(need, capacity // 4 // 64 * 64))
 
 

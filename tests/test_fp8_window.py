@@ -36,3 +36,10 @@ def test_the_default_takes_the_handles_rows_where_a_quarter_holds_them():
     assert binding.default_window(2048, 1, 2048) == 512    # a quarter of the capacity
     assert binding.default_window(2048, 1, 32768) == 1088  # more than 1024 rows a pass bring nothing
     assert binding.default_window(0, 1, 64) == 128
+
+
+@pytest.mark.parametrize("batch,capacity", [(0, 512), (-1, 512), (2, 0), (2, -64), (2, 100), (65536, 64)])
+def test_sizes_without_a_cache_are_refused_as_shapes(lib, batch, capacity):
+    with pytest.raises(binding.SpecdecError) as e:
+        binding.Fp8KVCache(synth.LLAMA_1B, batch, capacity, n_layers=1, device="cpu")
+    assert e.value.status == -2
