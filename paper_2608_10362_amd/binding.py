@@ -446,8 +446,9 @@ class Fp8KVCache(KVCache):
     a bf16 model in every call, or serves a caller's own model through
     specdec_kv_append, specdec_attention and specdec_kv_advance.  ``of``: the
     Model that uses it, or a model shape (then ``n_layers`` of it).  ``window``:
-    positions of the bf16 ring, default_window's if not given.  Bytes, as a share of a
-    bf16 cache's: 0.5 and a little, and window / capacity."""
+    positions of the bf16 ring, default_window's if not given; a verify pass or an append of
+    n rows a sequence needs n + 63.  Bytes, as a share of a bf16 cache's: 0.5 and a
+    little, and window / capacity."""
 
     def __init__(self, of, batch: int, capacity: int, window: Optional[int] = None, n_layers: Optional[int] = None,
                  device="cuda", stream=None):
