@@ -316,6 +316,68 @@ SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer
                                              const float* q, float* out, void* workspace, size_t workspace_bytes,
                                              void* stream);
 
+/* The norm and the position rotation of a model's queries and keys, head by head
+ * (host POD; specdec_rope_init fills it, the caller keeps it):
+ *   y = gain * x / sqrt(mean(x^2) + eps) over a head's head_dim entries (queries
+ *     and keys each where their gain is given), then for the pairs j < rotary_dim
+ *     / 2, dims (a, b) = (j, j + rotary_dim / 2), or (2j, 2j + 1) if interleaved,
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t), t = position *
+ *     freq[j]; dims from rotary_dim on stay.
+ * Angles and sums of squares are taken in float64, the rest in float32, and the
+ * result is rounded once to its type. */
+#define SPECDEC_ROPE_MAX_PAIRS 64
+typedef struct {
+  int32_t head_dim;    /* 32, 64 or 128 */
+  int32_t rotary_dim;  /* a multiple of 16, 0 (no rotation) .. head_dim */
+  int32_t interleaved; /* 0 or 1 */
+  int32_t gain_dtype;  /* SPECDEC_F32 or SPECDEC_BF16 */
+  const void* q_gain;  /* device [head_dim], or NULL: no norm */
+  const void* k_gain;
+  float eps;           /* >= 0 */
+  double freq[SPECDEC_ROPE_MAX_PAIRS]; /* radians a position: specdec_rope_init sets base^(-2j/rotary_dim); a
+                                          caller may set others (stretched contexts) */
+} specdec_rope;
+SPECDEC_API specdec_status specdec_rope_init(specdec_rope* rope, int32_t head_dim, int32_t rotary_dim, double base,
+                                             int32_t interleaved, const void* q_gain, const void* k_gain,
+                                             int32_t gain_dtype, float eps);
+
+/* Norm and rotation of `batch` x n rows of queries and keys: row r = b * n + i of
+ * q (n_heads heads of head_dim, consecutive) at q + r * ld_q elements, of k
+ * (n_kv_heads) at k + r * ld_k: views of a fused projection need no copy.  Results go
+ * to q_out and k_out with the strides ld_qo and ld_ko.  dtype (of q and k),
+ * out_dtype: SPECDEC_F32 or SPECDEC_BF16.  Either of q and k may be absent (NULL,
+ * no heads).  Position of row r: offset + positions[r] (device, [batch * n]), or,
+ * positions == NULL, offset + i.
+ * An output may be its own input (same address, stride and type); otherwise no
+ * output may overlap an input or the other output, but for rows of one stride
+ * that lie between each other's.
+ * Asynchronous, no workspace.  Errors: INVALID_ARG, SHAPE (head_dim, rotary_dim;
+ * batch * n past 2^25 rows), HIP. */
+SPECDEC_API specdec_status specdec_rope_apply(const specdec_rope* rope, int32_t batch, int32_t n, int32_t n_heads,
+                                              int32_t n_kv_heads, int32_t dtype, const void* q, int64_t ld_q,
+                                              const void* k, int64_t ld_k, const int32_t* positions, int64_t offset,
+                                              int32_t out_dtype, void* q_out, int64_t ld_qo, void* k_out, int64_t ld_ko,
+                                              void* stream);
+
+/* The same, and specdec_kv_append, in one pass over an FP8 cache (UNSUPPORTED
+ * otherwise): the n new rows of every sequence, keys normalised and rotated and
+ * values as they are, go to `layer` as specdec_kv_append puts them (bf16, positions
+ * len[b] .. len[b]+n-1, not committed), the queries to q_out [batch, n, n_heads,
+ * head_dim] (float32 for specdec_attention, either type for
+ * specdec_attention_shared).  Rows of v at v + r * ld_v.  positions == NULL: row i of
+ * sequence b turns by offset + len[b] + i (offset: what came before the cache's
+ * first position, as a shared prefix), else by offset + positions[r].
+ * q_out may be q (same type, ld_q = n_heads * head_dim) and may not overlap an
+ * input otherwise.
+ * Errors: INVALID_ARG, UNSUPPORTED, SHAPE (as above; head_dim not the cache's,
+ * n_heads not a multiple of its kv heads, n > window - 63), KV_CAPACITY
+ * (len_upper + n > capacity). */
+SPECDEC_API specdec_status specdec_rope_append(specdec_kv* kv, int32_t layer, const specdec_rope* rope, int32_t n,
+                                               int32_t n_heads, int32_t dtype, const void* q, int64_t ld_q,
+                                               const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                                               const int32_t* positions, int64_t offset, int32_t out_dtype, void* q_out,
+                                               void* stream);
+
 /* Set lengths and pending tokens from HOST arrays: len[B], pending[2B]
  * (right-aligned: pending[2b+1] is the newest token), n_pending[B] in {1,2}.
  * Clears the status word and leaves the commit counter as it is.

@@ -69,6 +69,12 @@ class Sampling(ctypes.Structure):
                 ("min_p", ctypes.c_void_p)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("gain_dtype", ctypes.c_int32), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("freq", ctypes.c_double * 64)]
+
+
 _lib = None
 
 _SIGS = {
@@ -140,6 +146,19 @@ _SIGS = {
     "specdec_kv_append": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                                          ctypes.c_void_p, ctypes.c_void_p]),
     "specdec_kv_advance": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_void_p]),
+    "specdec_rope_init": (ctypes.c_int, [ctypes.POINTER(RopeDesc), ctypes.c_int32, ctypes.c_int32, ctypes.c_double,
+                                         ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                         ctypes.c_float]),
+    "specdec_rope_apply": (ctypes.c_int, [ctypes.POINTER(RopeDesc), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                          ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
+                                          ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                          ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                          ctypes.c_int64, ctypes.c_void_p]),
+    "specdec_rope_append": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.POINTER(RopeDesc),
+                                           ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
+                                           ctypes.c_void_p, ctypes.c_void_p]),
     "specdec_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32]),
     "specdec_attention": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
@@ -573,6 +592,121 @@ def specdec_kv_advance(kv: KVCache, n: int, stream=None):
     import torch
     _on_current(kv.data, "kv", torch.uint8)
     _check(lib().specdec_kv_advance(ctypes.byref(kv.kv), n, _stream(stream)), "specdec_kv_advance")
+
+
+class Rope:
+    """The norm and position rotation of a model's heads (see specdec_rope).  ``rotary_dim``:
+    dims that turn (all of them if not given); ``q_gain``, ``k_gain``: device
+    tensors [head_dim], both float32 or both bfloat16, or None (no norm); ``freqs``: radians
+    a position of every pair in place of base^(-2j / rotary_dim)."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0,
+                 interleaved: bool = False, q_gain=None, k_gain=None, eps: float = 1e-6, freqs=None):
+        import torch
+        gains = [g for g in (q_gain, k_gain) if g is not None]
+        dtype = gains[0].dtype if gains else torch.float32
+        for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
+            if g is not None:
+                _dev(g, name, dtype)
+                _same_device(g, name, gains[0])
+                if tuple(g.shape) != (head_dim,):
+                    raise ValueError(f"{name}: expected [{head_dim}]")
+        self.gains = (q_gain, k_gain)  # (kept alive with the rule)
+        self.c = RopeDesc()
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        _check(lib().specdec_rope_init(ctypes.byref(self.c), head_dim, rotary_dim, base, int(interleaved),
+                                       _ptr(q_gain), _ptr(k_gain), _float_type(dtype, "gains"), eps),
+               "specdec_rope_init")
+        if freqs is not None:
+            freqs = [float(f) for f in freqs]
+            if len(freqs) != rotary_dim // 2:
+                raise ValueError(f"freqs: expected {rotary_dim // 2} entries")
+            self.c.freq[:len(freqs)] = freqs
+
+    def _on(self, t):
+        for g in self.gains:
+            if g is not None:
+                _same_device(t, "inputs", g)
+
+
+def _float_type(dtype, name: str) -> int:
+    import torch
+    if dtype == torch.bfloat16:
+        return SPECDEC_BF16
+    if dtype == torch.float32:
+        return SPECDEC_F32
+    raise ValueError(f"{name}: expected float32 or bfloat16, got {dtype}")
+
+
+def _head_rows(t, name: str, head_dim: int, dtype=None) -> int:
+    """The stride between the rows of t [batch, n, heads, head_dim], whose heads lie side by side."""
+    if t.dim() != 4 or t.shape[3] != head_dim:
+        raise ValueError(f"{name}: expected [batch, n, heads, {head_dim}]")
+    _on_current(t, name, t.dtype if dtype is None else dtype)
+    if t.is_contiguous():
+        return t.shape[2] * head_dim
+    if t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != head_dim):
+        raise ValueError(f"{name}: a row's heads must lie side by side")
+    return _row_stride(t[:, :, 0], name, t.shape[2] * head_dim)
+
+
+def _positions(positions, batch: int, n: int, like):
+    import torch
+    if positions is None:
+        return None
+    if tuple(positions.shape) != (batch, n):
+        raise ValueError(f"positions: expected [{batch}, {n}]")
+    _same_device(positions, "positions", like)
+    return _dev(positions, "positions", torch.int32)
+
+
+def specdec_rope_apply(rope: Rope, q, k, q_out, k_out, positions=None, offset: int = 0, stream=None):
+    """q, q_out [batch, n, n_heads, head_dim], k, k_out [batch, n, n_kv_heads, head_dim], float32 or
+    bfloat16 (inputs of one type, outputs of one), each with one stride between its rows; q and
+    q_out, or k and k_out, may be None.  positions: int32 [batch, n] (0 .. n-1 if not given).
+    An output may be its own input."""
+    given = [t for t in (q, k) if t is not None]
+    if not given or (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q, k: expected one of them at least, each with its output")
+    out = q_out if q_out is not None else k_out
+    batch, n = given[0].shape[:2]
+    hd, lds = rope.c.head_dim, []
+    for name, t, to in (("q", q, q_out), ("k", k, k_out)):
+        if t is None:
+            lds += [0, 0]
+            continue
+        lds += [_head_rows(t, name, hd, given[0].dtype), _head_rows(to, name + "_out", hd, out.dtype)]
+        if t.shape != to.shape or tuple(t.shape[:2]) != (batch, n):
+            raise ValueError(f"{name}, {name}_out: expected one shape, of one batch of rows")
+    rope._on(given[0])
+    _check(lib().specdec_rope_apply(ctypes.byref(rope.c), batch, n, 0 if q is None else q.shape[2],
+                                    0 if k is None else k.shape[2], _float_type(given[0].dtype, "inputs"), _ptr(q),
+                                    lds[0], _ptr(k), lds[2], _positions(positions, batch, n, given[0]), offset,
+                                    _float_type(out.dtype, "outputs"), _ptr(q_out), lds[1], _ptr(k_out), lds[3],
+                                    _stream(stream)), "specdec_rope_apply")
+
+
+def specdec_rope_append(kv: KVCache, layer: int, rope: Rope, q, k, v, q_out, positions=None, offset: int = 0,
+                        stream=None):
+    """q [batch, n, n_heads, head_dim], k, v [batch, n, n_kv_heads, head_dim], float32 or bfloat16, each
+    with one stride between its rows; q_out: contiguous, of q's shape, float32 or
+    bfloat16 (may be q).  positions: int32 [batch, n], the cache's own (offset + len[b] + i) if
+    not given."""
+    hd, G = kv.kv.head_dim, kv.kv.n_kv_heads
+    lds = [_head_rows(t, name, hd, q.dtype) for name, t in (("q", q), ("k", k), ("v", v))]
+    n = q.shape[1]
+    if q.shape[0] != kv.batch or k.shape != v.shape or tuple(k.shape) != (kv.batch, n, G, hd):
+        raise ValueError(f"q, k, v: expected rows of a batch of {kv.batch}, {G} kv heads")
+    _on_current(q_out, "q_out", q_out.dtype)
+    if q_out.shape != q.shape or not q_out.is_contiguous():
+        raise ValueError("q_out: expected a contiguous tensor of q's shape")
+    _same_device(kv.data, "kv", q)
+    rope._on(q)
+    _check(lib().specdec_rope_append(ctypes.byref(kv.kv), layer, ctypes.byref(rope.c), n, q.shape[2],
+                                     _float_type(q.dtype, "inputs"), q.data_ptr(), lds[0], k.data_ptr(), lds[1],
+                                     v.data_ptr(), lds[2], _positions(positions, kv.batch, n, q), offset,
+                                     _float_type(q_out.dtype, "q_out"), q_out.data_ptr(), _stream(stream)),
+           "specdec_rope_append")
 
 
 def attention_workspace(kv: KVCache, n_heads: int, n: int):

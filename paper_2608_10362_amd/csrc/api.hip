@@ -1,6 +1,7 @@
 // C ABI of the speculative-decoding hot path: argument validation, workspace
 // carving, and the launch sequence of one forward pass (verify or draft step).
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <vector>
 
@@ -281,6 +282,56 @@ specdec_status check_attention(const specdec_kv* kv, int n_heads, int n) {
       !attention8_fits(n, kv->batch, n_heads, kv->n_kv_heads))
     return SPECDEC_ERR_SHAPE;
   return SPECDEC_OK;
+}
+
+// Whether n rows of `bytes_a` at a (stride ld_a, in bytes too) and as many of `bytes_b` at b may
+// share memory: by their extents, but for rows of one stride that lie between each
+// other's (two slots of one buffer).
+bool rows_overlap(const void* a, int64_t ld_a, int64_t bytes_a, const void* b, int64_t ld_b, int64_t bytes_b,
+                  int64_t n) {
+  const intptr_t a0 = (intptr_t)a, b0 = (intptr_t)b;
+  const intptr_t a1 = a0 + (n - 1) * ld_a + bytes_a, b1 = b0 + (n - 1) * ld_b + bytes_b;
+  if (b0 >= a1 || a0 >= b1) return false;
+  if (ld_a != ld_b) return true;
+  const intptr_t at = ((b0 - a0) % ld_a + ld_a) % ld_a;
+  return at < bytes_a || at + bytes_b > ld_a;
+}
+
+specdec_status check_rope(const specdec_rope* r) {
+  if (!r || (r->gain_dtype != SPECDEC_F32 && r->gain_dtype != SPECDEC_BF16) || !(r->eps >= 0.f) ||
+      (r->interleaved != 0 && r->interleaved != 1) || r->head_dim <= 0 || r->rotary_dim < 0)
+    return SPECDEC_ERR_INVALID_ARG;
+  if ((r->head_dim != 32 && r->head_dim != 64 && r->head_dim != 128) || r->rotary_dim % 16 ||
+      r->rotary_dim > r->head_dim)
+    return SPECDEC_ERR_SHAPE;
+  return SPECDEC_OK;
+}
+
+bool is_float_type(int dtype) { return dtype == SPECDEC_F32 || dtype == SPECDEC_BF16; }
+
+// What a rotation's launch takes from its rule and its inputs.
+RopeArgs rope_args(const specdec_rope* r, int n, int n_heads, int n_kv_heads, const void* q, int64_t ld_q,
+                   const void* k, int64_t ld_k, const int32_t* positions, int64_t offset, void* q_out, int64_t ld_qo) {
+  RopeArgs a{};
+  a.q = q;
+  a.k = k;
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.q_out = q_out;
+  a.ld_qo = ld_qo;
+  a.n = n;
+  a.n_heads = n_heads;
+  a.n_kv_heads = n_kv_heads;
+  a.q_gain = r->q_gain;
+  a.k_gain = r->k_gain;
+  a.gain_bf16 = r->gain_dtype == SPECDEC_BF16;
+  a.eps = r->eps;
+  a.rotary = r->rotary_dim;
+  a.interleaved = r->interleaved;
+  a.positions = positions;
+  a.offset = offset;
+  for (int j = 0; j < r->rotary_dim / 2; ++j) a.turns[j] = r->freq[j] * 0.15915494309189533577;  // 1 / (2 pi)
+  return a;
 }
 
 // Runs GEMM `g` over the rows [0, M) in launches of at most gemm_launch_rows rows
@@ -804,6 +855,94 @@ specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_
   return hip_status(launch_attention8(a, (hipStream_t)stream));
 }
 
+specdec_status specdec_rope_init(specdec_rope* rope, int32_t head_dim, int32_t rotary_dim, double base,
+                                 int32_t interleaved, const void* q_gain, const void* k_gain, int32_t gain_dtype,
+                                 float eps) {
+  if (!rope || !(base > 0.0) || !std::isfinite(base)) return SPECDEC_ERR_INVALID_ARG;
+  specdec_rope r{};
+  r.head_dim = head_dim;
+  r.rotary_dim = rotary_dim;
+  r.interleaved = interleaved;
+  r.gain_dtype = gain_dtype;
+  r.q_gain = q_gain;
+  r.k_gain = k_gain;
+  r.eps = eps;
+  const specdec_status st = check_rope(&r);
+  if (st != SPECDEC_OK) return st;
+  for (int j = 0; j < rotary_dim / 2; ++j) r.freq[j] = std::pow(base, -2.0 * j / rotary_dim);
+  *rope = r;
+  return SPECDEC_OK;
+}
+
+specdec_status specdec_rope_apply(const specdec_rope* rope, int32_t batch, int32_t n, int32_t n_heads,
+                                  int32_t n_kv_heads, int32_t dtype, const void* q, int64_t ld_q, const void* k,
+                                  int64_t ld_k, const int32_t* positions, int64_t offset, int32_t out_dtype,
+                                  void* q_out, int64_t ld_qo, void* k_out, int64_t ld_ko, void* stream) {
+  const specdec_status st = check_rope(rope);
+  if (st != SPECDEC_OK) return st;
+  if (batch <= 0 || n <= 0 || n_heads < 0 || n_kv_heads < 0 || !is_float_type(dtype) || !is_float_type(out_dtype) ||
+      (!q && !k) || (q != nullptr) != (n_heads > 0) || (k != nullptr) != (n_kv_heads > 0) ||
+      (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr))
+    return SPECDEC_ERR_INVALID_ARG;
+  const int64_t wq = (int64_t)n_heads * rope->head_dim, wk = (int64_t)n_kv_heads * rope->head_dim;
+  if ((q && (ld_q < wq || ld_qo < wq)) || (k && (ld_k < wk || ld_ko < wk))) return SPECDEC_ERR_INVALID_ARG;
+  if (!rope_fits(batch, n, false) || wq + wk > 1 << 24) return SPECDEC_ERR_SHAPE;
+  const int64_t in = elem_bytes(dtype), out = elem_bytes(out_dtype), rows = (int64_t)batch * n;
+  struct Rows {
+    const void* at;
+    int64_t ld, bytes;
+  };
+  const Rows ins[2] = {{q, in * ld_q, in * wq}, {k, in * ld_k, in * wk}};
+  const Rows outs[2] = {{q_out, out * ld_qo, out * wq}, {k_out, out * ld_ko, out * wk}};
+  auto overlap = [&](const Rows& x, const Rows& y) {
+    return x.at && y.at && rows_overlap(x.at, x.ld, x.bytes, y.at, y.ld, y.bytes, rows);
+  };
+  for (int i = 0; i < 2; ++i)
+    for (int o = 0; o < 2; ++o)
+      if (!(i == o && ins[i].at == outs[o].at && ins[i].ld == outs[o].ld && dtype == out_dtype) &&
+          overlap(ins[i], outs[o]))
+        return SPECDEC_ERR_INVALID_ARG;
+  if (overlap(outs[0], outs[1])) return SPECDEC_ERR_INVALID_ARG;
+  RopeArgs a = rope_args(rope, n, n_heads, n_kv_heads, q, ld_q, k, ld_k, positions, offset, q_out, ld_qo);
+  a.k_out = k_out;
+  a.ld_ko = ld_ko;
+  return hip_status(launch_rope(a, rope->head_dim, batch, dtype == SPECDEC_F32, out_dtype == SPECDEC_F32, false,
+                                (hipStream_t)stream));
+}
+
+specdec_status specdec_rope_append(specdec_kv* kv, int32_t layer, const specdec_rope* rope, int32_t n, int32_t n_heads,
+                                   int32_t dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                                   const void* v, int64_t ld_v, const int32_t* positions, int64_t offset,
+                                   int32_t out_dtype, void* q_out, void* stream) {
+  const specdec_status st = check_rope(rope);
+  if (st != SPECDEC_OK) return st;
+  if (!kv || !kv->data || !kv->state || layer < 0 || layer >= kv->n_layers || n <= 0 || n_heads <= 0 ||
+      !is_float_type(dtype) || !is_float_type(out_dtype) || !q || !k || !v || !q_out)
+    return SPECDEC_ERR_INVALID_ARG;
+  if (!is_fp8(kv)) return SPECDEC_ERR_UNSUPPORTED;
+  const int64_t wq = (int64_t)n_heads * rope->head_dim, wk = (int64_t)kv->n_kv_heads * rope->head_dim;
+  if (rope->head_dim != kv->head_dim || n_heads % kv->n_kv_heads || !ring_holds(kv, n) ||
+      !rope_fits(kv->batch, n, true) || wq > 1 << 24)
+    return SPECDEC_ERR_SHAPE;
+  if (ld_q < wq || ld_k < wk || ld_v < wk) return SPECDEC_ERR_INVALID_ARG;
+  const int64_t in = elem_bytes(dtype), out = elem_bytes(out_dtype), rows = (int64_t)kv->batch * n;
+  const bool in_place = q_out == q && ld_q == wq && dtype == out_dtype;
+  if ((!in_place && rows_overlap(q, in * ld_q, in * wq, q_out, out * wq, out * wq, rows)) ||
+      rows_overlap(k, in * ld_k, in * wk, q_out, out * wq, out * wq, rows) ||
+      rows_overlap(v, in * ld_v, in * wk, q_out, out * wq, out * wq, rows))
+    return SPECDEC_ERR_INVALID_ARG;
+  if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  RopeArgs a = rope_args(rope, n, n_heads, kv->n_kv_heads, q, ld_q, k, ld_k, positions, offset, q_out, wq);
+  a.v = v;
+  a.ld_v = ld_v;
+  a.f8 = kv8_of(kv);
+  a.layer = layer;
+  a.pos_limit = kv->capacity;
+  a.status = kv_status(kv);
+  return hip_status(launch_rope(a, kv->head_dim, kv->batch, dtype == SPECDEC_F32, out_dtype == SPECDEC_F32, true,
+                                (hipStream_t)stream));
+}
+
 specdec_status specdec_kv_write_context(specdec_kv* kv, int32_t layer, int32_t b, int32_t pos0, int32_t n,
                                         const void* k, const void* v, void* stream) {
   if (!kv || !kv->data || !k || !v || layer < 0 || layer >= kv->n_layers || b < 0 || b >= kv->batch || pos0 < 0 ||
@@ -1055,18 +1194,6 @@ specdec_status check_accept(int32_t batch, int32_t gamma, int32_t vocab, int32_t
   return SPECDEC_OK;
 }
 
-// Whether n rows of `width` floats at a (stride ld_a) and as many at b may share
-// memory: by their extents, but for rows of one stride that lie between each
-// other's (two slots of one buffer).
-bool rows_overlap(const float* a, int64_t ld_a, const float* b, int64_t ld_b, int64_t n, int64_t width) {
-  const intptr_t a0 = (intptr_t)a, b0 = (intptr_t)b;
-  const intptr_t a1 = a0 + 4 * ((n - 1) * ld_a + width), b1 = b0 + 4 * ((n - 1) * ld_b + width);
-  if (b0 >= a1 || a0 >= b1) return false;
-  if (ld_a != ld_b) return true;
-  const intptr_t period = 4 * ld_a, at = ((b0 - a0) % period + period) % period;
-  return at < 4 * width || at + 4 * width > period;
-}
-
 specdec_status check_rules(int32_t batch, int32_t rows, int32_t vocab) {
   if (batch <= 0 || rows <= 0 || vocab <= 0) return SPECDEC_ERR_INVALID_ARG;
   if (vocab > kRulesMaxVocab || (int64_t)batch * rows > 65535) return SPECDEC_ERR_UNSUPPORTED;
@@ -1199,7 +1326,9 @@ specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab,
       !workspace || (uintptr_t)workspace % kAlign || workspace_bytes < rules_scratch_bytes(batch * rows, vocab))
     return SPECDEC_ERR_INVALID_ARG;
   // (the draw reads logits again after other workgroups have stored probabilities)
-  if (probs && rows_overlap(logits, ld, probs, ld_probs, (int64_t)batch * rows, vocab)) return SPECDEC_ERR_INVALID_ARG;
+  if (probs && rows_overlap(logits, 4 * ld, 4 * (int64_t)vocab, probs, 4 * ld_probs, 4 * (int64_t)vocab,
+                            (int64_t)batch * rows))
+    return SPECDEC_ERR_INVALID_ARG;
   RulesArgs a{};
   a.B = batch;
   a.rows = rows;

@@ -381,6 +381,32 @@ struct RulesArgs {
 };
 hipError_t launch_rules(const RulesArgs& a, hipStream_t s);
 
+// Norm and rotation of queries and keys (rope.hip).
+struct RopeArgs {
+  const void* q;              // row r of q, k, v at r * ld elements
+  const void* k;
+  const void* v;              // (a cache's launches)
+  int64_t ld_q, ld_k, ld_v;
+  void* q_out;
+  void* k_out;                // (launches without a cache)
+  int64_t ld_qo, ld_ko;
+  int n, n_heads, n_kv_heads; // rows a sequence
+  const void* q_gain;         // [head_dim], or null: not normalised
+  const void* k_gain;
+  int gain_bf16;
+  float eps;
+  int rotary, interleaved;
+  const int32_t* positions;   // [batch * n], or null: len[b] + i (a cache), i
+  int64_t offset;             // added to every position
+  Kv8Layout f8;
+  int layer, pos_limit;
+  int32_t* status;
+  int rows, groups, per, chunks;  // (set by launch_rope: all rows, groups of rows of a sequence, units a workgroup, workgroups a group)
+  double turns[SPECDEC_ROPE_MAX_PAIRS];  // of a pair, a position
+};
+bool rope_fits(int batch, int n, bool cache);
+hipError_t launch_rope(RopeArgs a, int head_dim, int batch, bool in_f32, bool out_f32, bool cache, hipStream_t s);
+
 // Streaming-read ceiling probe (stream.hip): reads bytes / 1024 KB-chunks of buf.
 hipError_t launch_stream_read(const void* buf, size_t bytes, uint32_t* sink, hipStream_t s);
 

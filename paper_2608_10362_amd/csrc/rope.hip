@@ -1,0 +1,292 @@
+// Norm and position rotation of queries and keys, head by head, in one pass; for an FP8
+// cache the rotated keys and the values go to its ring in that pass too.
+//
+//   y = gain x / sqrt(mean(x^2) + eps)            (per row and head; optional)
+//   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position freq_j
+//
+// for the pairs j < rotary / 2 of a head: dims (j, j + rotary / 2) or (2j, 2j + 1).
+//
+// Every element is read once and written once: the bytes are the bound.  A lane holds 8
+// dims of a row's head, 16 bytes of bf16; the half that a pair's other dim lies in comes
+// from the lane rotary / 16 further.  The angles depend on the row alone: a workgroup takes
+// 8 rows and some heads, computes the rows' cosines and sines once (the angle in turns in
+// 64 bits, where a far position keeps its fraction, the functions in 32) and keeps them in
+// LDS.  Squares are summed in 64 bits: no float32 input overflows or vanishes there.
+//
+// The 8 rows are 8 positions of one sequence from a multiple of 8 on: a lane then holds a
+// whole piece of V's operand order (8 positions of a dim, 16 bytes), turned in registers,
+// and K's pieces of neighbouring positions leave from one CU.
+#include <algorithm>
+
+#include "device_common.h"
+#include "fp8.h"
+#include "internal.h"
+
+namespace specdec {
+
+namespace {
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopeRows = 8;
+
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const f32x4 a = *(const f32x4_a4*)p, b = *(const f32x4_a4*)(p + 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = a[e];
+    x[4 + e] = b[e];
+  }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+  const u32x4 a = *(const u32x4_a2*)p;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(a[e] << 16);
+    x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+  }
+}
+// (nearest even, by the conversion instruction)
+__device__ __forceinline__ u32x4 to_bf16x8(const float (&x)[8]) {
+  u32x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    o[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * e], x[2 * e + 1]}, bf16x2));
+  return o;
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *(f32x4_a4*)p = f32x4{x[0], x[1], x[2], x[3]};
+  *(f32x4_a4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) { *(u32x4_a2*)p = to_bf16x8(x); }
+
+// 8 dims of a value row as bf16.
+__device__ __forceinline__ u32x4 bf16_row(const float* p) {
+  float x[8];
+  load8(p, x);
+  return to_bf16x8(x);
+}
+__device__ __forceinline__ u32x4 bf16_row(const uint16_t* p) { return *(const u32x4_a2*)p; }
+
+// Sum over the LPH lanes of a head.
+template <int LPH>
+__device__ __forceinline__ double head_sum(double v) {
+#pragma unroll
+  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// 1 / sqrt(m) in 64 bits: the instruction's 2^-23 squared by one step.
+__device__ __forceinline__ double inv_sqrt(double m) {
+  const double y = __builtin_amdgcn_rsq(m);
+  return isinf(m) ? 0.0 : y * (1.5 - 0.5 * m * y * y);
+}
+
+// Workgroup: kRopeRows rows (CACHE: positions of a sequence from a multiple of 8 on, those of
+// the call's), and `per` of the units of HPW heads: Q|K together, then V's.
+template <int HD, typename TI, typename TO, bool CACHE>
+__global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
+  constexpr int LPH = HD / 8, HPW = kWave / LPH, NW = kRopeThreads / kWave;
+  __shared__ alignas(16) float cs[2][kRopeRows][HD / 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunk = blockIdx.x % a.chunks, grp = blockIdx.x / a.chunks;
+  int r0, T, first = 0, at0 = 0, b = 0;  // first row; rows; the first row's place among the 8, its position
+  bool stored = true;
+  if constexpr (CACHE) {
+    b = grp / a.groups;
+    const int len = a.f8.len[b];
+    const int lo = max(len, (len >> 3) * 8 + (grp - b * a.groups) * 8), hi = min((lo & ~7) + 8, len + a.n);
+    T = hi - lo;
+    if (T <= 0) return;  // (workgroup-uniform)
+    r0 = b * a.n + lo - len;
+    first = lo & 7;
+    at0 = lo;
+    stored = lo >= 0 && hi <= a.pos_limit;
+    if (!stored && threadIdx.x == 0) set_status(a.status, kStatusKvCapacity);  // (the host's bound was wrong)
+  } else {
+    r0 = grp * kRopeRows;
+    T = min(kRopeRows, a.rows - r0);
+  }
+  const int rot = a.rotary, half = rot >> 1;
+  for (int e = threadIdx.x; e < T * half; e += kRopeThreads) {
+    const int t = e / half, j = e - t * half;
+    const int64_t base = a.positions ? a.positions[r0 + t] : CACHE ? at0 + t : (r0 + t) % a.n;
+    const double turns = (double)(base + a.offset) * a.turns[j];
+    float s, c;
+    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+    cs[0][t][j] = c;
+    cs[1][t][j] = s;
+  }
+  const int H = a.n_heads, G = a.n_kv_heads, n_qk = (H + G + HPW - 1) / HPW, n_v = CACHE ? (G + HPW - 1) / HPW : 0;
+  const int u0 = chunk * a.per, u1 = min(u0 + a.per, n_qk + n_v);
+  const int hl = lane / LPH, l = lane % LPH, d0 = 8 * l;
+  const int window = CACHE ? a.f8.ring.capacity : 0;
+  float gq[8], gk[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f;
+  if (a.q_gain) {
+    if (a.gain_bf16) load8((const uint16_t*)a.q_gain + d0, gq);
+    else load8((const float*)a.q_gain + d0, gq);
+  }
+  if (a.k_gain) {
+    if (a.gain_bf16) load8((const uint16_t*)a.k_gain + d0, gk);
+    else load8((const float*)a.k_gain + d0, gk);
+  }
+  __syncthreads();
+
+  const int n_qk_here = max(0, min(u1, n_qk) - u0) * T;
+#pragma unroll 2
+  for (int i = wave; i < n_qk_here; i += NW) {
+    const int u = i / T, t = i - u * T, head = (u0 + u) * HPW + hl, row = r0 + t;
+    const bool is_q = head < H, valid = head < H + G;
+    const TI* src = is_q ? (const TI*)a.q + (int64_t)row * a.ld_q + (int64_t)head * HD
+                         : (const TI*)a.k + (int64_t)row * a.ld_k + (int64_t)(head - H) * HD;
+    float x[8];
+    if (valid) load8(src + d0, x);
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    if (a.q_gain || a.k_gain) {
+      double m = 0.0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
+      const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
+      if (is_q ? a.q_gain != nullptr : a.k_gain != nullptr) {
+        if (rs > 1e-30 && rs < 1e30) {
+          const float f = (float)rs;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * f * (is_q ? gq[e] : gk[e]);
+        } else {  // (a factor that float32 would not hold)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * rs) * (is_q ? gq[e] : gk[e]);
+        }
+      }
+    }
+    if (a.interleaved) {
+      if (d0 < rot) {
+        const f32x4 c = *(const f32x4*)&cs[0][t][d0 / 2], s = *(const f32x4*)&cs[1][t][d0 / 2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = x[2 * e], r = x[2 * e + 1];
+          x[2 * e] = p * c[e] - r * s[e];
+          x[2 * e + 1] = r * c[e] + p * s[e];
+        }
+      }
+    } else if (rot) {
+      const int far = rot / 16;  // lanes of a half
+      const bool low = l < far, in = l < 2 * far;
+      const int from = lane + (in ? (low ? far : -far) : 0), j = in ? (low ? l : l - far) * 8 : 0;
+      float c[8], s[8];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f32x4 cv = *(const f32x4*)&cs[0][t][j + 4 * k], sv = *(const f32x4*)&cs[1][t][j + 4 * k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          c[4 * k + e] = cv[e];
+          s[4 * k + e] = low ? -sv[e] : sv[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = __shfl(x[e], from, kWave);
+        if (in) x[e] = x[e] * c[e] + y * s[e];
+      }
+    }
+    if (!valid) continue;
+    if (is_q) {
+      store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x);
+    } else if constexpr (CACHE) {
+      if (stored) {
+        uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head - H);
+        *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
+      }
+    } else {
+      store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)(head - H) * HD + d0, x);
+    }
+  }
+
+  if constexpr (CACHE) {
+    if (!stored) return;
+    const int p0 = (at0 & ~7) % window;
+    for (int u = max(u0, n_qk) + wave; u < u1; u += NW) {
+      const int g = (u - n_qk) * HPW + hl;
+      if (g >= G) continue;
+      const TI* src = (const TI*)a.v + (int64_t)r0 * a.ld_v + (int64_t)g * HD + d0;
+      uint16_t* dst = k_block<uint16_t>(a.f8.ring, a.layer, b, g) + KvIndex<uint16_t>::v(p0, d0, HD, window);
+      if (T == kRopeRows) {
+        u32x4 x[kRopeRows];
+#pragma unroll
+        for (int t = 0; t < kRopeRows; ++t) x[t] = bf16_row(src + (int64_t)t * a.ld_v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          u32x4 y;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)  // (the e-th 16 bits of two rows)
+            y[w] = __builtin_amdgcn_perm(x[2 * w + 1][e >> 1], x[2 * w][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+          *(u32x4*)(dst + 8 * e) = y;
+        }
+      } else {
+        for (int t = 0; t < T; ++t) {
+          const u32x4 x = bf16_row(src + (int64_t)t * a.ld_v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dst[8 * e + first + t] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+        }
+      }
+    }
+  }
+}
+
+template <int HD>
+hipError_t launch_hd(const RopeArgs& a, bool in_f32, bool out_f32, bool cache, dim3 grid, hipStream_t s) {
+#define SD_ROPE(TI, TO)                                                                                     \
+  if (cache) hipLaunchKernelGGL((rope_kernel<HD, TI, TO, true>), grid, dim3(kRopeThreads), 0, s, a);        \
+  else hipLaunchKernelGGL((rope_kernel<HD, TI, TO, false>), grid, dim3(kRopeThreads), 0, s, a);
+  if (in_f32) {
+    if (out_f32) { SD_ROPE(float, float) }
+    else { SD_ROPE(float, uint16_t) }
+  } else {
+    if (out_f32) { SD_ROPE(uint16_t, float) }
+    else { SD_ROPE(uint16_t, uint16_t) }
+  }
+#undef SD_ROPE
+  return hipGetLastError();
+}
+
+// Groups of rows of a launch.
+int64_t groups_of(int batch, int n, bool cache) {
+  return cache ? (int64_t)batch * ((n + kRopeRows - 2) / kRopeRows + 1)
+               : ((int64_t)batch * n + kRopeRows - 1) / kRopeRows;
+}
+
+}  // namespace
+
+// (a grid of at most 2^24 workgroups of 256 threads, one at least for a group of rows)
+bool rope_fits(int batch, int n, bool cache) {
+  return (int64_t)batch * n <= 0x7fffffff && groups_of(batch, n, cache) < 1 << 22;
+}
+
+hipError_t launch_rope(RopeArgs a, int head_dim, int batch, bool in_f32, bool out_f32, bool cache, hipStream_t s) {
+  const int hpw = 512 / head_dim;
+  const int units = (a.n_heads + a.n_kv_heads + hpw - 1) / hpw + (cache ? (a.n_kv_heads + hpw - 1) / hpw : 0);
+  const int64_t groups = groups_of(batch, a.n, cache);
+  a.rows = batch * a.n;
+  a.groups = (int)(groups / batch);
+  // Heads are split over workgroups until the card is full, each wave with a row's unit at least.
+  const int64_t slots = 8L * device_compute_units();
+  const int rows = std::min(a.n * (cache ? 1 : batch), kRopeRows);
+  const int64_t least = (kRopeThreads / kWave + rows - 1) / rows;
+  a.per = (int)std::min<int64_t>(units, std::max<int64_t>({least, (units * groups + slots - 1) / slots, (int64_t)1}));
+  a.chunks = (units + a.per - 1) / a.per;
+  if (groups * a.chunks >= 1 << 24) {  // (few heads a workgroup: as many as the grid takes)
+    a.per = units;
+    a.chunks = 1;
+  }
+  const dim3 grid((unsigned)(groups * a.chunks));
+  switch (head_dim) {
+    case 32: return launch_hd<32>(a, in_f32, out_f32, cache, grid, s);
+    case 64: return launch_hd<64>(a, in_f32, out_f32, cache, grid, s);
+    case 128: return launch_hd<128>(a, in_f32, out_f32, cache, grid, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace specdec
