@@ -316,6 +316,32 @@ SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer
                                              const float* q, float* out, void* workspace, size_t workspace_bytes,
                                              void* stream);
 
+/* The same for a batch whose sequences begin with the same text, held once: `prefix`
+ * is another FP8 cache of the same kv heads and head_dim, its committed sequence
+ * prefix_b the keys and values of what all share (P = its length, read on the
+ * device; 0: nothing), `kv` the sequences' own text behind it.  Row i of sequence b
+ * sees all P keys of the prefix and keys 0 .. len[b]+i of its own cache: it is the
+ * row P + len[b] + i of the whole text (positions, and so K's and q's rotation, are
+ * the caller's: specdec_rope_append with an offset of P).  The prefix's codes are
+ * read once for many rows instead of once a sequence.  The prefix is only read:
+ * any number of calls may use one at once, on any streams.
+ * dtype: the type of q and out (SPECDEC_F32, as specdec_attention, or SPECDEC_BF16:
+ * products of one part, twice the speed where there are many rows; out rounded
+ * once).  Everything else as for specdec_attention.
+ * workspace: specdec_attention_shared_workspace_bytes bytes (0 for arguments the
+ * call rejects).
+ * Graph capture: the prefix's part is sized from prefix->len_upper.
+ * Errors: as specdec_attention for kv; INVALID_ARG (prefix_b, layer past either
+ * cache's); SHAPE (other kv heads or head_dim; batch * n rows past what
+ * specdec_kv_init_fp8 names for the rows of one sequence, or 2^20 query rows of a
+ * kv head); UNSUPPORTED (a prefix that is no FP8 cache). */
+SPECDEC_API size_t specdec_attention_shared_workspace_bytes(const specdec_kv* prefix, const specdec_kv* kv,
+                                                            int32_t n_heads, int32_t n, int32_t dtype);
+SPECDEC_API specdec_status specdec_attention_shared(const specdec_kv* prefix, int32_t prefix_b, const specdec_kv* kv,
+                                                    int32_t layer, int32_t n_heads, int32_t n, int32_t dtype,
+                                                    const void* q, void* out, void* workspace, size_t workspace_bytes,
+                                                    void* stream);
+
 /* The norm and the position rotation of a model's queries and keys, head by head
  * (host POD; specdec_rope_init fills it, the caller keeps it):
  *   y = gain * x / sqrt(mean(x^2) + eps) over a head's head_dim entries (queries

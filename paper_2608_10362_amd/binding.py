@@ -146,6 +146,12 @@ _SIGS = {
     "specdec_kv_append": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                                          ctypes.c_void_p, ctypes.c_void_p]),
     "specdec_kv_advance": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.c_void_p]),
+    "specdec_attention_shared_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(KV), ctypes.POINTER(KV),
+                                                                   ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "specdec_attention_shared": (ctypes.c_int, [ctypes.POINTER(KV), ctypes.c_int32, ctypes.POINTER(KV),
+                                                ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                                ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                                ctypes.c_void_p]),
     "specdec_rope_init": (ctypes.c_int, [ctypes.POINTER(RopeDesc), ctypes.c_int32, ctypes.c_int32, ctypes.c_double,
                                          ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
                                          ctypes.c_float]),
@@ -739,6 +745,46 @@ def specdec_attention(kv: KVCache, layer: int, q, out, workspace=None, stream=No
     _same_device(workspace, "workspace", q)
     _check(lib().specdec_attention(ctypes.byref(kv.kv), layer, n_heads, n, q.data_ptr(), out.data_ptr(),
                                    workspace.data_ptr(), workspace.numel(), _stream(stream)), "specdec_attention")
+
+
+def shared_attention_workspace(prefix: KVCache, kv: KVCache, n_heads: int, n: int, dtype=None):
+    """A device buffer large enough for specdec_attention_shared's workspace (dtype: of its
+    queries, float32 if not given)."""
+    import torch
+    kind = SPECDEC_F32 if dtype is None else _float_type(dtype, "dtype")
+    nbytes = lib().specdec_attention_shared_workspace_bytes(ctypes.byref(prefix.kv), ctypes.byref(kv.kv), n_heads, n,
+                                                            kind)
+    if nbytes == 0:
+        raise ValueError("specdec_attention_shared does not support these caches or sizes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=kv.data.device)
+
+
+def specdec_attention_shared(prefix: KVCache, kv: KVCache, layer: int, q, out, workspace=None, prefix_b: int = 0,
+                             stream=None):
+    """q, out: device float32 or bfloat16 [batch, n, n_heads, head_dim] (out may be q); `prefix`'s sequence
+    `prefix_b` is what every sequence of `kv` begins with.
+    `workspace` (from shared_attention_workspace) is allocated per call, on the call's stream,
+    when not given.
+    Calls on one `kv` must be ordered on one stream; `prefix` is only read."""
+    import torch
+    if q.dim() != 4 or q.shape[0] != kv.batch or q.shape[3] != kv.kv.head_dim or out.shape != q.shape:
+        raise ValueError("q, out: expected [batch, n, n_heads, head_dim]")
+    kind = _float_type(q.dtype, "q")
+    for name, t in (("q", q), ("out", out)):
+        _on_current(t, name, q.dtype)
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
+    _same_device(kv.data, "kv", q)
+    _same_device(prefix.data, "prefix", q)
+    n, n_heads = q.shape[1], q.shape[2]
+    if workspace is None:
+        with _memory_of(stream):
+            workspace = shared_attention_workspace(prefix, kv, n_heads, n, q.dtype)
+    _dev(workspace, "workspace", torch.uint8, 1)
+    _same_device(workspace, "workspace", q)
+    _check(lib().specdec_attention_shared(ctypes.byref(prefix.kv), prefix_b, ctypes.byref(kv.kv), layer, n_heads, n,
+                                          kind, q.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                          _stream(stream)), "specdec_attention_shared")
 
 
 def specdec_draft_step(draft: Model, kv: KVCache, gamma: int, slot: int, temperature: float, seed: int, step: int,

@@ -334,6 +334,49 @@ RopeArgs rope_args(const specdec_rope* r, int n, int n_heads, int n_kv_heads, co
   return a;
 }
 
+// The launch of specdec_attention (its workspace: outputs of the parts, then their maxima and sums).
+AttnArgs attention_args(const specdec_kv* kv, int layer, int n_heads, int n, const float* q, float* out,
+                        void* workspace) {
+  AttnArgs a{};
+  a.M = kv->batch * n;
+  a.rps = n;
+  a.n_heads = n_heads;
+  a.n_kv_heads = kv->n_kv_heads;
+  a.head_dim = kv->head_dim;
+  a.qr = const_cast<float*>(q);
+  a.kv = kv_layout(kv);
+  a.layer = layer;
+  a.max_ctx = (int)kv->len_upper + n;
+  a.n_split = attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->head_dim, kv->capacity);
+  a.o_part = (float*)workspace;
+  a.ml_part = (float*)((char*)workspace + align_up((size_t)a.M * n_heads * a.n_split * kv->head_dim * 4));
+  a.o = out;
+  a.status = kv_status(kv);
+  a.f8 = kv8_of(kv);
+  return a;
+}
+
+specdec_status check_shared(const specdec_kv* prefix, const specdec_kv* kv, int n_heads, int n, int dtype) {
+  if (!prefix || !prefix->data || !prefix->state || !is_float_type(dtype)) return SPECDEC_ERR_INVALID_ARG;
+  const specdec_status st = check_attention(kv, n_heads, n);
+  if (st != SPECDEC_OK) return st;
+  if (!is_fp8(prefix)) return SPECDEC_ERR_UNSUPPORTED;
+  if (prefix->n_kv_heads != kv->n_kv_heads || prefix->head_dim != kv->head_dim ||
+      !attention_shared_fits((int64_t)kv->batch * n, n_heads, kv->n_kv_heads))
+    return SPECDEC_ERR_SHAPE;
+  return SPECDEC_OK;
+}
+
+// Parts of a (row, head) over a prefix of any length its cache holds, and what they take.
+int shared_parts(const specdec_kv* prefix, const specdec_kv* kv, int n_heads, int n, int dtype) {
+  return attention_shared_parts(kv->batch * n, n_heads, kv->n_kv_heads, kv->head_dim, prefix->capacity,
+                                dtype == SPECDEC_BF16);
+}
+size_t shared_prefix_bytes(const specdec_kv* prefix, const specdec_kv* kv, int n_heads, int n, int dtype) {
+  const size_t slots = (size_t)kv->batch * n * n_heads * shared_parts(prefix, kv, n_heads, n, dtype);
+  return align_up(slots * kv->head_dim * 4) + align_up(slots * 2 * 4);
+}
+
 // Runs GEMM `g` over the rows [0, M) in launches of at most gemm_launch_rows rows
 // (the kernel family is chosen by the whole pass's M, so every launch of a pass
 // writes the same number of ss partials).
@@ -835,24 +878,42 @@ specdec_status specdec_attention(const specdec_kv* kv, int32_t layer, int32_t n_
   if (out != q && (uintptr_t)out < (uintptr_t)q + bytes && (uintptr_t)q < (uintptr_t)out + bytes)
     return SPECDEC_ERR_INVALID_ARG;
   if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
-  AttnArgs a{};
-  a.M = kv->batch * n;
-  a.rps = n;
-  a.n_heads = n_heads;
-  a.n_kv_heads = kv->n_kv_heads;
-  a.head_dim = kv->head_dim;
-  a.qr = const_cast<float*>(q);
-  a.kv = kv_layout(kv);
-  a.layer = layer;
-  a.max_ctx = (int)kv->len_upper + n;
-  a.n_split = attention8_parts(n, kv->batch, n_heads, kv->n_kv_heads, kv->head_dim, kv->capacity);
-  a.o_part = (float*)workspace;
-  a.ml_part = (float*)((char*)workspace + align_up((size_t)a.M * n_heads * a.n_split * kv->head_dim * 4));
-  a.o = out;
-  a.status = kv_status(kv);
-  a.f8 = kv8_of(kv);
+  const AttnArgs a = attention_args(kv, layer, n_heads, n, q, out, workspace);
   Timed t(SPECDEC_KERNEL_ATTENTION, (hipStream_t)stream);
   return hip_status(launch_attention8(a, (hipStream_t)stream));
+}
+
+size_t specdec_attention_shared_workspace_bytes(const specdec_kv* prefix, const specdec_kv* kv, int32_t n_heads,
+                                                int32_t n, int32_t dtype) {
+  if (check_shared(prefix, kv, n_heads, n, dtype) != SPECDEC_OK) return 0;
+  return shared_prefix_bytes(prefix, kv, n_heads, n, dtype) + specdec_attention_workspace_bytes(kv, n_heads, n);
+}
+
+specdec_status specdec_attention_shared(const specdec_kv* prefix, int32_t prefix_b, const specdec_kv* kv, int32_t layer,
+                                        int32_t n_heads, int32_t n, int32_t dtype, const void* q, void* out,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  const specdec_status st = check_shared(prefix, kv, n_heads, n, dtype);
+  if (st != SPECDEC_OK) return st;
+  if (!q || !out || layer < 0 || layer >= kv->n_layers || layer >= prefix->n_layers || prefix_b < 0 ||
+      prefix_b >= prefix->batch || !workspace || (uintptr_t)workspace % kAlign ||
+      workspace_bytes < specdec_attention_shared_workspace_bytes(prefix, kv, n_heads, n, dtype))
+    return SPECDEC_ERR_INVALID_ARG;
+  const size_t rows = (size_t)kv->batch * n, bytes = rows * n_heads * kv->head_dim * elem_bytes(dtype);
+  if (out != q && (uintptr_t)out < (uintptr_t)q + bytes && (uintptr_t)q < (uintptr_t)out + bytes)
+    return SPECDEC_ERR_INVALID_ARG;
+  if (kv->len_upper + n > kv->capacity || prefix->len_upper > prefix->capacity) return SPECDEC_ERR_KV_CAPACITY;
+  SharedAttn sh{};
+  sh.prefix = kv8_of(prefix);
+  sh.b = prefix_b;
+  sh.max_len = (int)prefix->len_upper;
+  sh.bf16 = dtype == SPECDEC_BF16;
+  sh.parts = shared_parts(prefix, kv, n_heads, n, dtype);
+  sh.o = (float*)workspace;
+  sh.ml = (float*)((char*)workspace + align_up(rows * n_heads * sh.parts * kv->head_dim * 4));
+  const AttnArgs a = attention_args(kv, layer, n_heads, n, (const float*)q, (float*)out,
+                                    (char*)workspace + shared_prefix_bytes(prefix, kv, n_heads, n, dtype));
+  Timed t(SPECDEC_KERNEL_ATTENTION, (hipStream_t)stream);
+  return hip_status(launch_attention_shared(a, sh, (hipStream_t)stream));
 }
 
 specdec_status specdec_rope_init(specdec_rope* rope, int32_t head_dim, int32_t rotary_dim, double base,

@@ -275,6 +275,14 @@ struct AttnArgs {
   Kv8Layout f8;
   int c0;
 };
+// The parts that a pass over a shared prefix leaves of every (row, head), and what tells how many: the
+// prefix's length on the device, of which `max_len` at most counts, `keys` to a part.
+struct SharedParts {
+  const float* o;        // [rows, h, stride, hd]
+  const float* ml;       // [rows, h, stride, 2]
+  const int32_t* len;
+  int max_len, keys, stride;
+};
 constexpr uint32_t kNextWeightsPerBlock = 48u << 10;
 constexpr int kMaxParts = 64;  // parts of one head that the one-round in-kernel and the long-context combine take (one per lane)
 // Counter words a model workspace holds for the one-round in-kernel combine.
@@ -290,6 +298,19 @@ int attention8_parts(int rps, int batch, int n_heads, int n_kv_heads, int head_d
 bool attention8_fits(int rps, int batch, int n_heads, int n_kv_heads);
 hipError_t launch_attention8(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
+// Attention over a shared prefix (attention_shared.hip): `own` as for launch_attention8, but for the type
+// of its queries and results.
+struct SharedAttn {
+  Kv8Layout prefix;
+  int b, max_len;  // its sequence that holds the prefix, the host's bound of its length
+  bool bf16;       // queries and results
+  float* o;        // its parts (see SharedParts), `parts` of a (row, head)
+  float* ml;
+  int parts;
+};
+bool attention_shared_fits(int64_t rows, int n_heads, int n_kv_heads);
+int attention_shared_parts(int rows, int n_heads, int n_kv_heads, int head_dim, int max_len, bool bf16);
+hipError_t launch_attention_shared(const AttnArgs& own, const SharedAttn& sh, hipStream_t s);
 
 // ------------------------------------------------------------------ sampling / bookkeeping
 struct DraftFinishArgs {
