@@ -154,18 +154,20 @@ def test_without_a_prefix_it_is_the_plain_attention(n, H):
     hd, G, lens = 128, 2, [500, 0, 64]
     prefix, _, _ = _prefix(rng, hd, G, 0, n_layers=1)
     kv = _cache(_shape(hd, H, G, 1), 3, 640, 128)
-    _fill(kv, rng, lens, n, G, hd)
+    kvs = _fill(kv, rng, lens, n, G, hd)
     q = _queries(rng, (3, n, H, hd), "f32")
+    none = np.zeros((0, G, hd))
     plain = torch.empty_like(q)
-    binding.specdec_attention(kv, 0, q, plain)
-    assert torch.equal(_attend(prefix, kv, q), plain)
+    binding.specdec_attention(kv, 0, q, plain)  # (sums of another order: both within the bound)
+    _check(plain, q, none, none, kvs, lens)
+    _check(_attend(prefix, kv, q), q, none, none, kvs, lens)
     # an empty prefix under a host bound of its whole capacity
     big = _cache(_shape(hd, G, G, 1), 2, 4096)
     big.set_state([0, 0], [[0, 1]] * 2, [1] * 2)
     big.kv.len_upper = 4096
     ws = binding.shared_attention_workspace(big, kv, H, n)
     ws.fill_(255)
-    assert torch.equal(_attend(big, kv, q, ws=ws), plain)
+    _check(_attend(big, kv, q, ws=ws), q, none, none, kvs, lens)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
