@@ -368,6 +368,354 @@ hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStre
   return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- many rows of 16-bit queries
+// One workgroup: 16 RT rows of a kv head and a range of keys, its waves every fourth chunk of
+// 32 or 64 (all rows each), merged at the end as attn8_kernel's are.  Queries of bf16 are one
+// part of their product, with K's codes as bf16 (exact); probabilities are one fp16 part
+// with V's codes as fp16 (exact), off by 2^-11 of each; the sums are taken of the rounded ones,
+// by a product with ones.  bf16 rows of the ring take two bf16 parts.
+//
+// What bounds it is the vector unit beside the matrix unit: a chunk's conversions, 64 of two
+// codes each for 32 keys of 128 dims, are shared by RT tiles; a score costs a maximum, a
+// multiply-add, an exponential and half a conversion.  The running maximum is raised only when
+// a score exceeds it by 2^kSlack (then exactly): no value crosses lanes in a chunk that
+// does not.
+constexpr float kSlack = 4.f, kWideLift = 11.f;  // (2^(kSlack + kWideLift) is fp16's; held down to 2^-25 in full)
+
+template <int HD, int RT, class X>
+__global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, int parts, int per, X x) {
+  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, SP = steps_of(HD), OS = HD + 4, NW = 4;
+  __shared__ float so[NW][16][OS];
+  __shared__ float sml[NW][16][2];
+  typedef uint16_t T;
+  int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, grp = lane >> 4;
+  const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, nq = rps * group, window = a.f8.ring.capacity;
+  const int b = blockIdx.z, u = blockIdx.y, part = blockIdx.x, tile = u / G, g = u - tile * G;
+  const float qscale = 1.44269504088896341f / sqrtf((float)HD), inv_group = 1.0f / (float)group;
+  int seq = b;
+  if constexpr (X::kPrefix) seq = x.b;
+  const int nb = __builtin_amdgcn_readfirstlane(chunks_of<chunk_of(HD)>(a, x, b)), k_lo = part * per;
+  if (k_lo >= nb) return;  // (workgroup-uniform)
+  const int k_hi = min(nb, k_lo + per);
+
+  bf16x8 qq[RT][KST];
+#pragma unroll
+  for (int q = 0; q < RT; ++q) {
+    const int qa = (tile * RT + q) * 16 + c16, qr = div_small(qa, inv_group);
+#pragma unroll
+    for (int s = 0; s < KST; ++s) {
+      const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (qa < nq) v = *(const u32x4_a2*)((const T*)a.qr + ((size_t)(b * rps + qr) * H + g * group + qa - qr * group) * HD + d);
+      qq[q][s] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  const int sealed = __builtin_amdgcn_readfirstlane(a.f8.len[seq]) / kF8Block * (kF8Block / kF8Sub / SP);
+  const int j_sealed = min(k_hi, sealed);
+  const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, seq, g), (uint32_t)j_sealed * SP * 2 * kF8Sub * HD);
+  const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, seq, g), (uint32_t)((j_sealed * SP + 1) & ~1) * 4);
+  u32x4 kc[SP][FS], vc[SP][FS];
+  float ks, vs;
+  auto load_k = [&](int j) {
+    const uint32_t at = (uint32_t)j * SP * 2 * kF8Sub * HD + lane * 16;
+#pragma unroll
+    for (int i = 0; i < SP * FS; ++i)
+      kc[i / FS][i % FS] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i / FS * 2 * kF8Sub * HD + i % FS * 1024, 0, 0));
+    ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP & ~1) * 4, 0, 0));
+  };
+  auto load_v = [&](int j) {
+    const uint32_t at = (uint32_t)j * SP * 2 * kF8Sub * HD + kF8Sub * HD + lane * 16;
+#pragma unroll
+    for (int i = 0; i < SP * FS; ++i)
+      vc[i / FS][i % FS] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i / FS * 2 * kF8Sub * HD + i % FS * 1024, 0, 0));
+    vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP | 1) * 4, 0, 0));
+  };
+  int j = k_lo + wave, jr = max(j, j + (sealed - j + NW - 1) / NW * NW);  // (jr: the first of the ring's)
+  load_k(j);
+  load_v(j);
+
+  floatx4 of[RT][DT], sums[RT];
+  float mx[RT];
+#pragma unroll
+  for (int q = 0; q < RT; ++q) {
+    mx[q] = kLeast;
+    sums[q] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) of[q][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  // Scores (unscaled) of tile q become probabilities times 2^kWideLift.
+  auto softmax = [&](int q, auto& p) {
+    constexpr int N = sizeof(p) / sizeof(float);
+    float m = fmaxf(p[0], p[1]);
+#pragma unroll
+    for (int e = 2; e < N; ++e) m = fmaxf(m, p[e]);
+    if (__any(__builtin_fmaf(m, qscale, -mx[q]) > kSlack)) {
+      const float mnew = fmaxf(mx[q], groups_max(m) * qscale);
+      const float alpha = __builtin_amdgcn_exp2f(mx[q] - mnew);
+      sums[q] *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) of[q][dt] *= alpha;
+      mx[q] = mnew;
+    }
+    const float off = kWideLift - mx[q];
+#pragma unroll
+    for (int e = 0; e < N; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], qscale, off));
+  };
+  f16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.f;
+
+  for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
+    float p[RT][8 * SP];
+#pragma unroll
+    for (int sp = 0; sp < SP; ++sp) {
+      floatx4 acc[RT][2];
+#pragma unroll
+      for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KST; ++s) {
+        bf16x8 kk[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 w = HD >= 64 ? kc[sp][t * (HD / 64) + s / 2] : kc[sp][0];
+          const int h = HD >= 64 ? s & 1 : t;
+          kk[t] = fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
+        }
+#pragma unroll
+        for (int q = 0; q < RT; ++q) {
+          acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[0], qq[q][s], acc[q][0], 0, 0, 0);
+          acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[1], qq[q][s], acc[q][1], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < RT; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
+    }
+    load_k(j + NW);
+    f16x8 pp[RT][SP];
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      softmax(q, p[q]);
+#pragma unroll
+      for (int sp = 0; sp < SP; ++sp) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[q][8 * sp + 2 * e], p[q][8 * sp + 2 * e + 1]}, f16x2));
+        pp[q][sp] = __builtin_bit_cast(f16x8, w);
+      }
+    }
+    const int ve = __builtin_amdgcn_readfirstlane((int)__float_as_uint(vs) >> 23) - 127;
+#pragma unroll
+    for (int sp = 0; sp < SP; ++sp)
+#pragma unroll
+      for (int q = 0; q < RT; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pp[q][sp], sums[q], 0, 0, 0);
+    if (ve >= -15 && ve <= 7) {  // (V's values are fp16's)
+#pragma unroll
+      for (int sp = 0; sp < SP; ++sp)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const f16x8 vv = fp8x8_to_f16(vc[sp][dt / 2][2 * (dt & 1)], vc[sp][dt / 2][2 * (dt & 1) + 1], vs);
+#pragma unroll
+          for (int q = 0; q < RT; ++q) of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], of[q][dt], 0, 0, 0);
+        }
+    } else {  // the codes' products, times the scale
+#pragma unroll
+      for (int sp = 0; sp < SP; ++sp)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const f16x8 vv = fp8x8_to_f16(vc[sp][dt / 2][2 * (dt & 1)], vc[sp][dt / 2][2 * (dt & 1) + 1], 1.0f);
+#pragma unroll
+          for (int q = 0; q < RT; ++q)
+            of[q][dt] += __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0) * vs;
+        }
+    }
+    load_v(j + NW);
+  }
+
+  if (jr < k_hi) {  // (wave-uniform) the ring's rows
+    int qpos[RT], vis = 0, lowest = 0x7fffffff;
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      const int qa = (tile * RT + q) * 16 + c16;
+      const RowDesc rd = row_of(a, x, b, qa < nq ? div_small(qa, inv_group) : 0);
+      qpos[q] = qa < nq && rd.valid ? rd.pos : -1;
+      if (qpos[q] >= 0) {
+        vis = max(vis, qpos[q] + 1);
+        lowest = min(lowest, qpos[q]);
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      vis = max(vis, __shfl_xor(vis, o, kWave));
+      lowest = min(lowest, __shfl_xor(lowest, o, kWave));
+    }
+    vis = __builtin_amdgcn_readfirstlane(vis);
+    lowest = __builtin_amdgcn_readfirstlane(lowest);
+    const uint16_t* ring = k_block<uint16_t>(a.f8.ring, a.layer, seq, g);
+    bf16x8 one;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) one[e] = (__bf16)1.f;
+#pragma unroll 1
+    for (; jr < k_hi; jr += NW)
+#pragma unroll 1
+      for (int sp = 0; sp < SP; ++sp) {
+        const int k0 = (jr * SP + sp) * kF8Sub, w0 = k0 % window;
+        if (k0 >= vis) break;
+        const bool diagonal = k0 + kF8Sub - 1 > lowest;
+        floatx4 acc[RT][2];
+#pragma unroll
+        for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KST; ++s) {
+          const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
+          bf16x8 kk[2];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            kk[t] = *(const bf16x8*)(ring + KvIndex<uint16_t>::k(w0 + 8 * (c16 >> 2) + 4 * t + (c16 & 3), d, HD, window));
+#pragma unroll
+          for (int q = 0; q < RT; ++q) {
+            acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[0], qq[q][s], acc[q][0], 0, 0, 0);
+            acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[1], qq[q][s], acc[q][1], 0, 0, 0);
+          }
+        }
+        float p[RT][8];
+        bf16x8 pp[RT][2];
+#pragma unroll
+        for (int q = 0; q < RT; ++q) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[q][e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
+          softmax(q, p[q]);
+          split_parts<2>(p[q], pp[q]);
+#pragma unroll
+          for (int k = 1; k >= 0; --k) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pp[q][k], sums[q], 0, 0, 0);
+        }
+        // (stale entries, NaN and infinities where some query does not see all rows: see attn8_kernel)
+        const int nvalid = vis - (k0 + 8 * grp);
+        bool odd = false;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          u32x4 v = *(const u32x4*)(ring + KvIndex<uint16_t>::v(w0 + 8 * grp, 16 * dt + c16, HD, window));
+          if (diagonal) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              if (2 * w >= nvalid) v[w] = 0u;
+              else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
+              const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
+              odd |= lo || up;
+              if (lo) v[w] &= 0xffff0000u;
+              if (up) v[w] &= 0xffffu;
+            }
+          }
+#pragma unroll
+          for (int k = 1; k >= 0; --k)
+#pragma unroll
+            for (int q = 0; q < RT; ++q)
+              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pp[q][k], of[q][dt], 0, 0, 0);
+        }
+        if (__any(odd)) {
+          for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
+            const uint16_t* vrow = ring + KvIndex<uint16_t>::v(w0 + i, 0, HD, window);
+#pragma unroll
+            for (int q = 0; q < RT; ++q) {
+              float pi = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) pi = (i & 7) == e ? p[q][e] : pi;
+              pi = __shfl(pi, 16 * (i >> 3) + c16, kWave);
+#pragma unroll
+              for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  const float v = bf16_bits_to_f32(vrow[(size_t)dt * kWave * 8 + (4 * grp + r) * 8]);
+                  if (k0 + i <= qpos[q] && !isfinite(v)) of[q][dt][r] += pi * v;
+                }
+            }
+          }
+        }
+      }
+  }
+
+  // The waves' results, tile by tile.
+#pragma unroll
+  for (int q = 0; q < RT; ++q) {
+    const int n_here = min(16, nq - (tile * RT + q) * 16);
+    if (n_here <= 0) break;
+    __syncthreads();
+    if (c16 < n_here) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *(floatx4*)&so[wave][c16][16 * dt + 4 * grp] = of[q][dt];
+      if (grp == 0) {
+        sml[wave][c16][0] = mx[q];
+        sml[wave][c16][1] = sums[q][0];
+      }
+    }
+    __syncthreads();
+    const int d = threadIdx.x % (HD / 4) * 4;
+    for (int i = threadIdx.x / (HD / 4); i < n_here; i += 64 * NW / (HD / 4)) {
+      float M = kLeast, L = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) M = fmaxf(M, sml[w][i][0]);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float e = __builtin_amdgcn_exp2f(sml[w][i][0] - M) * 0x1p-11f;  // (2^-kWideLift)
+        L += e * sml[w][i][1];
+        o += e * *(const f32x4*)&so[w][i][d];
+      }
+      const int qa = (tile * RT + q) * 16 + i, qr = div_small(qa, inv_group), head = g * group + qa - qr * group;
+      if constexpr (X::kPrefix) {
+        const size_t slot = ((size_t)(b * rps + qr) * H + head) * parts + part;
+        *(f32x4*)(a.o_part + slot * HD + d) = o;
+        if (d == 0) *(float2*)(a.ml_part + 2 * slot) = make_float2(M, L);
+      } else {
+        finish_row(a, x, b, qr, head, d, o, 1.0f, M, L);
+      }
+    }
+  }
+}
+
+// Rows of a kv head from which bf16 queries take it, and how the work is split: query tiles of
+// 16 RT rows, as many parts of the keys as fill the card twice.
+constexpr int kWideTiles = 2;
+bool is_wide(int nq) { return nq > 32; }
+Plan wide_plan(int rps, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
+  Plan p{};
+  const int nq = rps * (n_heads / n_kv_heads);
+  p.n_tiles = (nq + 16 * kWideTiles - 1) / (16 * kWideTiles);
+  const long nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim), units = (long)n_kv_heads * p.n_tiles;
+  const long slots = 2L * device_compute_units(), all = std::max(1L, slots / units);
+  const long per = std::max({(nb + all - 1) / all, (nb + kPartsMax8 - 1) / kPartsMax8, 4L});
+  p.per = (int)per;
+  p.nwg = (int)((nb + per - 1) / per);
+  p.parts = (int)std::min<long>({nb, all, (long)kPartsMax8});
+  return p;
+}
+
+template <class X>
+hipError_t launch_wide(const AttnArgs& a, const Plan& p, int B, const X& x, hipStream_t s) {
+  const dim3 grid(p.nwg, (unsigned)(a.n_kv_heads * p.n_tiles), B);
+#define SD_WIDE(HD) \
+  hipLaunchKernelGGL((wide_kernel<HD, kWideTiles, X>), grid, dim3(256), 0, s, a, p.n_tiles, p.parts, p.per, x)
+  switch (a.head_dim) {
+    case 32: SD_WIDE(32); break;
+    case 64: SD_WIDE(64); break;
+    case 128: SD_WIDE(128); break;
+    default: return hipErrorInvalidValue;
+  }
+#undef SD_WIDE
+  return hipGetLastError();
+}
+
+Plan prefix_plan(int rows, int n_heads, int n_kv_heads, int head_dim, int max_len, bool bf16) {
+  return bf16 && is_wide(rows * (n_heads / n_kv_heads)) ? wide_plan(rows, n_heads, n_kv_heads, head_dim, max_len)
+                                                        : plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len);
+}
+
 template <typename T>
 hipError_t launch_typed(AttnArgs own, const SharedAttn& sh, hipStream_t s) {
   SharedParts parts{sh.o, sh.ml, sh.prefix.len + sh.b, sh.max_len, 1, 1};
@@ -378,16 +726,27 @@ hipError_t launch_typed(AttnArgs own, const SharedAttn& sh, hipStream_t s) {
     a.max_ctx = sh.max_len;
     a.o_part = sh.o;
     a.ml_part = sh.ml;
-    const Plan p = plan_of(a.rps, 1, a.n_heads, a.n_kv_heads, a.head_dim, a.max_ctx);
+    const bool wide = sh.bf16 && is_wide(a.rps * (a.n_heads / a.n_kv_heads));
+    const Plan p = prefix_plan(a.rps, a.n_heads, a.n_kv_heads, a.head_dim, a.max_ctx, sh.bf16);
     if (p.parts > sh.parts) return hipErrorInvalidValue;  // (the caller has checked)
     parts.keys = p.per * chunk_of(a.head_dim);
     parts.stride = p.parts;
-    const hipError_t e = launch_plan(a, p, 1, PrefixPass<T>{sh.b}, s);
+    hipError_t e;
+    if constexpr (sizeof(T) == 2) e = wide ? launch_wide(a, p, 1, PrefixPass<T>{sh.b}, s) : launch_plan(a, p, 1, PrefixPass<T>{sh.b}, s);
+    else e = launch_plan(a, p, 1, PrefixPass<T>{sh.b}, s);
     if (e != hipSuccess) return e;
   }
   const int B = own.M / own.rps;
   const int nw = own_waves(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
   if (nw > 0) return launch_own<T>(own, parts, nw, s);
+  if constexpr (sizeof(T) == 2) {
+    Plan p = wide_plan(own.rps, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
+    if (is_wide(own.rps * (own.n_heads / own.n_kv_heads)) && own.max_ctx <= 8192) {
+      p.per = p.nwg * p.per;  // (a workgroup a unit)
+      p.nwg = 1;
+      return launch_wide(own, p, B, OwnPass<T>{parts}, s);
+    }
+  }
   const Plan p = plan_of(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
   if (p.parts > own.n_split) return hipErrorInvalidValue;
   return launch_plan(own, p, B, OwnPass<T>{parts}, s);
@@ -401,7 +760,7 @@ bool attention_shared_fits(int64_t rows, int n_heads, int n_kv_heads) {
 }
 
 int attention_shared_parts(int rows, int n_heads, int n_kv_heads, int head_dim, int max_len, bool bf16) {
-  return plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len).parts;
+  return prefix_plan(rows, n_heads, n_kv_heads, head_dim, max_len, bf16).parts;
 }
 
 hipError_t launch_attention_shared(const AttnArgs& own, const SharedAttn& sh, hipStream_t s) {

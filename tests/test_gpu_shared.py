@@ -6,9 +6,10 @@ that file's (the parts of queries and probabilities, float32 sums) with the join
 exponentials and sums:
   ds  = (2^-18 + (hd + 2) 2^-24) max_j sum_d |q_d k_jd| / sqrt(hd) + 2^-22 max|s|
   |o - ref| <= (2 ds + 2^-17 + 2^-21 + (keys + 128) 2^-24) max|v|
-bfloat16: a probability may enter its product as one fp16 value, off by half a step of it,
-2^-11 (weights whose sum is 1: 2^-11 max|v| in all; below 2^-29 of the largest by 2^-40 each),
-and the result is rounded to bfloat16, half a step, 2^-8 of it.
+bfloat16: a probability may enter its product and the sum as one fp16 value, off by half a step of
+it, 2^-11, and below 2^-25 of the largest by half of 2^-24 2^-11 (which is 1 / 2^36 of it):
+sum (p + e) v / sum (p + e) - o = sum e (v - o) / sum (p + e), at most 2 2^-11 (1 + 2^-10) max|v|,
+and keys 2^-35 max|v|; the result is rounded to bfloat16, half a step, 2^-8 of it.
 """
 import numpy as np
 import pytest
@@ -70,7 +71,7 @@ def _reference(q, pk, pv, kvs, lens):
         back = lambda x: x.reshape(G, H // G, n, -1).permute(2, 0, 1, 3).reshape(n, H, -1)  # noqa: E731
         ref[b], tol[b] = back(o), back(t)
         if q.dtype == torch.bfloat16:
-            tol[b] += back((2.0 ** -11 + m * 2.0 ** -40) * big.expand(-1, t.shape[1]))
+            tol[b] += back((2.0 ** -10 * (1 + 2.0 ** -10) + m * 2.0 ** -35) * big.expand(-1, t.shape[1]))
     if q.dtype == torch.bfloat16:
         tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
     return ref, tol
