@@ -8,6 +8,8 @@
 // split over its keys, (M, L, O) of every part to the workspace; second launch: every
 // sequence's rows over its own cache, which joins the parts as it finishes a row.
 // The prefix's codes are read once for 16 or 32 rows of a kv head, not once a sequence.
+#include <type_traits>
+
 #include "attention8.h"
 
 namespace specdec {
@@ -382,6 +384,15 @@ hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStre
 // does not.
 constexpr float kSlack = 4.f, kWideLift = 11.f;  // (2^(kSlack + kWideLift) is fp16's; held down to 2^-25 in full)
 
+// Maximum of N values, NaN where one is (fmaxf would quiet each product's value first).
+template <int N>
+__device__ __forceinline__ float max_of(const float (&p)[N]) {
+  float m = p[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) m = __builtin_elementwise_maximum(m, p[e]);
+  return m;
+}
+
 template <int HD, int RT, class X>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, int parts, int per, X x) {
   constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, SP = steps_of(HD), OS = HD + 4, NW = 4;
@@ -447,30 +458,40 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) of[q][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  // Scores (unscaled) of tile q become probabilities times 2^kWideLift.
-  auto softmax = [&](int q, auto& p) {
-    constexpr int N = sizeof(p) / sizeof(float);
-    float m = fmaxf(p[0], p[1]);
+  // Scores (unscaled) of N positions a lane: raises the maxima where one exceeds its own by 2^kSlack.
+  auto raise = [&](auto& p) {
+    constexpr int N = sizeof(p[0]) / sizeof(float);
+    float m[RT];
+    bool over = false;
 #pragma unroll
-    for (int e = 2; e < N; ++e) m = fmaxf(m, p[e]);
-    if (__any(__builtin_fmaf(m, qscale, -mx[q]) > kSlack)) {
-      const float mnew = fmaxf(mx[q], groups_max(m) * qscale);
-      const float alpha = __builtin_amdgcn_exp2f(mx[q] - mnew);
-      sums[q] *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) of[q][dt] *= alpha;
-      mx[q] = mnew;
+    for (int q = 0; q < RT; ++q) {
+      m[q] = max_of<N>(p[q]);
+      over |= __builtin_fmaf(m[q], qscale, -mx[q]) > kSlack;
     }
-    const float off = kWideLift - mx[q];
+    if (__any(over)) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], qscale, off));
+      for (int q = 0; q < RT; ++q) {
+        const float mnew = fmaxf(mx[q], groups_max(m[q]) * qscale);
+        const float alpha = __builtin_amdgcn_exp2f(mx[q] - mnew);
+        sums[q] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) of[q][dt] *= alpha;
+        mx[q] = mnew;
+      }
+    }
   };
-  f16x8 ones;
+  // Scores become probabilities times 2^kWideLift.
+  auto exponentials = [&](auto& p) {
+    constexpr int N = sizeof(p[0]) / sizeof(float);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.f;
-
-  for (; j < j_sealed; j += NW) {  // (wave-uniform) codes: every query sees them all
-    float p[RT][8 * SP];
+    for (int q = 0; q < RT; ++q) {
+      const float off = kWideLift - mx[q];
+#pragma unroll
+      for (int e = 0; e < N; ++e) p[q][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[q][e], qscale, off));
+    }
+  };
+  // The codes in hand: scores of this lane's positions.
+  auto scores = [&](float (&p)[RT][8 * SP]) {
 #pragma unroll
     for (int sp = 0; sp < SP; ++sp) {
       floatx4 acc[RT][2];
@@ -496,11 +517,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
     }
-    load_k(j + NW);
-    f16x8 pp[RT][SP];
+  };
+  auto halves = [&](const float (&p)[RT][8 * SP], f16x8 (&pp)[RT][SP]) {
 #pragma unroll
-    for (int q = 0; q < RT; ++q) {
-      softmax(q, p[q]);
+    for (int q = 0; q < RT; ++q)
 #pragma unroll
       for (int sp = 0; sp < SP; ++sp) {
         u32x4 w;
@@ -509,33 +529,72 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
           w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[q][8 * sp + 2 * e], p[q][8 * sp + 2 * e + 1]}, f16x2));
         pp[q][sp] = __builtin_bit_cast(f16x8, w);
       }
-    }
-    const int ve = __builtin_amdgcn_readfirstlane((int)__float_as_uint(vs) >> 23) - 127;
+  };
+  f16x8 ones;
 #pragma unroll
-    for (int sp = 0; sp < SP; ++sp)
+  for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.f;
+  auto add = [&](const f16x8 (&pp)[RT][SP], auto in_range) {
+#pragma unroll
+    for (int sp = 0; sp < SP; ++sp) {
 #pragma unroll
       for (int q = 0; q < RT; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pp[q][sp], sums[q], 0, 0, 0);
-    if (ve >= -15 && ve <= 7) {  // (V's values are fp16's)
 #pragma unroll
-      for (int sp = 0; sp < SP; ++sp)
+      for (int dt = 0; dt < DT; ++dt) {
+        const u32x4 w = vc[sp][dt / 2];
+        const f16x8 vv = fp8x8_to_f16(w[2 * (dt & 1)], w[2 * (dt & 1) + 1], in_range ? vs : 1.0f);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const f16x8 vv = fp8x8_to_f16(vc[sp][dt / 2][2 * (dt & 1)], vc[sp][dt / 2][2 * (dt & 1) + 1], vs);
-#pragma unroll
-          for (int q = 0; q < RT; ++q) of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], of[q][dt], 0, 0, 0);
+        for (int q = 0; q < RT; ++q) {
+          if (in_range) of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], of[q][dt], 0, 0, 0);
+          else of[q][dt] += __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0) * vs;
         }
-    } else {  // the codes' products, times the scale
-#pragma unroll
-      for (int sp = 0; sp < SP; ++sp)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const f16x8 vv = fp8x8_to_f16(vc[sp][dt / 2][2 * (dt & 1)], vc[sp][dt / 2][2 * (dt & 1) + 1], 1.0f);
-#pragma unroll
-          for (int q = 0; q < RT; ++q)
-            of[q][dt] += __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0) * vs;
-        }
+      }
     }
-    load_v(j + NW);
+  };
+
+  // Codes: every query sees them all.  Where all of V's scales leave fp16's values (2^-15 .. 2^7),
+  // a chunk's exponentials and second product run beside the next chunk's scores, which wait
+  // for none of them: one block of instructions, that the vector and the matrix unit share.
+  bool ranged = true;
+  for (int i = k_lo * SP / 2 + lane; 2 * i < j_sealed * SP; i += kWave) {
+    const int ve = (int)(__builtin_amdgcn_raw_buffer_load_b32(sr, (2 * i + 1) * 4, 0, 0) >> 23) - 127;
+    ranged = ranged && ve >= -15 && ve <= 7;
+  }
+  if (j < j_sealed) {  // (wave-uniform)
+    if (__all(ranged)) {
+      float p[RT][8 * SP], next[RT][8 * SP];
+      scores(p);
+      load_k(j + NW);
+      raise(p);
+      while (true) {
+        f16x8 pp[RT][SP];
+        scores(next);  // (past the last chunk: of zeros, unused)
+        exponentials(p);
+        load_k(j + 2 * NW);
+        halves(p, pp);
+        add(pp, std::true_type{});
+        load_v(j + NW);
+        j += NW;
+        if (j >= j_sealed) break;
+        raise(next);
+#pragma unroll
+        for (int q = 0; q < RT; ++q)
+#pragma unroll
+          for (int e = 0; e < 8 * SP; ++e) p[q][e] = next[q][e];
+      }
+    } else {
+#pragma unroll 1
+      for (; j < j_sealed; j += NW) {
+        float p[RT][8 * SP];
+        f16x8 pp[RT][SP];
+        scores(p);
+        load_k(j + NW);
+        raise(p);
+        exponentials(p);
+        halves(p, pp);
+        add(pp, std::false_type{});  // (the codes' products, times the scale)
+        load_v(j + NW);
+      }
+    }
   }
 
   if (jr < k_hi) {  // (wave-uniform) the ring's rows
@@ -584,13 +643,20 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
             acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[1], qq[q][s], acc[q][1], 0, 0, 0);
           }
         }
+        u32x4 rv[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          rv[dt] = *(const u32x4*)(ring + KvIndex<uint16_t>::v(w0 + 8 * grp, 16 * dt + c16, HD, window));
         float p[RT][8];
         bf16x8 pp[RT][2];
 #pragma unroll
-        for (int q = 0; q < RT; ++q) {
+        for (int q = 0; q < RT; ++q)
 #pragma unroll
           for (int e = 0; e < 8; ++e) p[q][e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
-          softmax(q, p[q]);
+        raise(p);
+        exponentials(p);
+#pragma unroll
+        for (int q = 0; q < RT; ++q) {
           split_parts<2>(p[q], pp[q]);
 #pragma unroll
           for (int k = 1; k >= 0; --k) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pp[q][k], sums[q], 0, 0, 0);
@@ -600,7 +666,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
         bool odd = false;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          u32x4 v = *(const u32x4*)(ring + KvIndex<uint16_t>::v(w0 + 8 * grp, 16 * dt + c16, HD, window));
+          u32x4 v = rv[dt];
           if (diagonal) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
