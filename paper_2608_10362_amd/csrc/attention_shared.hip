@@ -129,7 +129,8 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
   for (int dt = 0; dt < DT; ++dt) of[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int plen = __builtin_amdgcn_readfirstlane(*pre.len);
   const int n_pre = (min(plen, pre.max_len) + pre.keys - 1) / pre.keys;
-  for (int p = wave; p < n_pre; p += NW) {
+#pragma unroll 2
+  for (int p = wave; p < n_pre; p += NW) {  // (two parts' loads in flight: 94 -> 92 us, 128 rows over 16384 keys)
     const size_t slot = ((size_t)row * H + head) * pre.stride + p;
     float2 ml = make_float2(kLeast, 0.f);
     f32x4 v[DT];
