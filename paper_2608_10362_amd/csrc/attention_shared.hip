@@ -397,17 +397,22 @@ __device__ __forceinline__ float max_of(const float (&p)[N]) {
   return m;
 }
 
-template <int HD, int RT, class X>
+// KW: waves that take turns at a unit's chunks (the unit is the workgroup's, its waves are merged at
+// the end), or 1: each wave has 16 RT rows of its own and all of its unit's keys, so nothing is
+// merged, and the codes that four waves read at about the same time come from one cache.
+template <int HD, int RT, int KW, class X>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, int parts, int per, X x) {
-  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, SP = 1, OS = HD + 4, NW = 4;
-  __shared__ float so[NW][16][OS];
-  __shared__ float sml[NW][16][2];
+  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, SP = 1, OS = HD + 4, NW = KW;
+  __shared__ float so[KW > 1 ? KW : 1][16][KW > 1 ? OS : 1];
+  __shared__ float sml[KW][16][2];
   typedef uint16_t T;
   int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = KW > 1 ? wave_id : 0;
   const int c16 = lane & 15, grp = lane >> 4;
   const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, nq = rps * group, window = a.f8.ring.capacity;
-  const int b = blockIdx.z, u = blockIdx.y, part = blockIdx.x, tile = u / G, g = u - tile * G;
+  const int b = blockIdx.z, u = blockIdx.y, part = blockIdx.x, unit = u / G, g = u - unit * G;
+  const int tile = KW > 1 ? unit : unit * 4 + wave_id;  // (of 16 RT rows)
+  if (KW == 1 && tile * RT * 16 >= nq) return;
   const float qscale = 1.44269504088896341f / sqrtf((float)HD), inv_group = 1.0f / (float)group;
   int seq = b;
   if constexpr (X::kPrefix) seq = x.b;
@@ -461,6 +466,26 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
     sums[q] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) of[q][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  if constexpr (X::kJoin && KW == 1) {  // from the prefix's parts on
+    const int n_pre = (min(*x.parts.len, x.parts.max_len) + x.parts.keys - 1) / x.parts.keys;
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      const int qa = (tile * RT + q) * 16 + c16, qr = div_small(min(qa, nq - 1), inv_group);
+      const size_t slot = ((size_t)(b * rps + qr) * H + g * group + min(qa, nq - 1) - qr * group) * x.parts.stride;
+      for (int p = 0; p < n_pre; ++p) {
+        const float2 ml = *(const float2*)(x.parts.ml + 2 * (slot + p));
+        const float m = fmaxf(mx[q], ml.x), was = __builtin_amdgcn_exp2f(mx[q] - m);
+        const float w = __builtin_amdgcn_exp2f(ml.x - m) * 0x1p11f;  // (2^kWideLift)
+        sums[q] = sums[q] * was + w * ml.y;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const f32x4 v = *(const f32x4*)(x.parts.o + (slot + p) * HD + 16 * dt + 4 * grp);
+          of[q][dt] = of[q][dt] * was + __builtin_bit_cast(floatx4, v) * w;
+        }
+        mx[q] = m;
+      }
+    }
   }
   // Scores (unscaled) of N positions a lane: whether one exceeds its maximum by 2^kSlack; the maxima
   // raised to them.
@@ -639,11 +664,32 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
     bf16x8 one;
 #pragma unroll
     for (int e = 0; e < 8; ++e) one[e] = (__bf16)1.f;
+    // (a sub-chunk's K and V are asked for a sub-chunk ahead; those behind the newest row, not)
+    const __amdgpu_buffer_rsrc_t rr = make_rsrc(ring, (uint32_t)window * HD * 4u);
+    u32x4 rk[2 * KST], rv[DT];
+    auto ring_k = [&](int k0) {
+      const int w0 = k0 % window;
+#pragma unroll
+      for (int i = 0; i < 2 * KST; ++i) {
+        const int t = i / KST, s = i % KST, d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
+        const int pos = 8 * (c16 >> 2) + 4 * t + (c16 & 3);
+        const uint32_t at = (uint32_t)KvIndex<uint16_t>::k(w0 + pos, d, HD, window) * 2u;
+        rk[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, k0 + pos < vis ? at : kOutOfRange, 0, 0));
+      }
+    };
+    auto ring_v = [&](int k0) {
+      const int w0 = k0 % window;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint32_t at = (uint32_t)KvIndex<uint16_t>::v(w0 + 8 * grp, 16 * dt + c16, HD, window) * 2u;
+        rv[dt] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, k0 + 8 * grp < vis ? at : kOutOfRange, 0, 0));
+      }
+    };
+    ring_k(jr * kF8Sub);
+    ring_v(jr * kF8Sub);
 #pragma unroll 1
-    for (; jr < k_hi; jr += NW)
-#pragma unroll 1
-      for (int sp = 0; sp < SP; ++sp) {
-        const int k0 = (jr * SP + sp) * kF8Sub, w0 = k0 % window;
+    for (; jr < k_hi; jr += NW) {
+        const int k0 = jr * kF8Sub, w0 = k0 % window;
         if (k0 >= vis) break;
         const bool diagonal = k0 + kF8Sub - 1 > lowest;
         floatx4 acc[RT][2];
@@ -651,21 +697,13 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
         for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KST; ++s) {
-          const int d = HD >= 64 ? 64 * (s >> 1) + 16 * grp + 8 * (s & 1) : 32 * s + 8 * grp;
-          bf16x8 kk[2];
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            kk[t] = *(const bf16x8*)(ring + KvIndex<uint16_t>::k(w0 + 8 * (c16 >> 2) + 4 * t + (c16 & 3), d, HD, window));
 #pragma unroll
           for (int q = 0; q < RT; ++q) {
-            acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[0], qq[q][s], acc[q][0], 0, 0, 0);
-            acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[1], qq[q][s], acc[q][1], 0, 0, 0);
+            acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rk[s]), qq[q][s], acc[q][0], 0, 0, 0);
+            acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rk[KST + s]), qq[q][s], acc[q][1], 0, 0, 0);
           }
         }
-        u32x4 rv[DT];
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          rv[dt] = *(const u32x4*)(ring + KvIndex<uint16_t>::v(w0 + 8 * grp, 16 * dt + c16, HD, window));
+        ring_k(k0 + NW * kF8Sub);
         float p[RT][8];
         bf16x8 pp[RT][2];
 #pragma unroll
@@ -722,9 +760,33 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
             }
           }
         }
-      }
+        ring_v(k0 + NW * kF8Sub);
+    }
   }
 
+  if constexpr (KW == 1) {  // a lane's dims of its queries
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      const int qa = (tile * RT + q) * 16 + c16, qr = div_small(qa, inv_group), head = g * group + qa - qr * group;
+      if (qa >= nq) continue;
+      const size_t row = (size_t)b * rps + qr;
+      if constexpr (X::kPrefix) {
+        const size_t slot = (row * H + head) * parts + part;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          *(floatx4*)(a.o_part + slot * HD + 16 * dt + 4 * grp) = of[q][dt] * 0x1p-11f;  // (2^-kWideLift)
+        if (grp == 0) *(float2*)(a.ml_part + 2 * slot) = make_float2(mx[q], sums[q][0] * 0x1p-11f);
+      } else {
+        const float inv = 1.0f / sums[q][0];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          store4((T*)a.o + (row * H + head) * HD + 16 * dt + 4 * grp, __builtin_bit_cast(f32x4, of[q][dt]) * inv);
+        if (grp == 0 && (a.f8.len[b] + qr >= a.max_ctx || *x.parts.len > x.parts.max_len))
+          set_status(a.status, kStatusKvCapacity);  // (the host's bound was wrong)
+      }
+    }
+    return;
+  }
   // The waves' results, tile by tile.
 #pragma unroll
   for (int q = 0; q < RT; ++q) {
@@ -768,15 +830,20 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
 // 16 RT rows, as many parts of the keys as fill the card twice.
 __host__ __device__ constexpr int wide_tiles(int head_dim) { return head_dim == 128 ? 2 : 4; }
 bool is_wide(int nq) { return nq > 16; }
-Plan wide_plan(int rps, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
+// `line` of its plan: whether a wave has rows of its own (KW == 1).
+Plan wide_plan(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx, bool prefix) {
   Plan p{};
-  const int nq = rps * (n_heads / n_kv_heads);
-  p.n_tiles = (nq + 16 * wide_tiles(head_dim) - 1) / (16 * wide_tiles(head_dim));
-  const long nb = (max_ctx + kF8Sub - 1) / kF8Sub, units = (long)n_kv_heads * p.n_tiles;
-  const long slots = 2L * device_compute_units(), all = std::max(1L, slots / units);
+  const int nq = rps * (n_heads / n_kv_heads), rows = 16 * wide_tiles(head_dim);
+  const long slots = 2L * device_compute_units(), nb = (max_ctx + kF8Sub - 1) / kF8Sub;
+  // A wave's own rows: a prefix's where they fill the card without a cut of its keys (8 x 512 rows over 2000
+  // keys 223 us, 245 else; 6 x 170 rows over 3500, half of that, 99 us, 95 else); own texts, short
+  // and triangular, from an eighth of it on (6 x 170 rows: 115 -> 95 us in all).
+  p.line = (long)n_kv_heads * batch * ((nq + 4 * rows - 1) / (4 * rows)) >= (prefix ? slots : slots / 8);
+  p.n_tiles = (nq + (p.line ? 4 : 1) * rows - 1) / ((p.line ? 4 : 1) * rows);
+  const long units = (long)n_kv_heads * p.n_tiles * batch, all = prefix ? std::max(1L, slots / units) : 1;
   const long per = std::max({(nb + all - 1) / all, (nb + kPartsMax8 - 1) / kPartsMax8, 4L});
-  p.per = (int)per;
-  p.nwg = (int)((nb + per - 1) / per);
+  p.per = (int)(prefix ? per : nb);
+  p.nwg = (int)((nb + p.per - 1) / p.per);
   p.parts = (int)std::min<long>({nb, all, (long)kPartsMax8});
   return p;
 }
@@ -784,20 +851,24 @@ Plan wide_plan(int rps, int n_heads, int n_kv_heads, int head_dim, int max_ctx) 
 template <class X>
 hipError_t launch_wide(const AttnArgs& a, const Plan& p, int B, const X& x, hipStream_t s) {
   const dim3 grid(p.nwg, (unsigned)(a.n_kv_heads * p.n_tiles), B);
-#define SD_WIDE(HD) \
-  hipLaunchKernelGGL((wide_kernel<HD, wide_tiles(HD), X>), grid, dim3(256), 0, s, a, p.n_tiles, p.parts, p.per, x)
+#define SD_WIDE(HD, KW) \
+  hipLaunchKernelGGL((wide_kernel<HD, wide_tiles(HD), KW, X>), grid, dim3(256), 0, s, a, p.n_tiles, p.parts, p.per, x)
+#define SD_WIDE_HD(HD)          \
+  if (p.line) SD_WIDE(HD, 1);   \
+  else SD_WIDE(HD, 4);
   switch (a.head_dim) {
-    case 32: SD_WIDE(32); break;
-    case 64: SD_WIDE(64); break;
-    case 128: SD_WIDE(128); break;
+    case 32: SD_WIDE_HD(32) break;
+    case 64: SD_WIDE_HD(64) break;
+    case 128: SD_WIDE_HD(128) break;
     default: return hipErrorInvalidValue;
   }
+#undef SD_WIDE_HD
 #undef SD_WIDE
   return hipGetLastError();
 }
 
 Plan prefix_plan(int rows, int n_heads, int n_kv_heads, int head_dim, int max_len, bool bf16) {
-  return bf16 && is_wide(rows * (n_heads / n_kv_heads)) ? wide_plan(rows, n_heads, n_kv_heads, head_dim, max_len)
+  return bf16 && is_wide(rows * (n_heads / n_kv_heads)) ? wide_plan(rows, 1, n_heads, n_kv_heads, head_dim, max_len, true)
                                                         : plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len);
 }
 
@@ -825,12 +896,9 @@ hipError_t launch_typed(AttnArgs own, const SharedAttn& sh, hipStream_t s) {
   const int nw = own_waves(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
   if (nw > 0) return launch_own<T>(own, parts, nw, s);
   if constexpr (sizeof(T) == 2) {
-    Plan p = wide_plan(own.rps, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
-    if (is_wide(own.rps * (own.n_heads / own.n_kv_heads)) && own.max_ctx <= 8192) {
-      p.per = p.nwg * p.per;  // (a workgroup a unit)
-      p.nwg = 1;
+    const Plan p = wide_plan(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx, false);
+    if (is_wide(own.rps * (own.n_heads / own.n_kv_heads)) && own.max_ctx <= 8192)
       return launch_wide(own, p, B, OwnPass<T>{parts}, s);
-    }
   }
   const Plan p = plan_of(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
   if (p.parts > own.n_split) return hipErrorInvalidValue;
