@@ -957,11 +957,12 @@ struct Plan {
 };
 inline int tiles_a_wave(int nq) { return nq <= 64 ? 1 : 2; }
 inline int tiles_of(int nq) { return (nq + 16 * tiles_a_wave(nq) - 1) / (16 * tiles_a_wave(nq)); }
-inline Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
+// qt: query tiles a wave, 0: as tiles_a_wave says.
+inline Plan plan_of(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx, int qt = 0) {
   Plan p;
   const int nq = rps * (n_heads / n_kv_heads);
-  p.qt = tiles_a_wave(nq);
-  p.n_tiles = tiles_of(nq);
+  p.qt = qt ? qt : tiles_a_wave(nq);
+  p.n_tiles = (nq + 16 * p.qt - 1) / (16 * p.qt);
   const long nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim), units = (long)n_kv_heads * p.n_tiles;
   const long slots = 2L * device_compute_units();  // workgroups resident at once
   // Several sequences of unlike lengths, one query tile, more than four chunks a wave:

@@ -869,7 +869,8 @@ hipError_t launch_wide(const AttnArgs& a, const Plan& p, int B, const X& x, hipS
 
 Plan prefix_plan(int rows, int n_heads, int n_kv_heads, int head_dim, int max_len, bool bf16) {
   return bf16 && is_wide(rows * (n_heads / n_kv_heads)) ? wide_plan(rows, 1, n_heads, n_kv_heads, head_dim, max_len, true)
-                                                        : plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len);
+                                                        : plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len,
+                                                                  rows * (n_heads / n_kv_heads) > 16 ? 2 : 1);
 }
 
 template <typename T>

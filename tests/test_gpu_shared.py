@@ -133,6 +133,59 @@ def test_long_prefixes_and_many_rows(hd, H, G, P, B, n, dtype):
     log(f"worst error {_check(_attend(prefix, kv, q), q, pk, pv, kvs, lens):.3g}")
 
 
+# many rows, cut as the largest calls are: hd, H, G, P, B, n
+MANY = [(64, 16, 8, 300, 8, 35),    # own texts: a wave's rows are its own
+        (128, 8, 4, 200, 18, 67),
+        (32, 12, 6, 1000, 11, 50),
+        (128, 64, 32, 700, 8, 128),  # and the prefix's
+        (64, 64, 64, 500, 4, 512)]
+
+
+@pytest.mark.parametrize("case", MANY, ids=lambda c: f"hd{c[0]}h{c[1]}-{c[2]}p{c[3]}b{c[4]}n{c[5]}")
+def test_many_sequences_of_many_rows(case):
+    hd, H, G, P, B, n = case
+    rng = np.random.default_rng(P + n)
+    log(f"shared many {case}")
+    prefix, pk, pv = _prefix(rng, hd, G, P, n_layers=1)
+    lens = [int(x) for x in rng.integers(0, 150, B)]
+    lens[0] = 0
+    kv = _cache(_shape(hd, H, G, 1), B, 704, (n + 63 + 63) // 64 * 64)
+    kvs = _fill(kv, rng, lens, n, G, hd)
+    q = _queries(rng, (B, n, H, hd), "bf16")
+    log(f"worst error {_check(_attend(prefix, kv, q), q, pk, pv, kvs, lens):.3g}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,n,G", [(1, 7, 2), (3, 40, 2), (20, 40, 4)])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_bad_rows_that_are_not_seen(hd, B, n, G, dtype):
+    """NaN and infinities in K and V rows of the newest: the queries that see them, and no others."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(hd + n + B)
+    group, P = 2, 100
+    H, L = group * G, 77
+    prefix, pk, pv = _prefix(rng, hd, G, P, n_layers=1)
+    kv = _cache(_shape(hd, H, G, 1), B, 192, 128)
+    kvs = _fill(kv, rng, [L] * B, n, G, hd)
+    q = _queries(rng, (B, n, H, hd), dtype)
+    log(f"bad rows not seen hd={hd} B={B} n={n} {dtype}")
+    clean = _attend(prefix, kv, q)
+    _check(clean, q, pk, pv, kvs, [L] * B)
+    k, v = (np.stack([kvs[b][i][L:] for b in range(B)]) for i in range(2))
+    first, nan, key = n // 3, n // 2, 2 * n // 3
+    v[:, first, 0, 5], v[:, nan, 0, 6], k[:, key, 1, 2] = np.inf, np.nan, np.nan
+    binding.specdec_kv_append(kv, 0, _bf16(k), _bf16(v))
+    got = _attend(prefix, kv, q)
+    _check(got[:, :first], q[:, :first], pk, pv, kvs, [L] * B)
+    h0, h1 = got[:, :, :group], got[:, :, group:2 * group]
+    assert (h0[:, first:, :, 5] == float("inf")).all() or not torch.isfinite(h0[:, first:, :, 5]).any()
+    assert torch.isfinite(h0[:, :nan, :, 6]).all() and torch.isnan(h0[:, nan:, :, 6]).all()
+    assert torch.isfinite(h1[:, :key]).all() and torch.isnan(h1[:, key:]).all()
+    got[:, first:, :group, 5], got[:, nan:, :group, 6] = clean[:, first:, :group, 5], clean[:, nan:, :group, 6]
+    got[:, key:, group:2 * group] = clean[:, key:, group:2 * group]
+    _check(got, q, pk, pv, kvs, [L] * B)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [1, 70])
 def test_magnitudes(dtype, n):
