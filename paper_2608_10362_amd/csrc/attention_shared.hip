@@ -867,10 +867,12 @@ hipError_t launch_wide(const AttnArgs& a, const Plan& p, int B, const X& x, hipS
   return hipGetLastError();
 }
 
+// float32 queries: two tiles a wave from 17 rows on where the codes' second reading would count (32 rows of
+// 7B-like heads over 65536 keys 112 us, 183 with one; over 8192 32 both; over 4000 27 and 24).
 Plan prefix_plan(int rows, int n_heads, int n_kv_heads, int head_dim, int max_len, bool bf16) {
-  return bf16 && is_wide(rows * (n_heads / n_kv_heads)) ? wide_plan(rows, 1, n_heads, n_kv_heads, head_dim, max_len, true)
-                                                        : plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len,
-                                                                  rows * (n_heads / n_kv_heads) > 16 ? 2 : 1);
+  const int nq = rows * (n_heads / n_kv_heads);
+  if (bf16 && is_wide(nq)) return wide_plan(rows, 1, n_heads, n_kv_heads, head_dim, max_len, true);
+  return plan_of(rows, 1, n_heads, n_kv_heads, head_dim, max_len, nq > 64 || (nq > 16 && max_len > 8192) ? 2 : 1);
 }
 
 template <typename T>

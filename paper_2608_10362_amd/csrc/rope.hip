@@ -11,7 +11,8 @@
 // from the lane rotary / 16 further.  The angles depend on the row alone: a workgroup takes
 // 8 rows and some heads, computes the rows' cosines and sines once (the angle in turns in
 // 64 bits, where a far position keeps its fraction, the functions in 32) and keeps them in
-// LDS.  Squares are summed in 64 bits: no float32 input overflows or vanishes there.
+// LDS.  Squares are summed in 32 bits, and again in 64 where their mean is not well inside float32's
+// range: no float32 input overflows or vanishes.
 //
 // The 8 rows are 8 positions of one sequence from a multiple of 8 on: a lane then holds a
 // whole piece of V's operand order (8 positions of a dim, 16 bytes), turned in registers,
@@ -68,8 +69,8 @@ __device__ __forceinline__ u32x4 bf16_row(const float* p) {
 __device__ __forceinline__ u32x4 bf16_row(const uint16_t* p) { return *(const u32x4_a2*)p; }
 
 // Sum over the LPH lanes of a head.
-template <int LPH>
-__device__ __forceinline__ double head_sum(double v) {
+template <int LPH, typename T>
+__device__ __forceinline__ T head_sum(T v) {
 #pragma unroll
   for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
   return v;
@@ -79,6 +80,32 @@ __device__ __forceinline__ double head_sum(double v) {
 __device__ __forceinline__ double inv_sqrt(double m) {
   const double y = __builtin_amdgcn_rsq(m);
   return isinf(m) ? 0.0 : y * (1.5 - 0.5 * m * y * y);
+}
+
+// x of the lane `far` further (the low half of a pair of halves) or nearer: inside a row of 16 lanes
+// without LDS where far is a power of two.
+template <int CTRL, int BANKS = 15>
+__device__ __forceinline__ float dpp(float x, float old) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(old), __float_as_uint(x), CTRL, 0xf, BANKS, false));
+}
+__device__ __forceinline__ void exchange(const float (&x)[8], int far, int from, float (&y)[8]) {
+  constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kShl4 = 0x104, kShr4 = 0x114, kRor8 = 0x128;
+  if (far == 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = dpp<kRor8>(x[e], x[e]);
+  } else if (far == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = dpp<kShr4, 10>(x[e], dpp<kShl4, 5>(x[e], x[e]));
+  } else if (far == 2) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = dpp<kXor2>(x[e], x[e]);
+  } else if (far == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = dpp<kXor1>(x[e], x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], from, kWave);
+  }
 }
 
 // Workgroup: kRopeRows rows (CACHE: positions of a sequence from a multiple of 8 on, those of
@@ -133,74 +160,90 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   }
   __syncthreads();
 
-  const int n_qk_here = max(0, min(u1, n_qk) - u0) * T;
-#pragma unroll 2
-  for (int i = wave; i < n_qk_here; i += NW) {
-    const int u = i / T, t = i - u * T, head = (u0 + u) * HPW + hl, row = r0 + t;
-    const bool is_q = head < H, valid = head < H + G;
-    const TI* src = is_q ? (const TI*)a.q + (int64_t)row * a.ld_q + (int64_t)head * HD
-                         : (const TI*)a.k + (int64_t)row * a.ld_k + (int64_t)(head - H) * HD;
-    float x[8];
-    if (valid) load8(src + d0, x);
-    else
+  // Waves over rows first (their angles stay in registers), over units where there are fewer rows.
+  const int across = T >= 4 ? 4 : T >= 2 ? 2 : 1, uq = min(u1, n_qk);
+  const int far = rot / 16;  // lanes of a half
+  const bool low = l < far, in = a.interleaved ? d0 < rot : l < 2 * far;
+  const int from = lane + (in ? (low ? far : -far) : 0);
+  const int j0 = !in ? 0 : a.interleaved ? d0 / 2 : (low ? l : l - far) * 8;
+  for (int t = wave % across; t < T; t += across) {
+    float c[8], s[8];  // (interleaved: of 4 pairs)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (a.q_gain || a.k_gain) {
-      double m = 0.0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
-      const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
-      if (is_q ? a.q_gain != nullptr : a.k_gain != nullptr) {
-        if (rs > 1e-30 && rs < 1e30) {
-          const float f = (float)rs;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * f * (is_q ? gq[e] : gk[e]);
-        } else {  // (a factor that float32 would not hold)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * rs) * (is_q ? gq[e] : gk[e]);
-        }
-      }
+    for (int e = 0; e < 8; ++e) {
+      c[e] = 1.f;
+      s[e] = 0.f;
     }
-    if (a.interleaved) {
-      if (d0 < rot) {
-        const f32x4 c = *(const f32x4*)&cs[0][t][d0 / 2], s = *(const f32x4*)&cs[1][t][d0 / 2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = x[2 * e], r = x[2 * e + 1];
-          x[2 * e] = p * c[e] - r * s[e];
-          x[2 * e + 1] = r * c[e] + p * s[e];
-        }
-      }
-    } else if (rot) {
-      const int far = rot / 16;  // lanes of a half
-      const bool low = l < far, in = l < 2 * far;
-      const int from = lane + (in ? (low ? far : -far) : 0), j = in ? (low ? l : l - far) * 8 : 0;
-      float c[8], s[8];
+    if (in) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const f32x4 cv = *(const f32x4*)&cs[0][t][j + 4 * k], sv = *(const f32x4*)&cs[1][t][j + 4 * k];
+        if (k == 1 && a.interleaved) break;
+        const f32x4 cv = *(const f32x4*)&cs[0][t][j0 + 4 * k], sv = *(const f32x4*)&cs[1][t][j0 + 4 * k];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           c[4 * k + e] = cv[e];
-          s[4 * k + e] = low ? -sv[e] : sv[e];
+          s[4 * k + e] = low && !a.interleaved ? -sv[e] : sv[e];
         }
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float y = __shfl(x[e], from, kWave);
-        if (in) x[e] = x[e] * c[e] + y * s[e];
-      }
     }
-    if (!valid) continue;
-    if (is_q) {
-      store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x);
-    } else if constexpr (CACHE) {
-      if (stored) {
-        uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head - H);
-        *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
+    const int row = r0 + t;
+#pragma unroll 2
+    for (int u = u0 + wave / across; u < uq; u += NW / across) {
+      const int head = u * HPW + hl;
+      const bool is_q = head < H, valid = head < H + G;
+      const TI* src = is_q ? (const TI*)a.q + (int64_t)row * a.ld_q + (int64_t)head * HD
+                           : (const TI*)a.k + (int64_t)row * a.ld_k + (int64_t)(head - H) * HD;
+      float x[8];
+      if (valid) load8(src + d0, x);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      if (a.q_gain || a.k_gain) {
+        const bool on = is_q ? a.q_gain != nullptr : a.k_gain != nullptr;
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = __builtin_fmaf(x[2 * e], x[2 * e], x[2 * e + 1] * x[2 * e + 1]);
+        const float v = head_sum<LPH>((p[0] + p[1]) + (p[2] + p[3])) * (1.0f / HD) + a.eps;
+        const bool fine = v > 1e-30f && v < 1e30f;
+        const float f = __builtin_amdgcn_rsqf(v);
+        if (__all(fine || !on || !valid)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = on ? x[e] * f * (is_q ? gq[e] : gk[e]) : x[e];
+        } else {  // squares that float32 may not hold
+          double m = 0.0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
+          const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = on ? (float)((double)x[e] * rs) * (is_q ? gq[e] : gk[e]) : x[e];
+        }
       }
-    } else {
-      store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)(head - H) * HD + d0, x);
+      if (a.interleaved) {
+        if (in) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = x[2 * e], r = x[2 * e + 1];
+            x[2 * e] = p * c[e] - r * s[e];
+            x[2 * e + 1] = r * c[e] + p * s[e];
+          }
+        }
+      } else if (rot) {
+        float y[8];
+        exchange(x, far, from, y);
+        if (in)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * c[e] + y[e] * s[e];
+      }
+      if (!valid) continue;
+      if (is_q) {
+        store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x);
+      } else if constexpr (CACHE) {
+        if (stored) {
+          uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head - H);
+          *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
+        }
+      } else {
+        store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)(head - H) * HD + d0, x);
+      }
     }
   }
 

@@ -1,11 +1,12 @@
 """Norm and rotation of queries and keys, alone and into an 8-bit cache, against the float64 oracle.
 
-The bound.  With y the normalised value, a pair's result y_a c - y_b s in float32: the factor
-1 / sqrt is one rounding, its product and the gain's two more (3 steps of 2^-24 each of y);
-the angle, reduced in float64 to at most half a turn, enters as a float32 of at most 1 in half
+The bound.  With y the normalised value, a pair's result y_a c - y_b s in float32: a sum of squares
+is 2 roundings of a pair and 6 levels of sums at most, the mean with eps one more (9 steps of 2^-24, 4.5 of its
+square root), the factor 1 / sqrt within 2^-23 (2 steps), its product and the gain's two more:
+8.5 steps of y; the angle, reduced in float64 to at most half a turn, enters as a float32 of at most 1 in half
 turns (half a step, 2^-25, times pi), the functions are within 4 units in the last place (2^-24 of
 1 each), products and sum are two roundings:
-  |out - ref| <= (3 + 2 + pi / 2 + 4) 2^-24 (|y_a| + |y_b|) < 11 2^-24 (|y_a| + |y_b|)
+  |out - ref| <= (8.5 + 2 + pi / 2 + 4) 2^-24 (|y_a| + |y_b|) < 16.1 2^-24 (|y_a| + |y_b|)
 and the angle itself, position times frequency in float64 on both sides, up to 8 roundings of
 2^-53 of it.  Results of 16 bits: half a step, 2^-8 of the value, more.  Below float32's normal values
 a rounding is half a step of 2^-149, eight of them at most.
@@ -38,8 +39,8 @@ def _tol(x, pos, freq, interleaved, gain, eps, out):
     size = np.abs(y)
     both = size[..., a] + size[..., b]
     angle = np.abs(np.asarray(pos, np.float64))[:, :, None, None] * freq
-    tol = 3 * 2.0 ** -24 * size
-    tol[..., a] = tol[..., b] = (11 * 2.0 ** -24 + 8 * 2.0 ** -53 * angle) * both
+    tol = 8.5 * 2.0 ** -24 * size
+    tol[..., a] = tol[..., b] = (16.1 * 2.0 ** -24 + 8 * 2.0 ** -53 * angle) * both
     ref = oracle.rotate(y, pos, freq, interleaved)
     return ref, tol * (1 + 2.0 ** -8) + (2.0 ** -8 * np.abs(ref) if out == "bf16" else 0.0)
 

@@ -412,8 +412,8 @@ def test_a_decode_loop(dtype):
     turned = lambda x, first, g: rope_oracle.apply(  # noqa: E731
         _np(x), first + np.arange(x.shape[1])[None], freq, False, _np(gains[g]), 1e-5)
     rows = lambda b, n: [f32(rng.normal(0, 1.3, (b, n, h, hd))) for h in (H, G, G)]  # noqa: E731
-    # (norm and rotation: 11 2^-24 of at most two normalised values below sqrt(hd) times a gain below 2)
-    near = 11 * 2.0 ** -24 * 2 * 2 * hd ** 0.5
+    # (norm and rotation: 16.1 2^-24 of at most two normalised values below sqrt(hd) times a gain below 2)
+    near = 16.1 * 2.0 ** -24 * 2 * 2 * hd ** 0.5
 
     prefix = _cache(_shape(hd, H, G, 1), 1, 384, 448)
     q, k, v = rows(1, P)
