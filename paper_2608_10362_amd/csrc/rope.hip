@@ -18,6 +18,7 @@
 // whole piece of V's operand order (8 positions of a dim, 16 bytes), turned in registers,
 // and K's pieces of neighbouring positions leave from one CU.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "fp8.h"
@@ -68,14 +69,6 @@ __device__ __forceinline__ u32x4 bf16_row(const float* p) {
 }
 __device__ __forceinline__ u32x4 bf16_row(const uint16_t* p) { return *(const u32x4_a2*)p; }
 
-// Sum over the LPH lanes of a head.
-template <int LPH, typename T>
-__device__ __forceinline__ T head_sum(T v) {
-#pragma unroll
-  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
-
 // 1 / sqrt(m) in 64 bits: the instruction's 2^-23 squared by one step.
 __device__ __forceinline__ double inv_sqrt(double m) {
   const double y = __builtin_amdgcn_rsq(m);
@@ -87,6 +80,22 @@ __device__ __forceinline__ double inv_sqrt(double m) {
 template <int CTRL, int BANKS = 15>
 __device__ __forceinline__ float dpp(float x, float old) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(old), __float_as_uint(x), CTRL, 0xf, BANKS, false));
+}
+// Sum over the LPH lanes of a head (4, 8 or 16 of a row of 16).
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+  constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;
+  v += dpp<kXor1>(v, v);
+  v += dpp<kXor2>(v, v);
+  if (LPH >= 8) v += dpp<kHalfMirror>(v, v);
+  if (LPH >= 16) v += dpp<kMirror>(v, v);
+  return v;
+}
+template <int LPH>
+__device__ __forceinline__ double head_sum(double v) {
+#pragma unroll
+  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
 }
 __device__ __forceinline__ void exchange(const float (&x)[8], int far, int from, float (&y)[8]) {
   constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kShl4 = 0x104, kShr4 = 0x114, kRor8 = 0x128;
@@ -109,7 +118,7 @@ __device__ __forceinline__ void exchange(const float (&x)[8], int far, int from,
 }
 
 // Workgroup: kRopeRows rows (CACHE: positions of a sequence from a multiple of 8 on, those of
-// the call's), and `per` of the units of HPW heads: Q|K together, then V's.
+// the call's), and `per` of the units of HPW heads: queries, then keys, then values.
 template <int HD, typename TI, typename TO, bool CACHE>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   constexpr int LPH = HD / 8, HPW = kWave / LPH, NW = kRopeThreads / kWave;
@@ -143,109 +152,118 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
     cs[0][t][j] = c;
     cs[1][t][j] = s;
   }
-  const int H = a.n_heads, G = a.n_kv_heads, n_qk = (H + G + HPW - 1) / HPW, n_v = CACHE ? (G + HPW - 1) / HPW : 0;
+  const int H = a.n_heads, G = a.n_kv_heads, n_q = (H + HPW - 1) / HPW, n_k = (G + HPW - 1) / HPW, n_qk = n_q + n_k;
+  const int n_v = CACHE ? n_k : 0;
   const int u0 = chunk * a.per, u1 = min(u0 + a.per, n_qk + n_v);
   const int hl = lane / LPH, l = lane % LPH, d0 = 8 * l;
   const int window = CACHE ? a.f8.ring.capacity : 0;
-  float gq[8], gk[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f;
-  if (a.q_gain) {
-    if (a.gain_bf16) load8((const uint16_t*)a.q_gain + d0, gq);
-    else load8((const float*)a.q_gain + d0, gq);
-  }
-  if (a.k_gain) {
-    if (a.gain_bf16) load8((const uint16_t*)a.k_gain + d0, gk);
-    else load8((const float*)a.k_gain + d0, gk);
-  }
   __syncthreads();
 
   // Waves over rows first (their angles stay in registers), over units where there are fewer rows.
-  const int across = T >= 4 ? 4 : T >= 2 ? 2 : 1, uq = min(u1, n_qk);
+  const int across = T >= 4 ? 4 : T >= 2 ? 2 : 1;
   const int far = rot / 16;  // lanes of a half
   const bool low = l < far, in = a.interleaved ? d0 < rot : l < 2 * far;
   const int from = lane + (in ? (low ? far : -far) : 0);
   const int j0 = !in ? 0 : a.interleaved ? d0 / 2 : (low ? l : l - far) * 8;
-  for (int t = wave % across; t < T; t += across) {
-    float c[8], s[8];  // (interleaved: of 4 pairs)
+  // Units [from, to) of the queries (or keys): heads of n, norm by `gain` or not.
+  auto turn = [&](auto queries, int from_unit, int to_unit, int n, const void* gain, const void* in_rows, int64_t ld) {
+    if (from_unit >= to_unit) return;
+    float g[8], pg[8];  // this lane's gains, its partner's
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      c[e] = 1.f;
-      s[e] = 0.f;
+    for (int e = 0; e < 8; ++e) g[e] = 1.f;
+    if (gain) {
+      if (a.gain_bf16) load8((const uint16_t*)gain + d0, g);
+      else load8((const float*)gain + d0, g);
     }
-    if (in) {
+    if (!a.interleaved) exchange(g, far, from, pg);
+    for (int t = wave % across; t < T; t += across) {
+      // out = f (x c + y s), f the norm's factor: the gains are in c and s (interleaved: c, s of 4 pairs, the gains apart)
+      float c[8], s[8];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (k == 1 && a.interleaved) break;
-        const f32x4 cv = *(const f32x4*)&cs[0][t][j0 + 4 * k], sv = *(const f32x4*)&cs[1][t][j0 + 4 * k];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          c[4 * k + e] = cv[e];
-          s[4 * k + e] = low && !a.interleaved ? -sv[e] : sv[e];
-        }
+      for (int e = 0; e < 8; ++e) {
+        c[e] = 1.f;
+        s[e] = 0.f;
       }
-    }
-    const int row = r0 + t;
-#pragma unroll 2
-    for (int u = u0 + wave / across; u < uq; u += NW / across) {
-      const int head = u * HPW + hl;
-      const bool is_q = head < H, valid = head < H + G;
-      const TI* src = is_q ? (const TI*)a.q + (int64_t)row * a.ld_q + (int64_t)head * HD
-                           : (const TI*)a.k + (int64_t)row * a.ld_k + (int64_t)(head - H) * HD;
-      float x[8];
-      if (valid) load8(src + d0, x);
-      else
+      if (in) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-      if (a.q_gain || a.k_gain) {
-        const bool on = is_q ? a.q_gain != nullptr : a.k_gain != nullptr;
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = __builtin_fmaf(x[2 * e], x[2 * e], x[2 * e + 1] * x[2 * e + 1]);
-        const float v = head_sum<LPH>((p[0] + p[1]) + (p[2] + p[3])) * (1.0f / HD) + a.eps;
-        const bool fine = v > 1e-30f && v < 1e30f;
-        const float f = __builtin_amdgcn_rsqf(v);
-        if (__all(fine || !on || !valid)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = on ? x[e] * f * (is_q ? gq[e] : gk[e]) : x[e];
-        } else {  // squares that float32 may not hold
-          double m = 0.0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
-          const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = on ? (float)((double)x[e] * rs) * (is_q ? gq[e] : gk[e]) : x[e];
-        }
-      }
-      if (a.interleaved) {
-        if (in) {
+        for (int k = 0; k < 2; ++k) {
+          if (k == 1 && a.interleaved) break;
+          const f32x4 cv = *(const f32x4*)&cs[0][t][j0 + 4 * k], sv = *(const f32x4*)&cs[1][t][j0 + 4 * k];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float p = x[2 * e], r = x[2 * e + 1];
-            x[2 * e] = p * c[e] - r * s[e];
-            x[2 * e + 1] = r * c[e] + p * s[e];
+            c[4 * k + e] = cv[e];
+            s[4 * k + e] = low && !a.interleaved ? -sv[e] : sv[e];
           }
         }
-      } else if (rot) {
-        float y[8];
-        exchange(x, far, from, y);
-        if (in)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * c[e] + y[e] * s[e];
       }
-      if (!valid) continue;
-      if (is_q) {
-        store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x);
-      } else if constexpr (CACHE) {
-        if (stored) {
-          uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head - H);
-          *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
+      if (!a.interleaved)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          c[e] *= g[e];
+          s[e] *= pg[e];
         }
-      } else {
-        store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)(head - H) * HD + d0, x);
+      const int row = r0 + t;
+      const TI* src = (const TI*)in_rows + (int64_t)row * ld + d0;
+#pragma unroll 2
+      for (int u = from_unit + wave / across; u < to_unit; u += NW / across) {
+        const int head = u * HPW + hl;
+        const bool valid = head < n;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        if (valid) load8(src + (int64_t)head * HD, x);
+        float f = 1.f;
+        if (gain) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = __builtin_fmaf(x[2 * e], x[2 * e], x[2 * e + 1] * x[2 * e + 1]);
+          const float v = head_sum<LPH>((p[0] + p[1]) + (p[2] + p[3])) * (1.0f / HD) + a.eps;
+          f = __builtin_amdgcn_rsqf(v);
+          if (!__all((v > 1e-30f && v < 1e30f) || !valid)) {  // squares that float32 may not hold
+            double m = 0.0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
+            const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * rs);
+            f = 1.f;
+          }
+        }
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * f * g[e];
+          if (in)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = x[2 * e], r = x[2 * e + 1];
+              x[2 * e] = p * c[e] - r * s[e];
+              x[2 * e + 1] = r * c[e] + p * s[e];
+            }
+        } else {
+          float y[8];
+          exchange(x, far, from, y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float z = x[e] * c[e];
+            x[e] = f * (in ? __builtin_fmaf(y[e], s[e], z) : z);
+          }
+        }
+        if (!valid) continue;
+        if constexpr (queries) {
+          store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x);
+        } else if constexpr (CACHE) {
+          if (stored) {
+            uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head);
+            *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
+          }
+        } else {
+          store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)head * HD + d0, x);
+        }
       }
     }
-  }
+  };
+  turn(std::true_type{}, u0, min(u1, n_q), H, a.q_gain, a.q, a.ld_q);
+  turn(std::false_type{}, max(u0 - n_q, 0), min(u1, n_qk) - n_q, G, a.k_gain, a.k, a.ld_k);
 
   if constexpr (CACHE) {
     if (!stored) return;
@@ -309,7 +327,7 @@ bool rope_fits(int batch, int n, bool cache) {
 
 hipError_t launch_rope(RopeArgs a, int head_dim, int batch, bool in_f32, bool out_f32, bool cache, hipStream_t s) {
   const int hpw = 512 / head_dim;
-  const int units = (a.n_heads + a.n_kv_heads + hpw - 1) / hpw + (cache ? (a.n_kv_heads + hpw - 1) / hpw : 0);
+  const int units = (a.n_heads + hpw - 1) / hpw + (cache ? 2 : 1) * ((a.n_kv_heads + hpw - 1) / hpw);
   const int64_t groups = groups_of(batch, a.n, cache);
   a.rows = batch * a.n;
   a.groups = (int)(groups / batch);
