@@ -423,6 +423,7 @@ struct RopeArgs {
   int layer, pos_limit;
   int32_t* status;
   int rows, groups, per, chunks;  // (set by launch_rope: all rows, groups of rows of a sequence, units a workgroup, workgroups a group)
+  bool stream;                    // (and whether results go past the caches)
   double turns[SPECDEC_ROPE_MAX_PAIRS];  // of a pair, a position
 };
 bool rope_fits(int batch, int n, bool cache);

@@ -55,11 +55,21 @@ __device__ __forceinline__ u32x4 to_bf16x8(const float (&x)[8]) {
     o[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * e], x[2 * e + 1]}, bf16x2));
   return o;
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *(f32x4_a4*)p = f32x4{x[0], x[1], x[2], x[3]};
-  *(f32x4_a4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+// (`stream`: past the caches)
+__device__ __forceinline__ void store8(float* p, const float (&x)[8], bool stream) {
+  const f32x4 lo = {x[0], x[1], x[2], x[3]}, up = {x[4], x[5], x[6], x[7]};
+  if (stream) {
+    __builtin_nontemporal_store(lo, (f32x4_a4*)p);
+    __builtin_nontemporal_store(up, (f32x4_a4*)(p + 4));
+  } else {
+    *(f32x4_a4*)p = lo;
+    *(f32x4_a4*)(p + 4) = up;
+  }
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) { *(u32x4_a2*)p = to_bf16x8(x); }
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8], bool stream) {
+  if (stream) __builtin_nontemporal_store(to_bf16x8(x), (u32x4_a2*)p);
+  else *(u32x4_a2*)p = to_bf16x8(x);
+}
 
 // 8 dims of a value row as bf16.
 __device__ __forceinline__ u32x4 bf16_row(const float* p) {
@@ -176,9 +186,9 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
       else load8((const float*)gain + d0, g);
     }
     if (!a.interleaved) exchange(g, far, from, pg);
-    for (int t = wave % across; t < T; t += across) {
-      // out = f (x c + y s), f the norm's factor: the gains are in c and s (interleaved: c, s of 4 pairs, the gains apart)
-      float c[8], s[8];
+    // out = f (x c + y s), f the norm's factor: the gains are in c and s (interleaved: c, s of 4 pairs, the gains apart)
+    float c[8], s[8];
+    auto angles = [&](int t) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         c[e] = 1.f;
@@ -202,64 +212,75 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
           c[e] *= g[e];
           s[e] *= pg[e];
         }
+    };
+    auto head_of = [&](int t, int head) {
+      const bool valid = head < n;
       const int row = r0 + t;
-      const TI* src = (const TI*)in_rows + (int64_t)row * ld + d0;
-#pragma unroll 2
-      for (int u = from_unit + wave / across; u < to_unit; u += NW / across) {
-        const int head = u * HPW + hl;
-        const bool valid = head < n;
-        float x[8];
+      float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (valid) load8(src + (int64_t)head * HD, x);
-        float f = 1.f;
-        if (gain) {
-          float p[4];
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      if (valid) load8((const TI*)in_rows + (int64_t)row * ld + (int64_t)head * HD + d0, x);
+      float f = 1.f;
+      if (gain) {
+        float p[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = __builtin_fmaf(x[2 * e], x[2 * e], x[2 * e + 1] * x[2 * e + 1]);
-          const float v = head_sum<LPH>((p[0] + p[1]) + (p[2] + p[3])) * (1.0f / HD) + a.eps;
-          f = __builtin_amdgcn_rsqf(v);
-          if (!__all((v > 1e-30f && v < 1e30f) || !valid)) {  // squares that float32 may not hold
-            double m = 0.0;
+        for (int e = 0; e < 4; ++e) p[e] = __builtin_fmaf(x[2 * e], x[2 * e], x[2 * e + 1] * x[2 * e + 1]);
+        const float v = head_sum<LPH>((p[0] + p[1]) + (p[2] + p[3])) * (1.0f / HD) + a.eps;
+        f = __builtin_amdgcn_rsqf(v);
+        if (!__all((v > 1e-30f && v < 1e30f) || !valid)) {  // squares that float32 may not hold
+          double m = 0.0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
-            const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
+          for (int e = 0; e < 8; ++e) m = __builtin_fma((double)x[e], (double)x[e], m);
+          const double rs = inv_sqrt(head_sum<LPH>(m) * (1.0 / HD) + (double)a.eps);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * rs);
-            f = 1.f;
-          }
-        }
-        if (a.interleaved) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * f * g[e];
-          if (in)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p = x[2 * e], r = x[2 * e + 1];
-              x[2 * e] = p * c[e] - r * s[e];
-              x[2 * e + 1] = r * c[e] + p * s[e];
-            }
-        } else {
-          float y[8];
-          exchange(x, far, from, y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float z = x[e] * c[e];
-            x[e] = f * (in ? __builtin_fmaf(y[e], s[e], z) : z);
-          }
-        }
-        if (!valid) continue;
-        if constexpr (queries) {
-          store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x);
-        } else if constexpr (CACHE) {
-          if (stored) {
-            uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head);
-            *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
-          }
-        } else {
-          store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)head * HD + d0, x);
+          for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * rs);
+          f = 1.f;
         }
       }
+      if (a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * f * g[e];
+        if (in)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = x[2 * e], r = x[2 * e + 1];
+            x[2 * e] = p * c[e] - r * s[e];
+            x[2 * e + 1] = r * c[e] + p * s[e];
+          }
+      } else {
+        float y[8];
+        exchange(x, far, from, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float z = x[e] * c[e];
+          x[e] = f * (in ? __builtin_fmaf(y[e], s[e], z) : z);
+        }
+      }
+      if (!valid) return;
+      if constexpr (queries) {
+        store8((TO*)a.q_out + (int64_t)row * a.ld_qo + (int64_t)head * HD + d0, x, a.stream);
+      } else if constexpr (CACHE) {
+        if (stored) {
+          uint16_t* blk = k_block<uint16_t>(a.f8.ring, a.layer, b, head);
+          *(u32x4*)(blk + KvIndex<uint16_t>::k((at0 + t) % window, d0, HD, window)) = to_bf16x8(x);
+        }
+      } else {
+        store8((TO*)a.k_out + (int64_t)row * a.ld_ko + (int64_t)head * HD + d0, x, a.stream);
+      }
+    };
+    if (CACHE && !queries && T == kRopeRows) {
+      // (positions of one head side by side: K's order has 16 bytes of each in a row)
+      const int m0 = from_unit * HPW * kRopeRows + hl, m1 = min(to_unit * HPW, n) * kRopeRows;
+      for (int m = m0 + wave * HPW; m - hl < m1; m += NW * HPW) {
+        angles(m % kRopeRows);
+        head_of(m % kRopeRows, m / kRopeRows);
+      }
+      return;
+    }
+    for (int t = wave % across; t < T; t += across) {
+      angles(t);
+#pragma unroll 4
+      for (int u = from_unit + wave / across; u < to_unit; u += NW / across) head_of(t, u * HPW + hl);
     }
   };
   turn(std::true_type{}, u0, min(u1, n_q), H, a.q_gain, a.q, a.ld_q);
@@ -267,25 +288,35 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
 
   if constexpr (CACHE) {
     if (!stored) return;
+    __shared__ u32x4 turned[NW][8 * kWave];
     const int p0 = (at0 & ~7) % window;
     for (int u = max(u0, n_qk) + wave; u < u1; u += NW) {
-      const int g = (u - n_qk) * HPW + hl;
-      if (g >= G) continue;
+      const int g0 = (u - n_qk) * HPW, g = g0 + hl;
       const TI* src = (const TI*)a.v + (int64_t)r0 * a.ld_v + (int64_t)g * HD + d0;
-      uint16_t* dst = k_block<uint16_t>(a.f8.ring, a.layer, b, g) + KvIndex<uint16_t>::v(p0, d0, HD, window);
       if (T == kRopeRows) {
-        u32x4 x[kRopeRows];
+        if (g < G) {
+          u32x4 x[kRopeRows];
 #pragma unroll
-        for (int t = 0; t < kRopeRows; ++t) x[t] = bf16_row(src + (int64_t)t * a.ld_v);
+          for (int t = 0; t < kRopeRows; ++t) x[t] = bf16_row(src + (int64_t)t * a.ld_v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          u32x4 y;
+          for (int e = 0; e < 8; ++e) {
+            u32x4 y;
 #pragma unroll
-          for (int w = 0; w < 4; ++w)  // (the e-th 16 bits of two rows)
-            y[w] = __builtin_amdgcn_perm(x[2 * w + 1][e >> 1], x[2 * w][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-          *(u32x4*)(dst + 8 * e) = y;
+            for (int w = 0; w < 4; ++w)  // (the e-th 16 bits of two rows)
+              y[w] = __builtin_amdgcn_perm(x[2 * w + 1][e >> 1], x[2 * w][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+            turned[wave][8 * lane + (e ^ (lane & 7))] = y;
+          }
         }
-      } else {
+        // (out through LDS, so that lanes store the dims' pieces side by side: 16 of them are 256 bytes)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = k * kWave + lane, head = g0 + at / HD;
+          if (head < G)
+            *(u32x4*)(k_block<uint16_t>(a.f8.ring, a.layer, b, head) + KvIndex<uint16_t>::v(p0, at % HD, HD, window)) =
+                turned[wave][(at & ~7) + ((at & 7) ^ (at >> 3 & 7))];
+        }
+      } else if (g < G) {
+        uint16_t* dst = k_block<uint16_t>(a.f8.ring, a.layer, b, g) + KvIndex<uint16_t>::v(p0, d0, HD, window);
         for (int t = 0; t < T; ++t) {
           const u32x4 x = bf16_row(src + (int64_t)t * a.ld_v);
 #pragma unroll
@@ -331,8 +362,11 @@ hipError_t launch_rope(RopeArgs a, int head_dim, int batch, bool in_f32, bool ou
   const int64_t groups = groups_of(batch, a.n, cache);
   a.rows = batch * a.n;
   a.groups = (int)(groups / batch);
-  // Heads are split over workgroups until the card is full, each wave with a row's unit at least.
-  const int64_t slots = 8L * device_compute_units();
+  // Results far larger than the caches go past them (134 MB: 60 -> 58 us).
+  a.stream = (int64_t)a.rows * (a.n_heads + a.n_kv_heads) * head_dim * (out_f32 ? 4 : 2) > 64 << 20;
+  // Heads are split over workgroups until the card is full twice, each wave with a row's unit at least.  (8189
+  // rows of 64 heads: 66 us with half as many workgroups, 65 with twice as many.)
+  const int64_t slots = 16L * device_compute_units();
   const int rows = std::min(a.n * (cache ? 1 : batch), kRopeRows);
   const int64_t least = (kRopeThreads / kWave + rows - 1) / rows;
   a.per = (int)std::min<int64_t>(units, std::max<int64_t>({least, (units * groups + slots - 1) / slots, (int64_t)1}));
