@@ -628,11 +628,13 @@ class Rope:
             if len(freqs) != rotary_dim // 2:
                 raise ValueError(f"freqs: expected {rotary_dim // 2} entries")
             self.c.freq[:len(freqs)] = freqs
+        self.ref = ctypes.byref(self.c)
 
     def _on(self, t):
-        for g in self.gains:
-            if g is not None:
-                _same_device(t, "inputs", g)
+        if self.gains[0] is not None:
+            _same_device(t, "inputs", self.gains[0])
+        elif self.gains[1] is not None:
+            _same_device(t, "inputs", self.gains[1])
 
 
 def _float_type(dtype, name: str) -> int:
@@ -644,24 +646,29 @@ def _float_type(dtype, name: str) -> int:
     raise ValueError(f"{name}: expected float32 or bfloat16, got {dtype}")
 
 
-def _head_rows(t, name: str, head_dim: int, dtype=None) -> int:
-    """The stride between the rows of t [batch, n, heads, head_dim], whose heads lie side by side."""
-    if t.dim() != 4 or t.shape[3] != head_dim:
-        raise ValueError(f"{name}: expected [batch, n, heads, {head_dim}]")
+def _head_rows(t, name: str, head_dim: int, dtype=None):
+    """The shape of t [batch, n, heads, head_dim], whose rows' heads lie side by side, and the stride between its rows."""
     _on_current(t, name, t.dtype if dtype is None else dtype)
+    shape = t.shape
+    if len(shape) != 4 or shape[3] != head_dim:
+        raise ValueError(f"{name}: expected [batch, n, heads, {head_dim}]")
     if t.is_contiguous():
-        return t.shape[2] * head_dim
-    if t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != head_dim):
+        return shape, shape[2] * head_dim
+    stride = t.stride()
+    if stride[3] != 1 or (shape[2] > 1 and stride[2] != head_dim):
         raise ValueError(f"{name}: a row's heads must lie side by side")
-    return _row_stride(t[:, :, 0], name, t.shape[2] * head_dim)
+    if shape[0] == 1 or stride[0] == shape[1] * stride[1]:
+        if shape[1] > 1 and stride[1] >= shape[2] * head_dim:
+            return shape, stride[1]
+    return shape, _row_stride(t[:, :, 0], name, shape[2] * head_dim)
 
 
-def _positions(positions, batch: int, n: int, like):
+def _positions(positions, rows, like):
     import torch
     if positions is None:
         return None
-    if tuple(positions.shape) != (batch, n):
-        raise ValueError(f"positions: expected [{batch}, {n}]")
+    if positions.shape != rows:
+        raise ValueError(f"positions: expected {list(rows)}")
     _same_device(positions, "positions", like)
     return _dev(positions, "positions", torch.int32)
 
@@ -671,24 +678,26 @@ def specdec_rope_apply(rope: Rope, q, k, q_out, k_out, positions=None, offset: i
     bfloat16 (inputs of one type, outputs of one), each with one stride between its rows; q and
     q_out, or k and k_out, may be None.  positions: int32 [batch, n] (0 .. n-1 if not given).
     An output may be its own input."""
-    given = [t for t in (q, k) if t is not None]
-    if not given or (q is None) != (q_out is None) or (k is None) != (k_out is None):
+    if (q is None and k is None) or (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("q, k: expected one of them at least, each with its output")
-    out = q_out if q_out is not None else k_out
-    batch, n = given[0].shape[:2]
-    hd, lds = rope.c.head_dim, []
-    for name, t, to in (("q", q, q_out), ("k", k, k_out)):
+    some, to = (q, q_out) if q is not None else (k, k_out)
+    hd, heads, lds = rope.c.head_dim, [], []
+    rows = some.shape[:2]
+    for name, t, out in (("q", q, q_out), ("k", k, k_out)):
         if t is None:
+            heads.append(0)
             lds += [0, 0]
             continue
-        lds += [_head_rows(t, name, hd, given[0].dtype), _head_rows(to, name + "_out", hd, out.dtype)]
-        if t.shape != to.shape or tuple(t.shape[:2]) != (batch, n):
+        shape, ld = _head_rows(t, name, hd, some.dtype)
+        shape_out, ld_out = _head_rows(out, name + "_out", hd, to.dtype)
+        if shape != shape_out or shape[:2] != rows:
             raise ValueError(f"{name}, {name}_out: expected one shape, of one batch of rows")
-    rope._on(given[0])
-    _check(lib().specdec_rope_apply(ctypes.byref(rope.c), batch, n, 0 if q is None else q.shape[2],
-                                    0 if k is None else k.shape[2], _float_type(given[0].dtype, "inputs"), _ptr(q),
-                                    lds[0], _ptr(k), lds[2], _positions(positions, batch, n, given[0]), offset,
-                                    _float_type(out.dtype, "outputs"), _ptr(q_out), lds[1], _ptr(k_out), lds[3],
+        heads.append(shape[2])
+        lds += [ld, ld_out]
+    rope._on(some)
+    _check(lib().specdec_rope_apply(rope.ref, rows[0], rows[1], heads[0], heads[1], _float_type(some.dtype, "inputs"),
+                                    _ptr(q), lds[0], _ptr(k), lds[2], _positions(positions, rows, some), offset,
+                                    _float_type(to.dtype, "outputs"), _ptr(q_out), lds[1], _ptr(k_out), lds[3],
                                     _stream(stream)), "specdec_rope_apply")
 
 
@@ -698,19 +707,20 @@ def specdec_rope_append(kv: KVCache, layer: int, rope: Rope, q, k, v, q_out, pos
     with one stride between its rows; q_out: contiguous, of q's shape, float32 or
     bfloat16 (may be q).  positions: int32 [batch, n], the cache's own (offset + len[b] + i) if
     not given."""
-    hd, G = kv.kv.head_dim, kv.kv.n_kv_heads
-    lds = [_head_rows(t, name, hd, q.dtype) for name, t in (("q", q), ("k", k), ("v", v))]
-    n = q.shape[1]
-    if q.shape[0] != kv.batch or k.shape != v.shape or tuple(k.shape) != (kv.batch, n, G, hd):
-        raise ValueError(f"q, k, v: expected rows of a batch of {kv.batch}, {G} kv heads")
+    hd, G, B = kv.kv.head_dim, kv.kv.n_kv_heads, kv.kv.batch
+    (shape, ld_q), (shape_k, ld_k), (shape_v, ld_v) = (_head_rows(t, name, hd, q.dtype)
+                                                       for name, t in (("q", q), ("k", k), ("v", v)))
+    n = shape[1]
+    if shape[0] != B or shape_k != shape_v or shape_k != (B, n, G, hd):
+        raise ValueError(f"q, k, v: expected rows of a batch of {B}, {G} kv heads")
     _on_current(q_out, "q_out", q_out.dtype)
-    if q_out.shape != q.shape or not q_out.is_contiguous():
+    if q_out.shape != shape or not q_out.is_contiguous():
         raise ValueError("q_out: expected a contiguous tensor of q's shape")
     _same_device(kv.data, "kv", q)
     rope._on(q)
-    _check(lib().specdec_rope_append(ctypes.byref(kv.kv), layer, ctypes.byref(rope.c), n, q.shape[2],
-                                     _float_type(q.dtype, "inputs"), q.data_ptr(), lds[0], k.data_ptr(), lds[1],
-                                     v.data_ptr(), lds[2], _positions(positions, kv.batch, n, q), offset,
+    _check(lib().specdec_rope_append(ctypes.byref(kv.kv), layer, rope.ref, n, shape[2],
+                                     _float_type(q.dtype, "inputs"), q.data_ptr(), ld_q, k.data_ptr(), ld_k,
+                                     v.data_ptr(), ld_v, _positions(positions, shape[:2], q), offset,
                                      _float_type(q_out.dtype, "q_out"), q_out.data_ptr(), _stream(stream)),
            "specdec_rope_append")
 
