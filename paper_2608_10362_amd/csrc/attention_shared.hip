@@ -339,16 +339,20 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
   }
 }
 
-// Waves of a unit: a wave a unit where the card is full of them, else as many as
-// fill it; 0: attn8_kernel, whose units are split over workgroups.
+// Waves of a unit: a wave a unit where the card is full of them, else as many as fill it; 0:
+// attn8_kernel, whose units are split over workgroups.  That is faster from 32 chunks a wave on where the card is full
+// (7B-like, 32 sequences: over 1000 own keys 52 us, 60 there; over 2000 108 and 100), from the fewer the emptier it is
+// (one sequence: over 1000 14 and 16, over 2000 18 and 17; 1.1B-like, 16: over 2000 15 and 18, over 4000 22 both).
 int own_waves(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
   const int nq = rps * (n_heads / n_kv_heads);
   if (nq > 64) return 0;
-  const int64_t units = (int64_t)batch * n_kv_heads * ((nq + 15) / 16), slots = 4L * own_resident(head_dim) * device_compute_units();
+  const int64_t units = (int64_t)batch * n_kv_heads * ((nq + 15) / 16);
+  const int64_t slots = 4L * own_resident(head_dim) * device_compute_units();
   const int nb = (max_ctx + chunk_of(head_dim) - 1) / chunk_of(head_dim);
   int nw = 8;
   while (nw > 1 && (units * nw > slots || nw > nb)) nw /= 2;
-  return nb <= 32 * nw && units < 1 << 24 ? nw : 0;
+  const int64_t most = std::max<int64_t>(6, std::min<int64_t>(32, 32 * units * nw / slots));
+  return nb <= most * nw && units < 1 << 24 ? nw : 0;
 }
 
 template <typename T>
@@ -491,10 +495,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
   // raised to them.
   auto over = [&](auto& p) {
     constexpr int N = sizeof(p[0]) / sizeof(float);
-    float m = -INFINITY;
+    bool any = false;  // (tile by tile: a NaN says nothing of the other tiles' queries)
 #pragma unroll
-    for (int q = 0; q < RT; ++q) m = __builtin_elementwise_maximum(m, __builtin_fmaf(max_of<N>(p[q]), qscale, -mx[q]));
-    return __any(m > kSlack);
+    for (int q = 0; q < RT; ++q) any |= __builtin_fmaf(max_of<N>(p[q]), qscale, -mx[q]) > kSlack;
+    return __any(any);
   };
   auto raise = [&](auto& p) {
     constexpr int N = sizeof(p[0]) / sizeof(float);

@@ -186,6 +186,51 @@ def test_bad_rows_that_are_not_seen(hd, B, n, G, dtype):
     _check(got, q, pk, pv, kvs, [L] * B)
 
 
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("B", [1, 40])
+@pytest.mark.parametrize("P,L", [(0, 0), (30, 0), (0, 70)])
+def test_each_key_in_turn_is_nan(hd, B, P, L):
+    """A NaN key among the newest of many rows: what one query sees leaves the maxima of the others', of
+    other tiles, alone; also where those have seen nothing before."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(hd + B)
+    G, H, n = 2, 4, 40
+    prefix, pk, pv = _prefix(rng, hd, G, P, n_layers=1)
+    kv = _cache(_shape(hd, H, G, 1), B, 128, 128)
+    kvs = _fill(kv, rng, [L] * B, n, G, hd)
+    q = _queries(rng, (B, n, H, hd), "bf16")
+    ref, tol = _reference(q, pk, pv, kvs, [L] * B)
+    k, v = (np.stack([kvs[b][i][L:] for b in range(B)]) for i in range(2))
+    for at in range(0, n, 3):
+        bad = k.copy()
+        bad[:, at] = np.nan
+        binding.specdec_kv_append(kv, 0, _bf16(bad), _bf16(v))
+        got = _attend(prefix, kv, q).double()
+        assert bool(((got - ref).abs() <= tol)[:, :at].all()), (hd, B, P, L, at)
+        assert bool(torch.isnan(got[:, at:]).all())
+
+
+# Own texts that are cut over workgroups: hd, H, G, P, lens, n
+LONG = [(128, 2, 2, 300, [20000], 1), (128, 2, 1, 100, [9000, 17000, 300], 20), (64, 4, 2, 500, [40000, 7], 5),
+        (128, 2, 1, 700, [9000, 0], 70), (32, 8, 2, 64, [30000, 33000, 5, 20000], 3), (64, 2, 2, 0, [30000], 100),
+        (128, 32, 32, 500, [9000] * 3, 1)]
+
+
+@pytest.mark.parametrize("case", LONG, ids=lambda c: f"hd{c[0]}h{c[1]}-{c[2]}b{len(c[4])}n{c[5]}")
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_own_texts(case, dtype):
+    hd, H, G, P, lens, n = case
+    rng = np.random.default_rng(P + n)
+    log(f"shared, long own texts {case} {dtype}")
+    prefix, pk, pv = _prefix(rng, hd, G, P, n_layers=1)
+    kv = _cache(_shape(hd, max(H, 2 * G), G, 1), len(lens), (max(lens) + n + 63) // 64 * 64, 192)
+    kvs = _fill(kv, rng, lens, n, G, hd)
+    q = _queries(rng, (len(lens), n, H, hd), dtype)
+    ws = binding.shared_attention_workspace(prefix, kv, H, n, q.dtype)
+    for _ in range(3):  # (counters of the parts are back at zero)
+        _check(_attend(prefix, kv, q, ws=ws), q, pk, pv, kvs, lens)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [1, 70])
 def test_magnitudes(dtype, n):
