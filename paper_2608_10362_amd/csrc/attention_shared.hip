@@ -6,8 +6,17 @@
 // values of each set, the result is sum_i e^(M_i - M) O_i / sum_i e^(M_i - M) L_i.
 // First launch: all rows of the batch against the prefix as if they were one sequence's,
 // split over its keys, (M, L, O) of every part to the workspace; second launch: every
-// sequence's rows over its own cache, which joins the parts as it finishes a row.
-// The prefix's codes are read once for 16 or 32 rows of a kv head, not once a sequence.
+// sequence's rows over its own cache, which joins the parts to its own.
+// The prefix's codes are read once for 16 to 64 rows of a kv head, not once a sequence.
+//
+//  prefix: float32 queries, or bf16 ones of at most 16 rows a kv head: attn8_kernel; bf16: wide_kernel;
+//  own texts: at most 64 rows, not long: own_kernel; more bf16 rows: wide_kernel; else attn8_kernel.
+//
+// Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
+// 32 us (two streams of 17 us, 4 and 3 TB/s), 128 rows over 16384 and up to 256 own 87 us (the prefix 50 us, 690 TFLOP/s,
+// own texts 38), 6 x 170 rows over 3500 94 us (635 TFLOP/s; the prefix 81), 16 x 5 float32 rows over 4001 and up to
+// 512 36 us.  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553 and 30 to 300 own keys 50 us,
+// 690 TFLOP/s, 2 float32 rows over 200 and 40 11 us (two launches of 5).
 #include <type_traits>
 
 #include "attention8.h"
@@ -17,6 +26,8 @@ namespace specdec {
 namespace {
 
 // ---------------------------------------------------------------- few rows over short texts
+// Bound by the stream of the own codes and of the ring's rows, twice as large (128 rows over up to 256 own keys:
+// 167 MB, 38 us; attn8_kernel 308: its eight waves a unit wait for each other's start and merge).
 // A wave's part of a unit (a sequence's kv head, 16 query rows): chunks wave, wave + NW, ... of the
 // row's own keys, on top of the prefix's parts wave, wave + NW, ..., from which its
 // running maximum, sum and outputs start.  Unlike attn8_kernel's, a unit is one
@@ -80,7 +91,9 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
   const int k_end = max(1, min(most, (len + rps - 1) / chunk_of(HD) + 1));
   const int j_sealed = min(k_end, sealed);
 
-  // Codes: loads past the sealed ones read nothing.
+  // Codes: loads past the sealed ones read nothing.  (Of large batches, one unit's alone: past the caches; 64 rows of
+  // 7B-like heads over 400 to 500 own keys 56 -> 49 us; 16 over 64 to 700, four waves a unit, 32 -> 34 us.)
+  constexpr int kCodes = NW == 1 ? kNonTemporal : 0;
   const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, b, g), (uint32_t)j_sealed * SP * 2 * kF8Sub * HD);
   const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, b, g), (uint32_t)((j_sealed * SP + 1) & ~1) * 4);
   u32x4 kc[SP][FS], vc[SP][FS];
@@ -90,8 +103,9 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
 #pragma unroll
     for (int i = 0; i < SP * FS; ++i) {
       const uint32_t k = at + i / FS * 2 * kF8Sub * HD + i % FS * 1024;
-      kc[i / FS][i % FS] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, k, 0, 0));
-      vc[i / FS][i % FS] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, k + kF8Sub * HD, 0, 0));
+      kc[i / FS][i % FS] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, k, 0, kCodes));
+      vc[i / FS][i % FS] =
+          __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, k + kF8Sub * HD, 0, kCodes));
     }
     ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP & ~1) * 4, 0, 0));
     vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP | 1) * 4, 0, 0));
@@ -387,9 +401,10 @@ hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStre
 //
 // What bounds it is the vector unit beside the matrix unit: a chunk's conversions, 64 of two
 // codes each for 32 keys of 128 dims, are shared by RT tiles; a score costs a maximum, a
-// multiply-add, an exponential and half a conversion.  The running maximum is raised only when
-// a score exceeds it by 2^kSlack (then exactly): no value crosses lanes in a chunk that
-// does not.
+// multiply-add, an exponential and half a conversion.  Of a chunk of 32 keys and 32 rows of 128 dims the products take
+// the matrix unit 544 cycles and the rest the vector unit's issue about 700, which overlap in part (128 rows over 65536
+// keys: matrix unit busy 42% of the time).  The running maximum is raised only when a score exceeds it by 2^kSlack (then
+// exactly): no value crosses lanes in a chunk that does not.
 constexpr float kSlack = 4.f, kWideLift = 11.f;  // (2^(kSlack + kWideLift) is fp16's; held down to 2^-25 in full)
 
 // Maximum of N values, NaN where one is (fmaxf would quiet each product's value first).
@@ -693,78 +708,78 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
     ring_v(jr * kF8Sub);
 #pragma unroll 1
     for (; jr < k_hi; jr += NW) {
-        const int k0 = jr * kF8Sub, w0 = k0 % window;
-        if (k0 >= vis) break;
-        const bool diagonal = k0 + kF8Sub - 1 > lowest;
-        floatx4 acc[RT][2];
+      const int k0 = jr * kF8Sub, w0 = k0 % window;
+      if (k0 >= vis) break;
+      const bool diagonal = k0 + kF8Sub - 1 > lowest;
+      floatx4 acc[RT][2];
 #pragma unroll
-        for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < KST; ++s) {
-#pragma unroll
-          for (int q = 0; q < RT; ++q) {
-            acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rk[s]), qq[q][s], acc[q][0], 0, 0, 0);
-            acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rk[KST + s]), qq[q][s], acc[q][1], 0, 0, 0);
-          }
-        }
-        ring_k(k0 + NW * kF8Sub);
-        float p[RT][8];
-        bf16x8 pp[RT][2];
-#pragma unroll
-        for (int q = 0; q < RT; ++q)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[q][e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
-        if (over(p)) raise(p);
-        exponentials(p);
+      for (int s = 0; s < KST; ++s) {
 #pragma unroll
         for (int q = 0; q < RT; ++q) {
-          split_parts<2>(p[q], pp[q]);
-#pragma unroll
-          for (int k = 1; k >= 0; --k) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pp[q][k], sums[q], 0, 0, 0);
+          acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rk[s]), qq[q][s], acc[q][0], 0, 0, 0);
+          acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rk[KST + s]), qq[q][s], acc[q][1], 0, 0, 0);
         }
-        // (stale entries, NaN and infinities where some query does not see all rows: see attn8_kernel)
-        const int nvalid = vis - (k0 + 8 * grp);
-        bool odd = false;
+      }
+      ring_k(k0 + NW * kF8Sub);
+      float p[RT][8];
+      bf16x8 pp[RT][2];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          u32x4 v = rv[dt];
-          if (diagonal) {
+      for (int q = 0; q < RT; ++q)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              if (2 * w >= nvalid) v[w] = 0u;
-              else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
-              const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
-              odd |= lo || up;
-              if (lo) v[w] &= 0xffff0000u;
-              if (up) v[w] &= 0xffffu;
-            }
-          }
+        for (int e = 0; e < 8; ++e) p[q][e] = k0 + 8 * grp + e > qpos[q] ? -INFINITY : acc[q][e >> 2][e & 3];
+      if (over(p)) raise(p);
+      exponentials(p);
 #pragma unroll
-          for (int k = 1; k >= 0; --k)
+      for (int q = 0; q < RT; ++q) {
+        split_parts<2>(p[q], pp[q]);
 #pragma unroll
-            for (int q = 0; q < RT; ++q)
-              of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pp[q][k], of[q][dt], 0, 0, 0);
-        }
-        if (__any(odd)) {
-          for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
-            const uint16_t* vrow = ring + KvIndex<uint16_t>::v(w0 + i, 0, HD, window);
+        for (int k = 1; k >= 0; --k) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pp[q][k], sums[q], 0, 0, 0);
+      }
+      // (stale entries, NaN and infinities where some query does not see all rows: see attn8_kernel)
+      const int nvalid = vis - (k0 + 8 * grp);
+      bool odd = false;
 #pragma unroll
-            for (int q = 0; q < RT; ++q) {
-              float pi = 0.f;
+      for (int dt = 0; dt < DT; ++dt) {
+        u32x4 v = rv[dt];
+        if (diagonal) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) pi = (i & 7) == e ? p[q][e] : pi;
-              pi = __shfl(pi, 16 * (i >> 3) + c16, kWave);
-#pragma unroll
-              for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  const float v = bf16_bits_to_f32(vrow[(size_t)dt * kWave * 8 + (4 * grp + r) * 8]);
-                  if (k0 + i <= qpos[q] && !isfinite(v)) of[q][dt][r] += pi * v;
-                }
-            }
+          for (int w = 0; w < 4; ++w) {
+            if (2 * w >= nvalid) v[w] = 0u;
+            else if (2 * w + 1 >= nvalid) v[w] &= 0xffffu;
+            const bool lo = (v[w] & 0x7f80u) == 0x7f80u, up = (v[w] & 0x7f800000u) == 0x7f800000u;
+            odd |= lo || up;
+            if (lo) v[w] &= 0xffff0000u;
+            if (up) v[w] &= 0xffffu;
           }
         }
-        ring_v(k0 + NW * kF8Sub);
+#pragma unroll
+        for (int k = 1; k >= 0; --k)
+#pragma unroll
+          for (int q = 0; q < RT; ++q)
+            of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pp[q][k], of[q][dt], 0, 0, 0);
+      }
+      if (__any(odd)) {
+        for (int i = 0; i < kF8Sub; ++i) {  // (position k0 + i; its probability lies in lane group i / 8)
+          const uint16_t* vrow = ring + KvIndex<uint16_t>::v(w0 + i, 0, HD, window);
+#pragma unroll
+          for (int q = 0; q < RT; ++q) {
+            float pi = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pi = (i & 7) == e ? p[q][e] : pi;
+            pi = __shfl(pi, 16 * (i >> 3) + c16, kWave);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float v = bf16_bits_to_f32(vrow[(size_t)dt * kWave * 8 + (4 * grp + r) * 8]);
+                if (k0 + i <= qpos[q] && !isfinite(v)) of[q][dt][r] += pi * v;
+              }
+          }
+        }
+      }
+      ring_v(k0 + NW * kF8Sub);
     }
   }
 
