@@ -325,9 +325,10 @@ SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer
  * the caller's: specdec_rope_append with an offset of P).  The prefix's codes are
  * read once for many rows instead of once a sequence.  The prefix is only read:
  * any number of calls may use one at once, on any streams.
- * dtype: the type of q and out (SPECDEC_F32, as specdec_attention, or SPECDEC_BF16:
- * products of one part, twice the speed where there are many rows; out rounded
- * once).  Everything else as for specdec_attention.
+ * dtype: the type of q and out: SPECDEC_F32, as precise as specdec_attention, or
+ * SPECDEC_BF16: where a kv head has more than 16 rows, probabilities enter their
+ * products as one fp16 value (off by 2^-11), and out is rounded once; about 1.6 times the
+ * speed there.  Everything else as for specdec_attention.
  * workspace: specdec_attention_shared_workspace_bytes bytes (0 for arguments the
  * call rejects).
  * Graph capture: the prefix's part is sized from prefix->len_upper.

@@ -13,10 +13,10 @@
 //  own texts: at most 64 rows, not long: own_kernel; more bf16 rows: wide_kernel; else attn8_kernel.
 //
 // Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
-// 32 us (two streams of 17 us, 4 and 3 TB/s), 128 rows over 16384 and up to 256 own 87 us (the prefix 50 us, 690 TFLOP/s,
-// own texts 38), 6 x 170 rows over 3500 94 us (635 TFLOP/s; the prefix 81), 16 x 5 float32 rows over 4001 and up to
-// 512 36 us.  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553 and 30 to 300 own keys 50 us,
-// 690 TFLOP/s, 2 float32 rows over 200 and 40 11 us (two launches of 5).
+// 32 us (two streams, 17 and 16 us, 3.9 and 3.4 TB/s), 128 rows over 16384 and up to 256 own 91 us (the prefix 50 us,
+// 690 TFLOP/s, own texts 45), 6 x 170 rows over 3500 93 us (645 TFLOP/s; the prefix 82, 710), 16 x 5 float32 rows over
+// 4001 and up to 512 36 us (25 and 14).  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553 and 30 to 300 own keys 50 us,
+// 690 TFLOP/s 2 float32 rows over 200 and 40 11 us (two launches of 5).
 #include <type_traits>
 
 #include "attention8.h"
@@ -27,7 +27,7 @@ namespace {
 
 // ---------------------------------------------------------------- few rows over short texts
 // Bound by the stream of the own codes and of the ring's rows, twice as large (128 rows over up to 256 own keys:
-// 167 MB, 38 us; attn8_kernel 308: its eight waves a unit wait for each other's start and merge).
+// 167 MB, 45 us, 3.7 TB/s; attn8_kernel 308: its eight waves a unit wait for each other's start and merge).
 // A wave's part of a unit (a sequence's kv head, 16 query rows): chunks wave, wave + NW, ... of the
 // row's own keys, on top of the prefix's parts wave, wave + NW, ..., from which its
 // running maximum, sum and outputs start.  Unlike attn8_kernel's, a unit is one
