@@ -119,19 +119,20 @@ __device__ __forceinline__ float groups_max(float v) {
 // (OwnPass).  T: the type of queries and results (float, or uint16_t: bf16).
 struct Alone {
   typedef float T;
-  static constexpr bool kPrefix = false, kJoin = false;
+  static constexpr bool kPrefix = false, kJoin = false, kOneTile = false;
 };
-// The batch's rows count as rows of one sequence; every workgroup stores a part.
+// The batch's rows count as rows of one sequence; every workgroup stores a part.  (bf16 queries: of at most 16
+// rows a kv head, one tile.)
 template <typename TT>
 struct PrefixPass {
   typedef TT T;
-  static constexpr bool kPrefix = true, kJoin = false;
+  static constexpr bool kPrefix = true, kJoin = false, kOneTile = sizeof(T) == 2;
   int b;  // the cache's sequence that holds the prefix
 };
 template <typename TT>
 struct OwnPass {
   typedef TT T;
-  static constexpr bool kPrefix = false, kJoin = true;
+  static constexpr bool kPrefix = false, kJoin = true, kOneTile = false;
   SharedParts parts;
 };
 
@@ -1004,7 +1005,9 @@ hipError_t launch_plan(const AttnArgs& a, const Plan& p, int B, const X& x, hipS
     if constexpr (!X::kPrefix) SD_A8(HDV, 1, true, ONCE);           \
   }
 #define SD_A8_HD(HDV)                                  \
-  if (p.qt == 2) {                                     \
+  if constexpr (X::kOneTile) {                         \
+    SD_A8(HDV, 1, false, true);                        \
+  } else if (p.qt == 2) {                                     \
     SD_A8(HDV, 2, false, false);                       \
   } else if (p.n_tiles == 1) {                         \
     if (p.line) SD_A8_LINE(HDV, true)                  \

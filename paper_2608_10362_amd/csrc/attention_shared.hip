@@ -394,7 +394,7 @@ hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStre
 
 // ---------------------------------------------------------------- many rows of 16-bit queries
 // One workgroup: 16 RT rows of a kv head and a range of keys, its waves every fourth chunk of
-// 32 or 64 (all rows each), merged at the end as attn8_kernel's are.  Queries of bf16 are one
+// 32 (all rows each), merged at the end as attn8_kernel's are; or 64 RT rows (KW, below).  Queries of bf16 are one
 // part of their product, with K's codes as bf16 (exact); probabilities are one fp16 part
 // with V's codes as fp16 (exact), off by 2^-11 of each; the sums are taken of the rounded ones,
 // by a product with ones.  bf16 rows of the ring take two bf16 parts.
@@ -407,12 +407,11 @@ hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStre
 // exactly): no value crosses lanes in a chunk that does not.
 constexpr float kSlack = 4.f, kWideLift = 11.f;  // (2^(kSlack + kWideLift) is fp16's; held down to 2^-25 in full)
 
-// Maximum of N values, NaN where one is (fmaxf would quiet each product's value first).
-template <int N>
-__device__ __forceinline__ float max_of(const float (&p)[N]) {
+// Maximum of a lane's scores, NaN where one is (fmaxf would quiet each product's value first).
+__device__ __forceinline__ float max_of(const float (&p)[8]) {
   float m = p[0];
 #pragma unroll
-  for (int e = 1; e < N; ++e) m = __builtin_elementwise_maximum(m, p[e]);
+  for (int e = 1; e < 8; ++e) m = __builtin_elementwise_maximum(m, p[e]);
   return m;
 }
 
@@ -421,11 +420,11 @@ __device__ __forceinline__ float max_of(const float (&p)[N]) {
 // merged, and the codes that four waves read at about the same time come from one cache.
 template <int HD, int RT, int KW, class X>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, int parts, int per, X x) {
-  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, SP = 1, OS = HD + 4, NW = KW;
+  constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, OS = HD + 4, NW = KW;
   __shared__ float so[KW > 1 ? KW : 1][16][KW > 1 ? OS : 1];
   __shared__ float sml[KW][16][2];
   typedef uint16_t T;
-  int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63;
   const int wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = KW > 1 ? wave_id : 0;
   const int c16 = lane & 15, grp = lane >> 4;
   const int H = a.n_heads, G = a.n_kv_heads, group = H / G, rps = a.rps, nq = rps * group, window = a.f8.ring.capacity;
@@ -451,27 +450,25 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
       qq[q][s] = __builtin_bit_cast(bf16x8, v);
     }
   }
-  const int sealed = __builtin_amdgcn_readfirstlane(a.f8.len[seq]) / kF8Block * (kF8Block / kF8Sub / SP);
+  const int sealed = __builtin_amdgcn_readfirstlane(a.f8.len[seq]) / kF8Block * (kF8Block / kF8Sub);
   const int j_sealed = min(k_hi, sealed);
-  const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, seq, g), (uint32_t)j_sealed * SP * 2 * kF8Sub * HD);
-  const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, seq, g), (uint32_t)((j_sealed * SP + 1) & ~1) * 4);
-  u32x4 kc[SP][FS], vc[SP][FS];
+  const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, seq, g), (uint32_t)j_sealed * 2 * kF8Sub * HD);
+  const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, seq, g), (uint32_t)((j_sealed + 1) & ~1) * 4);
+  u32x4 kc[FS], vc[FS];
   float ks, vs;
   auto load_k = [&](int j) {
-    const uint32_t at = (uint32_t)j * SP * 2 * kF8Sub * HD + lane * 16;
+    const uint32_t at = (uint32_t)j * 2 * kF8Sub * HD + lane * 16;
 #pragma unroll
-    for (int i = 0; i < SP * FS; ++i)
-      kc[i / FS][i % FS] = __builtin_bit_cast(
-          u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i / FS * 2 * kF8Sub * HD + i % FS * 1024, 0, 0));
-    ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP & ~1) * 4, 0, 0));
+    for (int i = 0; i < FS; ++i)
+      kc[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i * 1024, 0, 0));
+    ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j & ~1) * 4, 0, 0));
   };
   auto load_v = [&](int j) {
-    const uint32_t at = (uint32_t)j * SP * 2 * kF8Sub * HD + kF8Sub * HD + lane * 16;
+    const uint32_t at = (uint32_t)j * 2 * kF8Sub * HD + kF8Sub * HD + lane * 16;
 #pragma unroll
-    for (int i = 0; i < SP * FS; ++i)
-      vc[i / FS][i % FS] = __builtin_bit_cast(
-          u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i / FS * 2 * kF8Sub * HD + i % FS * 1024, 0, 0));
-    vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j * SP | 1) * 4, 0, 0));
+    for (int i = 0; i < FS; ++i)
+      vc[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(cr, at + i * 1024, 0, 0));
+    vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, (j | 1) * 4, 0, 0));
   };
   int j = k_lo + wave, jr = max(j, j + (sealed - j + NW - 1) / NW * NW);  // (jr: the first of the ring's)
   load_k(j);
@@ -508,18 +505,16 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
   }
   // Scores (unscaled) of N positions a lane: whether one exceeds its maximum by 2^kSlack; the maxima
   // raised to them.
-  auto over = [&](auto& p) {
-    constexpr int N = sizeof(p[0]) / sizeof(float);
+  auto over = [&](const float (&p)[RT][8]) {
     bool any = false;  // (tile by tile: a NaN says nothing of the other tiles' queries)
 #pragma unroll
-    for (int q = 0; q < RT; ++q) any |= __builtin_fmaf(max_of<N>(p[q]), qscale, -mx[q]) > kSlack;
+    for (int q = 0; q < RT; ++q) any |= __builtin_fmaf(max_of(p[q]), qscale, -mx[q]) > kSlack;
     return __any(any);
   };
-  auto raise = [&](auto& p) {
-    constexpr int N = sizeof(p[0]) / sizeof(float);
+  auto raise = [&](const float (&p)[RT][8]) {
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
-      const float mnew = fmaxf(mx[q], groups_max(max_of<N>(p[q])) * qscale), alpha = __builtin_amdgcn_exp2f(mx[q] - mnew);
+      const float mnew = fmaxf(mx[q], groups_max(max_of(p[q])) * qscale), alpha = __builtin_amdgcn_exp2f(mx[q] - mnew);
       sums[q] *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) of[q][dt] *= alpha;
@@ -527,72 +522,63 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
     }
   };
   // Scores become probabilities times 2^kWideLift.
-  auto exponentials = [&](auto& p) {
-    constexpr int N = sizeof(p[0]) / sizeof(float);
+  auto exponentials = [&](float (&p)[RT][8]) {
 #pragma unroll
     for (int q = 0; q < RT; ++q) {
       const float off = kWideLift - mx[q];
 #pragma unroll
-      for (int e = 0; e < N; ++e) p[q][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[q][e], qscale, off));
+      for (int e = 0; e < 8; ++e) p[q][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[q][e], qscale, off));
     }
   };
   // The codes in hand: scores of this lane's positions.
-  auto scores = [&](float (&p)[RT][8 * SP]) {
+  auto scores = [&](float (&p)[RT][8]) {
+    floatx4 acc[RT][2];
 #pragma unroll
-    for (int sp = 0; sp < SP; ++sp) {
-      floatx4 acc[RT][2];
+    for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int q = 0; q < RT; ++q) acc[q][0] = acc[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < KST; ++s) {
+      bf16x8 kk[2];
 #pragma unroll
-      for (int s = 0; s < KST; ++s) {
-        bf16x8 kk[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const u32x4 w = HD >= 64 ? kc[sp][t * (HD / 64) + s / 2] : kc[sp][0];
-          const int h = HD >= 64 ? s & 1 : t;
-          kk[t] = fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
-        }
-#pragma unroll
-        for (int q = 0; q < RT; ++q) {
-          acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[0], qq[q][s], acc[q][0], 0, 0, 0);
-          acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[1], qq[q][s], acc[q][1], 0, 0, 0);
-        }
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 w = HD >= 64 ? kc[t * (HD / 64) + s / 2] : kc[0];
+        const int h = HD >= 64 ? s & 1 : t;
+        kk[t] = fp8x8_to_bf16(w[2 * h], w[2 * h + 1], ks);
       }
 #pragma unroll
-      for (int q = 0; q < RT; ++q)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[q][8 * sp + e] = acc[q][e >> 2][e & 3];
+      for (int q = 0; q < RT; ++q) {
+        acc[q][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[0], qq[q][s], acc[q][0], 0, 0, 0);
+        acc[q][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[1], qq[q][s], acc[q][1], 0, 0, 0);
+      }
     }
-  };
-  auto halves = [&](const float (&p)[RT][8 * SP], f16x8 (&pp)[RT][SP]) {
 #pragma unroll
     for (int q = 0; q < RT; ++q)
 #pragma unroll
-      for (int sp = 0; sp < SP; ++sp) {
-        u32x4 w;
+      for (int e = 0; e < 8; ++e) p[q][e] = acc[q][e >> 2][e & 3];
+  };
+  auto halves = [&](const float (&p)[RT][8], f16x8 (&pp)[RT]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[q][8 * sp + 2 * e], p[q][8 * sp + 2 * e + 1]}, f16x2));
-        pp[q][sp] = __builtin_bit_cast(f16x8, w);
-      }
+    for (int q = 0; q < RT; ++q) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[q][2 * e], p[q][2 * e + 1]}, f16x2));
+      pp[q] = __builtin_bit_cast(f16x8, w);
+    }
   };
   f16x8 ones;
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.f;
-  auto add = [&](const f16x8 (&pp)[RT][SP], auto in_range) {
+  auto add = [&](const f16x8 (&pp)[RT], auto in_range) {
 #pragma unroll
-    for (int sp = 0; sp < SP; ++sp) {
+    for (int q = 0; q < RT; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pp[q], sums[q], 0, 0, 0);
 #pragma unroll
-      for (int q = 0; q < RT; ++q) sums[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pp[q][sp], sums[q], 0, 0, 0);
+    for (int dt = 0; dt < DT; ++dt) {
+      const u32x4 w = vc[dt / 2];
+      const f16x8 vv = fp8x8_to_f16(w[2 * (dt & 1)], w[2 * (dt & 1) + 1], in_range ? vs : 1.0f);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const u32x4 w = vc[sp][dt / 2];
-        const f16x8 vv = fp8x8_to_f16(w[2 * (dt & 1)], w[2 * (dt & 1) + 1], in_range ? vs : 1.0f);
-#pragma unroll
-        for (int q = 0; q < RT; ++q) {
-          if (in_range) of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], of[q][dt], 0, 0, 0);
-          else of[q][dt] += __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q][sp], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0) * vs;
-        }
+      for (int q = 0; q < RT; ++q) {
+        if (in_range) of[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q], of[q][dt], 0, 0, 0);
+        else of[q][dt] += __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pp[q], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0) * vs;
       }
     }
   };
@@ -601,21 +587,21 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
   // a chunk's exponentials and second product run beside the next chunk's scores, which wait
   // for none of them: one block of instructions, that the vector and the matrix unit share.
   bool ranged = true;
-  for (int i = k_lo * SP / 2 + lane; 2 * i < j_sealed * SP; i += kWave) {
+  for (int i = k_lo / 2 + lane; 2 * i < j_sealed; i += kWave) {
     const int ve = (int)(__builtin_amdgcn_raw_buffer_load_b32(sr, (2 * i + 1) * 4, 0, 0) >> 23) - 127;
     ranged = ranged && ve >= -15 && ve <= 7;
   }
   if (j < j_sealed) {  // (wave-uniform)
     if (__all(ranged)) {
       // (the maxima are raised outside of the loop over chunks: a branch inside it would cost copies of all outputs)
-      float p[RT][8 * SP], next[RT][8 * SP];
+      float p[RT][8], next[RT][8];
       scores(p);
       load_k(j + NW);
       while (true) {
         raise(p);
         bool more;
         do {
-          f16x8 pp[RT][SP];
+          f16x8 pp[RT];
           scores(next);  // (past the last chunk: of zeros, unused)
           exponentials(p);
           load_k(j + 2 * NW);
@@ -625,13 +611,13 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
           // (in this order: 4 vector instructions and an exponential to a product of the scores, 2 to one of the
           // values; 51.5 us against 55 in the compiler's, 128 rows over 16384 keys)
 #pragma unroll
-          for (int i = 0; i < 2 * RT * KST * SP; ++i) {
+          for (int i = 0; i < 2 * RT * KST; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           }
 #pragma unroll
-          for (int i = 0; i < RT * (DT + 1) * SP; ++i) {
+          for (int i = 0; i < RT * (DT + 1); ++i) {
             __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           }
@@ -640,15 +626,15 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
 #pragma unroll
           for (int q = 0; q < RT; ++q)
 #pragma unroll
-            for (int e = 0; e < 8 * SP; ++e) p[q][e] = next[q][e];
+            for (int e = 0; e < 8; ++e) p[q][e] = next[q][e];
         } while (more && !over(p));
         if (!more) break;
       }
     } else {
 #pragma unroll 1
       for (; j < j_sealed; j += NW) {
-        float p[RT][8 * SP];
-        f16x8 pp[RT][SP];
+        float p[RT][8];
+        f16x8 pp[RT];
         scores(p);
         load_k(j + NW);
         if (over(p)) raise(p);

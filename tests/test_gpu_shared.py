@@ -101,6 +101,9 @@ CASES = [  # hd, H, G, prefix, lens, n, window of the sequences' ring
     (64, 2, 2, 250, [130, 0], 129, 192),
     (128, 1, 1, 777, [10] * 33, 1, 128),           # 33 rows
     (64, 5, 5, 96, [1000, 3], 1, 128),             # own text longer than what is shared
+    (64, 71, 1, 300, [200, 0], 1, 128),            # many query heads a kv head
+    (128, 128, 1, 130, [33], 2, 128),
+    (32, 34, 17, 64, [64, 0, 65], 7, 128),
 ]
 
 
