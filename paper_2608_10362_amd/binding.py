@@ -657,10 +657,11 @@ def _head_rows(t, name: str, head_dim: int, dtype=None):
     stride = t.stride()
     if stride[3] != 1 or (shape[2] > 1 and stride[2] != head_dim):
         raise ValueError(f"{name}: a row's heads must lie side by side")
-    if shape[0] == 1 or stride[0] == shape[1] * stride[1]:
-        if shape[1] > 1 and stride[1] >= shape[2] * head_dim:
-            return shape, stride[1]
-    return shape, _row_stride(t[:, :, 0], name, shape[2] * head_dim)
+    width, one = shape[2] * head_dim, shape[0] == 1
+    ld = stride[1] if shape[1] > 1 else width if one else stride[0]
+    if ld >= width and (one or shape[1] == 1 or stride[0] == shape[1] * ld):
+        return shape, ld
+    return shape, _row_stride(t[:, :, 0], name, width)  # (raises)
 
 
 def _positions(positions, rows, like):
