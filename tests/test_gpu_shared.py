@@ -101,6 +101,8 @@ CASES = [  # hd, H, G, prefix, lens, n, window of the sequences' ring
     (64, 2, 2, 250, [130, 0], 129, 192),
     (128, 1, 1, 777, [10] * 33, 1, 128),           # 33 rows
     (64, 5, 5, 96, [1000, 3], 1, 128),             # own text longer than what is shared
+    (128, 4, 4, 300, [600], 1, 128),               # eight waves to a kv head's own text
+    (64, 8, 2, 100, [1000, 30], 2, 128),
     (64, 71, 1, 300, [200, 0], 1, 128),            # many query heads a kv head
     (128, 128, 1, 130, [33], 2, 128),
     (32, 34, 17, 64, [64, 0, 65], 7, 128),
