@@ -15,7 +15,7 @@
 // Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
 // 32 us (two streams, 17 and 16 us, 3.9 and 3.4 TB/s), 128 rows over 16384 and up to 256 own 91 us (the prefix 50 us,
 // 690 TFLOP/s, own texts 45), 6 x 170 rows over 3500 93 us (645 TFLOP/s; the prefix 82, 710), 16 x 5 float32 rows over
-// 4001 and up to 512 36 us (25 and 14).  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553 and 30 to 300 own keys 50 us,
+// 4001 and up to 512 36 us (25 and 14).  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553 and 30 to 300 own keys 48 us,
 // 690 TFLOP/s 2 float32 rows over 200 and 40 11 us (two launches of 5).
 #include <type_traits>
 
@@ -403,7 +403,7 @@ hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStre
 // codes each for 32 keys of 128 dims, are shared by RT tiles; a score costs a maximum, a
 // multiply-add, an exponential and half a conversion.  Of a chunk of 32 keys and 32 rows of 128 dims the products take
 // the matrix unit 544 cycles and the rest the vector unit's issue about 700, which overlap in part (128 rows over 65536
-// keys: matrix unit busy 42% of the time).  The running maximum is raised only when a score exceeds it by 2^kSlack (then
+// keys: matrix unit busy 41% of the time).  The running maximum is raised only when a score exceeds it by 2^kSlack (then
 // exactly): no value crosses lanes in a chunk that does not.
 constexpr float kSlack = 4.f, kWideLift = 11.f;  // (2^(kSlack + kWideLift) is fp16's; held down to 2^-25 in full)
 
@@ -602,11 +602,15 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
         bool more;
         do {
           f16x8 pp[RT];
+          // (a wave at its products before one at its maxima: 1.1B-like, 64 rows over 131072 keys 97 -> 92 us; no
+          // different for 128 dims)
+          if (HD < 128) __builtin_amdgcn_s_setprio(1);
           scores(next);  // (past the last chunk: of zeros, unused)
           exponentials(p);
           load_k(j + 2 * NW);
           halves(p, pp);
           add(pp, std::true_type{});
+          if (HD < 128) __builtin_amdgcn_s_setprio(0);
           load_v(j + NW);
           // (in this order: 4 vector instructions and an exponential to a product of the scores, 2 to one of the
           // values; 51.5 us against 55 in the compiler's, 128 rows over 16384 keys)
