@@ -15,8 +15,8 @@
 // Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
 // 32 us (two streams, 17 and 16 us, 3.9 and 3.4 TB/s), 128 rows over 16384 and up to 256 own 91 us (the prefix 50 us,
 // 690 TFLOP/s, own texts 45), 6 x 170 rows over 3500 93 us (645 TFLOP/s; the prefix 82, 710), 16 x 5 float32 rows over
-// 4001 and up to 512 36 us (25 and 14).  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553 and 30 to 300 own keys 48 us,
-// 690 TFLOP/s 2 float32 rows over 200 and 40 11 us (two launches of 5).
+// 4001 and up to 512 36 us (25 and 14).  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553
+// and 30 to 300 own keys 48 us (710 TFLOP/s), 2 float32 rows over 200 and 40 11 us (two launches of 5).
 #include <type_traits>
 
 #include "attention8.h"
