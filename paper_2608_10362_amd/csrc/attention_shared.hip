@@ -602,8 +602,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, i
         bool more;
         do {
           f16x8 pp[RT];
-          // (a wave at its products before one at its maxima: 1.1B-like, 64 rows over 131072 keys 97 -> 92 us; no
-          // different for 128 dims)
+          // (a wave at its products before one at its maxima: 1.1B-like, 64 rows over 131072 keys 97 -> 92 us, four
+          // runs of each; 128 dims, 128 rows: 112 to 119 us with it and without)
           if (HD < 128) __builtin_amdgcn_s_setprio(1);
           scores(next);  // (past the last chunk: of zeros, unused)
           exponentials(p);
