@@ -89,6 +89,14 @@ __device__ __forceinline__ double inv_sqrt(double m) {
   return isinf(m) ? 0.0 : y * (1.5 - 0.5 * m * y * y);
 }
 
+// Between LDS stores of a wave's lanes and loads of them by others: a wave's LDS operations take place
+// in the order they are issued in, and this keeps the compiler from another.
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // x of the lane `far` further (the low half of a pair of halves) or nearer: inside a row of 16 lanes
 // without LDS where far is a power of two.
 template <int CTRL, int BANKS = 15>
@@ -311,6 +319,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
             turned[wave][8 * lane + (e ^ (lane & 7))] = y;
           }
         }
+        lanes_meet();
         // (out through LDS, so that lanes store the dims' pieces side by side: 16 of them are 256 bytes)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -319,6 +328,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
             *(u32x4*)(k_block<uint16_t>(a.f8.ring, a.layer, b, head) + KvIndex<uint16_t>::v(p0, at % HD, HD, window)) =
                 turned[wave][(at & ~7) + ((at & 7) ^ (at >> 3 & 7))];
         }
+        lanes_meet();  // (before the next unit's)
       } else if (g < G) {
         uint16_t* dst = k_block<uint16_t>(a.f8.ring, a.layer, b, g) + KvIndex<uint16_t>::v(p0, d0, HD, window);
         for (int t = 0; t < T; ++t) {
