@@ -10,7 +10,8 @@
 // The prefix's codes are read once for 16 to 64 rows of a kv head, not once a sequence.
 //
 //  prefix: float32 queries, or bf16 ones of at most 16 rows a kv head: attn8_kernel; bf16: wide_kernel;
-//  own texts: at most 64 rows, not long: own_kernel; more bf16 rows: wide_kernel; else attn8_kernel.
+//  own texts: at most 64 rows, not long: own_kernel; more than 16 bf16 rows that fill the card or are short: wide_kernel
+//  (see wide_takes); else attn8_kernel.
 //
 // Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
 // 32 us (two streams, 17 and 16 us, 3.9 and 3.4 TB/s), 128 rows over 16384 and up to 256 own 91 us (the prefix 50 us,
@@ -353,8 +354,8 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
   }
 }
 
-// Waves of a unit: a wave a unit where the card is full of them, else as many as fill it; 0:
-// attn8_kernel, whose units are split over workgroups.  That is faster from 32 chunks a wave on where the card is full
+// Waves of a unit: a wave a unit where the card is full of them, else as many as fill it; 0: another kernel,
+// attn8_kernel but for many bf16 rows (see wide_takes), whose units are split over workgroups.  That is faster from 32 chunks a wave on where the card is full
 // (7B-like, 32 sequences: over 1000 own keys 52 us, 60 there; over 2000 108 and 100), from the fewer the emptier it is
 // (one sequence: over 1000 14 and 16, over 2000 18 and 17; 1.1B-like, 16: over 2000 15 and 18, over 4000 22 both).
 int own_waves(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
@@ -845,9 +846,17 @@ Plan wide_plan(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, in
   const int nq = rps * (n_heads / n_kv_heads), rows = 16 * wide_tiles(head_dim);
   const long slots = 2L * device_compute_units(), nb = (max_ctx + kF8Sub - 1) / kF8Sub;
   // A wave's own rows: a prefix's where they fill the card without a cut of its keys (8 x 512 rows over 2000
-  // keys 223 us, 245 else; 6 x 170 rows over 3500, half of that, 99 us, 95 else); own texts, short
-  // and triangular, from an eighth of it on (6 x 170 rows: 115 -> 95 us in all).
-  p.line = (long)n_kv_heads * batch * ((nq + 4 * rows - 1) / (4 * rows)) >= (prefix ? slots : slots / 8);
+  // keys 223 us, 245 else; 6 x 170 rows over 3500, half of that, 99 us, 95 else).  Own texts', whose keys are never cut:
+  // where tiles full of rows would fill the card and the texts have at most 32 chunks (7B-like, four waves a tile's keys
+  // and rows of their own: 8 x 70 rows over 500 keys 32 and 26 us, over 2000 49 and 58; 8 x 40, half as many, over 250
+  // 16 and 19), or the waves that have rows are three quarters of the card's and of their workgroups' (64 x 100 rows of
+  // 4 kv heads of 32 dims, 4 query heads each, over 2000 keys 76 and 62; 32 x 70 of 7B-like heads 193 and 178; 64
+  // dims: 64 x 65 of 1.1B-like heads over 4000 209 and 251, its registers spill).
+  const long groups = (long)n_kv_heads * batch, at_once = groups * ((nq + 4 * rows - 1) / (4 * rows));
+  const long live = groups * ((nq + rows - 1) / rows);
+  p.line = prefix ? at_once >= slots
+                  : groups * nq >= slots * rows &&
+                        (nb <= 32 || (head_dim != 64 && live >= 3 * slots && live >= 3 * at_once));
   p.n_tiles = (nq + (p.line ? 4 : 1) * rows - 1) / ((p.line ? 4 : 1) * rows);
   const long units = (long)n_kv_heads * p.n_tiles * batch, all = prefix ? std::max(1L, slots / units) : 1;
   const long per = std::max({(nb + all - 1) / all, (nb + kPartsMax8 - 1) / kPartsMax8, 4L});
@@ -855,6 +864,19 @@ Plan wide_plan(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, in
   p.nwg = (int)((nb + p.per - 1) / p.per);
   p.parts = (int)std::min<long>({nb, all, (long)kPartsMax8});
   return p;
+}
+
+// Whether own texts of bf16 rows are wide_kernel's, which is faster at full tiles but does not cut keys, or attn8_kernel's:
+// where tiles full of rows would fill a seventh of the card (wide_kernel and attn8_kernel, us: 7B-like, 2 x 40 rows over
+// 8000 keys 56 and 72, 32 x 40 over 16000 776 and 2094; 1.1B-like, 16 x 9 over 8000 60 and 53, 16 x 3 56 and 26), or,
+// more than 64 rows, at most 128 chunks (4 x 20 rows of 1.1B-like heads: over 2000 keys 20 and 25, 4000 30 and 26, 8000
+// 55 and 33; one sequence of 70 7B-like: 4000 33 and 39, 16000 99 and 81).  One sequence of 5 rows, 1.1B-like, over
+// 8000 keys: 47 and 13.
+bool wide_takes(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
+  const int nq = rps * (n_heads / n_kv_heads), nb = (max_ctx + kF8Sub - 1) / kF8Sub;
+  if (!is_wide(nq)) return false;
+  const int64_t slots = 2L * device_compute_units();
+  return 7 * (int64_t)n_kv_heads * batch * nq >= slots * 16 * wide_tiles(head_dim) || (nq > 64 && nb <= 128);
 }
 
 template <class X>
@@ -908,9 +930,10 @@ hipError_t launch_typed(AttnArgs own, const SharedAttn& sh, hipStream_t s) {
   const int nw = own_waves(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
   if (nw > 0) return launch_own<T>(own, parts, nw, s);
   if constexpr (sizeof(T) == 2) {
-    const Plan p = wide_plan(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx, false);
-    if (is_wide(own.rps * (own.n_heads / own.n_kv_heads)) && own.max_ctx <= 8192)
+    if (wide_takes(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx)) {
+      const Plan p = wide_plan(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx, false);
       return launch_wide(own, p, B, OwnPass<T>{parts}, s);
+    }
   }
   const Plan p = plan_of(own.rps, B, own.n_heads, own.n_kv_heads, own.head_dim, own.max_ctx);
   if (p.parts > own.n_split) return hipErrorInvalidValue;
