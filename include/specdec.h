@@ -379,8 +379,8 @@ SPECDEC_API specdec_status specdec_rope_init(specdec_rope* rope, int32_t head_di
  * no heads).  Position of row r: offset + positions[r] (device, [batch * n]), or,
  * positions == NULL, offset + i.
  * An output may be its own input (same address, stride and type); otherwise no
- * output may overlap an input or the other output, but for rows of one stride
- * that lie between each other's.
+ * output may overlap an input (the positions and gains too) or the other output,
+ * but for rows of one stride that lie between each other's.
  * Asynchronous, no workspace.  Errors: INVALID_ARG, SHAPE (head_dim, rotary_dim;
  * batch * n past 2^25 rows), HIP. */
 SPECDEC_API specdec_status specdec_rope_apply(const specdec_rope* rope, int32_t batch, int32_t n, int32_t n_heads,

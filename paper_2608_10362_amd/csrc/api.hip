@@ -297,6 +297,15 @@ bool rows_overlap(const void* a, int64_t ld_a, int64_t bytes_a, const void* b, i
   return at < bytes_a || at + bytes_b > ld_a;
 }
 
+// Whether `bytes` at p share memory with some of n rows of `row` bytes at a, ld (row at least) apart.
+bool block_overlaps(const void* p, int64_t bytes, const void* a, int64_t ld, int64_t row, int64_t n) {
+  if (!p) return false;
+  const int64_t at = (intptr_t)p - (intptr_t)a;  // (of the block, from the first row on)
+  if (at + bytes <= 0 || at >= (n - 1) * ld + row) return false;
+  const int64_t r = at < 0 ? 0 : at / ld;
+  return at - r * ld < row || (r + 1 < n && at + bytes > (r + 1) * ld);
+}
+
 specdec_status check_rope(const specdec_rope* r) {
   if (!r || (r->gain_dtype != SPECDEC_F32 && r->gain_dtype != SPECDEC_BF16) || !(r->eps >= 0.f) ||
       (r->interleaved != 0 && r->interleaved != 1) || r->head_dim <= 0 || r->rotary_dim < 0)
@@ -305,6 +314,14 @@ specdec_status check_rope(const specdec_rope* r) {
       r->rotary_dim > r->head_dim)
     return SPECDEC_ERR_SHAPE;
   return SPECDEC_OK;
+}
+
+// Whether a rotation's output rows lie over what every row reads: positions, gains.
+bool over_shared_inputs(const specdec_rope* r, const int32_t* positions, const void* out, int64_t ld, int64_t row,
+                        int64_t n) {
+  const int64_t gain = (int64_t)r->head_dim * elem_bytes(r->gain_dtype);
+  return block_overlaps(positions, 4 * n, out, ld, row, n) || block_overlaps(r->q_gain, gain, out, ld, row, n) ||
+         block_overlaps(r->k_gain, gain, out, ld, row, n);
 }
 
 bool is_float_type(int dtype) { return dtype == SPECDEC_F32 || dtype == SPECDEC_BF16; }
@@ -964,6 +981,8 @@ specdec_status specdec_rope_apply(const specdec_rope* rope, int32_t batch, int32
           overlap(ins[i], outs[o]))
         return SPECDEC_ERR_INVALID_ARG;
   if (overlap(outs[0], outs[1])) return SPECDEC_ERR_INVALID_ARG;
+  for (const Rows& o : outs)
+    if (o.at && over_shared_inputs(rope, positions, o.at, o.ld, o.bytes, rows)) return SPECDEC_ERR_INVALID_ARG;
   RopeArgs a = rope_args(rope, n, n_heads, n_kv_heads, q, ld_q, k, ld_k, positions, offset, q_out, ld_qo);
   a.k_out = k_out;
   a.ld_ko = ld_ko;
@@ -990,7 +1009,8 @@ specdec_status specdec_rope_append(specdec_kv* kv, int32_t layer, const specdec_
   const bool in_place = q_out == q && ld_q == wq && dtype == out_dtype;
   if ((!in_place && rows_overlap(q, in * ld_q, in * wq, q_out, out * wq, out * wq, rows)) ||
       rows_overlap(k, in * ld_k, in * wk, q_out, out * wq, out * wq, rows) ||
-      rows_overlap(v, in * ld_v, in * wk, q_out, out * wq, out * wq, rows))
+      rows_overlap(v, in * ld_v, in * wk, q_out, out * wq, out * wq, rows) ||
+      over_shared_inputs(rope, positions, q_out, out * wq, out * wq, rows))
     return SPECDEC_ERR_INVALID_ARG;
   if (kv->len_upper + n > kv->capacity) return SPECDEC_ERR_KV_CAPACITY;
   RopeArgs a = rope_args(rope, n, n_heads, kv->n_kv_heads, q, ld_q, k, ld_k, positions, offset, q_out, wq);
