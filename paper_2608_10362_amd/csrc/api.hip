@@ -284,6 +284,10 @@ specdec_status check_attention(const specdec_kv* kv, int n_heads, int n) {
   return SPECDEC_OK;
 }
 
+// Whether n rows that are ld entries of 4 bytes at most apart fit an address space of 2^56 bytes: what
+// strides are checked for before their bytes are reckoned in 64 bits.
+bool stride_fits(int64_t ld, int64_t n) { return ld <= ((int64_t)1 << 54) / n; }
+
 // Whether n rows of `bytes_a` at a (stride ld_a, in bytes too) and as many of `bytes_b` at b may
 // share memory: by their extents, but for rows of one stride that lie between each
 // other's (two slots of one buffer).
@@ -965,6 +969,8 @@ specdec_status specdec_rope_apply(const specdec_rope* rope, int32_t batch, int32
   const int64_t wq = (int64_t)n_heads * rope->head_dim, wk = (int64_t)n_kv_heads * rope->head_dim;
   if ((q && (ld_q < wq || ld_qo < wq)) || (k && (ld_k < wk || ld_ko < wk))) return SPECDEC_ERR_INVALID_ARG;
   if (!rope_fits(batch, n, false) || wq + wk > 1 << 24) return SPECDEC_ERR_SHAPE;
+  for (int64_t ld : {q ? ld_q : 0, q ? ld_qo : 0, k ? ld_k : 0, k ? ld_ko : 0})
+    if (!stride_fits(ld, (int64_t)batch * n)) return SPECDEC_ERR_INVALID_ARG;
   const int64_t in = elem_bytes(dtype), out = elem_bytes(out_dtype), rows = (int64_t)batch * n;
   struct Rows {
     const void* at;
@@ -1005,6 +1011,8 @@ specdec_status specdec_rope_append(specdec_kv* kv, int32_t layer, const specdec_
       !rope_fits(kv->batch, n, true) || wq > 1 << 24)
     return SPECDEC_ERR_SHAPE;
   if (ld_q < wq || ld_k < wk || ld_v < wk) return SPECDEC_ERR_INVALID_ARG;
+  for (int64_t ld : {ld_q, ld_k, ld_v})
+    if (!stride_fits(ld, (int64_t)kv->batch * n)) return SPECDEC_ERR_INVALID_ARG;
   const int64_t in = elem_bytes(dtype), out = elem_bytes(out_dtype), rows = (int64_t)kv->batch * n;
   const bool in_place = q_out == q && ld_q == wq && dtype == out_dtype;
   if ((!in_place && rows_overlap(q, in * ld_q, in * wq, q_out, out * wq, out * wq, rows)) ||
@@ -1405,6 +1413,8 @@ specdec_status specdec_sample_logits(int32_t batch, int32_t rows, int32_t vocab,
   if (!logits || ld < vocab || (!probs && !out) || (probs && ld_probs < vocab) || (out && ld_out < 1) ||
       misaligned8(step_dev) || purpose < 0 || purpose > 0xffff || index < 0 || index > 0xffff - (rows - 1) ||
       !workspace || (uintptr_t)workspace % kAlign || workspace_bytes < rules_scratch_bytes(batch * rows, vocab))
+    return SPECDEC_ERR_INVALID_ARG;
+  if (!stride_fits(ld, (int64_t)batch * rows) || (probs && !stride_fits(ld_probs, (int64_t)batch * rows)))
     return SPECDEC_ERR_INVALID_ARG;
   // (the draw reads logits again after other workgroups have stored probabilities)
   if (probs && rows_overlap(logits, 4 * ld, 4 * (int64_t)vocab, probs, 4 * ld_probs, 4 * (int64_t)vocab,
