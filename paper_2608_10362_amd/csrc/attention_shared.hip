@@ -62,7 +62,8 @@ __device__ __forceinline__ void split_parts(const float (&v)[8], bf16x8 (&part)[
 // Waves of a SIMD: what the registers allow (128 dims: outputs, codes, a ring's sub-chunk, queries).
 __host__ __device__ constexpr int own_resident(int head_dim) { return head_dim == 128 ? 2 : 3; }
 
-template <int HD, typename T, int NW>
+// ONCE: a sequence's codes are read by one unit.
+template <int HD, typename T, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs a, SharedParts pre, int n_tiles) {
   constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, SP = steps_of(HD), OS = HD + 4;
   constexpr int NQ = OwnParts<T>::kQ, NP = OwnParts<T>::kP;
@@ -92,9 +93,11 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
   const int k_end = max(1, min(most, (len + rps - 1) / chunk_of(HD) + 1));
   const int j_sealed = min(k_end, sealed);
 
-  // Codes: loads past the sealed ones read nothing.  (Of large batches, one unit's alone: past the caches; 64 rows of
-  // 7B-like heads over 400 to 500 own keys 56 -> 49 us; 16 over 64 to 700, four waves a unit, 32 -> 34 us.)
-  constexpr int kCodes = NW == 1 ? kNonTemporal : 0;
+  // Codes: loads past the sealed ones read nothing.  (Of large batches, where one unit reads them: past the caches; 64
+  // rows of 7B-like heads over 400 to 500 own keys 56 -> 49 us; 16 over 64 to 700, four waves a unit, 32 -> 34 us.  Where
+  // units of several tiles read them, not: 256 x 7 rows of 1.1B-like heads, four tiles, over 550 to 600 48 and 36 us;
+  // 256 x 4 of 64 heads of 128 over 8 kv heads, two tiles, 68 and 71.)
+  constexpr int kCodes = NW == 1 && ONCE ? kNonTemporal : 0;
   const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.f8.code_base(a.layer, b, g), (uint32_t)j_sealed * SP * 2 * kF8Sub * HD);
   const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.f8.scale_base(a.layer, b, g), (uint32_t)((j_sealed * SP + 1) & ~1) * 4);
   u32x4 kc[SP][FS], vc[SP][FS];
@@ -374,13 +377,16 @@ template <typename T>
 hipError_t launch_own(const AttnArgs& a, const SharedParts& pre, int nw, hipStream_t s) {
   const int nq = a.rps * (a.n_heads / a.n_kv_heads), n_tiles = (nq + 15) / 16;
   const dim3 grid((unsigned)(a.M / a.rps) * a.n_kv_heads * n_tiles);
-#define SD_OWN(HD, NW) hipLaunchKernelGGL((own_kernel<HD, T, NW>), grid, dim3(64 * NW), 0, s, a, pre, n_tiles)
-#define SD_OWN_HD(HD)                  \
-  switch (nw) {                        \
-    case 1: SD_OWN(HD, 1); break;      \
-    case 2: SD_OWN(HD, 2); break;      \
-    case 4: SD_OWN(HD, 4); break;      \
-    default: SD_OWN(HD, 8); break;     \
+#define SD_OWN(HD, NW, ONCE) hipLaunchKernelGGL((own_kernel<HD, T, NW, ONCE>), grid, dim3(64 * NW), 0, s, a, pre, n_tiles)
+#define SD_OWN_HD(HD)                          \
+  switch (nw) {                                \
+    case 1:                                    \
+      if (n_tiles == 1) SD_OWN(HD, 1, true);   \
+      else SD_OWN(HD, 1, false);               \
+      break;                                   \
+    case 2: SD_OWN(HD, 2, false); break;       \
+    case 4: SD_OWN(HD, 4, false); break;       \
+    default: SD_OWN(HD, 8, false); break;      \
   }
   switch (a.head_dim) {
     case 32: SD_OWN_HD(32) break;
