@@ -326,10 +326,11 @@ SPECDEC_API specdec_status specdec_attention(const specdec_kv* kv, int32_t layer
  * read once for many rows instead of once a sequence.  The prefix is only read:
  * any number of calls may use one at once, on any streams.
  * dtype: the type of q and out: SPECDEC_F32, as precise as specdec_attention, or
- * SPECDEC_BF16: where a kv head has more than 16 rows, probabilities enter their
- * products as one fp16 value (off by 2^-11), and out is rounded once; about 1.6 times the
- * speed there (q k^T itself, before the division by sqrt(head_dim), has to be inside
- * float32's range).  Everything else as for specdec_attention.
+ * SPECDEC_BF16: where a kv head has more than 16 rows, probabilities may enter their
+ * products as one fp16 value (off by 2^-11), and out is rounded once; 1.4 to 1.9 times
+ * the speed there over long prefixes (q k^T itself, before the division by
+ * sqrt(head_dim), has to be inside float32's range).  Everything else as for
+ * specdec_attention.
  * workspace: specdec_attention_shared_workspace_bytes bytes (0 for arguments the
  * call rejects).
  * Graph capture: the prefix's part is sized from prefix->len_upper.

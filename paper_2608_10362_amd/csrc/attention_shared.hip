@@ -16,7 +16,7 @@
 // Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
 // 32 us (two streams, 17 and 16 us, 3.9 and 3.4 TB/s), 128 rows over 16384 and up to 256 own 91 us (the prefix 50 us,
 // 690 TFLOP/s, own texts 45), 6 x 170 rows over 3500 93 us (645 TFLOP/s; the prefix 82, 710), 16 x 5 float32 rows over
-// 4001 and up to 512 36 us (25 and 14).  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553
+// 4001 and up to 512 36 us (25 and 14), 6 x 170 over 3500 183.  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553
 // and 30 to 300 own keys 48 us (710 TFLOP/s), 2 float32 rows over 200 and 40 11 us (two launches of 5).
 #include <type_traits>
 
@@ -424,7 +424,8 @@ __device__ __forceinline__ float max_of(const float (&p)[8]) {
 
 // KW: waves that take turns at a unit's chunks (the unit is the workgroup's, its waves are merged at
 // the end), or 1: each wave has 16 RT rows of its own and all of its unit's keys, so nothing is
-// merged, and the codes that four waves read at about the same time come from one cache.
+// merged, and the codes that four waves read at about the same time come from one cache.  (Own texts' form of it spills
+// 49 registers with 64 dims, 28 with 128, outside of the loop over codes whose scales are in range.)
 template <int HD, int RT, int KW, class X>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, int n_tiles, int parts, int per, X x) {
   constexpr int KST = HD / 32, DT = HD / 16, FS = HD / 32, OS = HD + 4, NW = KW;

@@ -13,16 +13,17 @@
 // 64 bits, where a far position keeps its fraction, the functions in 32) and keeps them in
 // LDS.  Squares are summed in 64 bits and the factor 1 / sqrt is applied there, before gain and rotation: no
 // float32 input overflows or vanishes on the way, and a head's bits depend on the head alone.  (Sums in 32 bits, with
-// these beside them for heads that they do not hold: 57.4 us in place of 58.5, 8189 rows of 64 heads of 128; into the
-// cache, 2048 rows, 31.7 and 33.1.)
+// these beside them for heads that they do not hold, took 1.1 us less of 8189 rows' 60, 1.4 less of 2048 rows' 33 into
+// the cache.)
 //
 // The 8 rows are 8 positions of one sequence from a multiple of 8 on: a lane then holds a
 // whole piece of V's operand order (8 positions of a dim, 16 bytes), turned in registers,
 // and K's pieces of neighbouring positions leave from one CU.
 //
-// Measured.  7B-like (32 + 32 heads of 128), bf16: 8189 rows 59 us, 4.5 TB/s (a copy of as many bytes: 50); one row 3.9 us
-// (10 with the host's call).  Into the cache, 2048 rows 32 us, 100 MB: K and V leave in pieces of 16 bytes, 64 and 256 bytes
-// of them side by side (37 us with the lanes' own order).  1.1B-like, 96 rows 5 us.
+// Measured.  7B-like (32 + 32 heads of 128), bf16: 8189 rows 60 us, 4.5 TB/s (a copy of as many bytes: 50), float32 111,
+// 4.8 TB/s; one row 4.1 us (10 with the host's call).  Into the cache, 2048 rows 33 us, 100 MB: K and V leave in pieces
+// of 16 bytes, 64 and 256 bytes of them side by side (5 us more with the lanes' own order); float32 40.  1.1B-like, 96
+// rows 5 us.
 #include <algorithm>
 #include <type_traits>
 
