@@ -15,9 +15,9 @@
 //
 // Measured (both launches).  7B-like (32 kv heads of 128): 16 bf16 rows over 8192 shared and 64 to 700 own keys
 // 32 us (two streams, 17 and 16 us, 3.9 and 3.4 TB/s), 128 rows over 16384 and up to 256 own 91 us (the prefix 50 us,
-// 690 TFLOP/s, own texts 45), 6 x 170 rows over 3500 93 us (645 TFLOP/s; the prefix 82, 710), 16 x 5 float32 rows over
-// 4001 and up to 512 36 us (25 and 14), 6 x 170 over 3500 183.  1.1B-like (4 kv heads of 64, 8 query heads each): 64 bf16 rows over 65553
-// and 30 to 300 own keys 48 us (710 TFLOP/s), 2 float32 rows over 200 and 40 11 us (two launches of 5).
+// 690 TFLOP/s, own texts 45), 6 x 170 rows over 3500 92 us (650 TFLOP/s; the prefix 80 to 82, 710), 16 x 5 float32 rows
+// over 4001 and up to 512 36 us (25 and 14), 6 x 170 over 3500 183.  1.1B-like (4 kv heads of 64, 8 query heads each): 64
+// bf16 rows over 65553 and 30 to 300 own keys 48 us (710 TFLOP/s), 2 float32 rows over 200 and 40 11 us (two launches of 5).
 #include <type_traits>
 
 #include "attention8.h"
@@ -357,10 +357,11 @@ __global__ __launch_bounds__(64 * NW, own_resident(HD)) void own_kernel(AttnArgs
   }
 }
 
-// Waves of a unit: a wave a unit where the card is full of them, else as many as fill it; 0: another kernel,
-// attn8_kernel but for many bf16 rows (see wide_takes), whose units are split over workgroups.  That is faster from 32 chunks a wave on where the card is full
-// (7B-like, 32 sequences: over 1000 own keys 52 us, 60 there; over 2000 108 and 100), from the fewer the emptier it is
-// (one sequence: over 1000 14 and 16, over 2000 18 and 17; 1.1B-like, 16: over 2000 15 and 18, over 4000 22 both).
+// Waves of a unit: a wave a unit where the card is full of them, else as many as fill it; 0: another kernel, for many
+// bf16 rows the one that wide_takes says, else attn8_kernel, whose units are split over workgroups.  That is faster from
+// 32 chunks a wave on where the card is full (7B-like, 32 sequences: over 1000 own keys 52 us, 60 there; over 2000 108 and
+// 100), from the fewer the emptier it is (one sequence: over 1000 14 and 16, over 2000 18 and 17; 1.1B-like, 16: over 2000
+// 15 and 18, over 4000 22 both).
 int own_waves(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
   const int nq = rps * (n_heads / n_kv_heads);
   if (nq > 64) return 0;
@@ -878,7 +879,7 @@ Plan wide_plan(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, in
 // 8000 keys 56 and 72, 32 x 40 over 16000 776 and 2094; 1.1B-like, 16 x 9 over 8000 60 and 53, 16 x 3 56 and 26), or,
 // more than 64 rows, at most 128 chunks (4 x 20 rows of 1.1B-like heads: over 2000 keys 20 and 25, 4000 30 and 26, 8000
 // 55 and 33; one sequence of 70 7B-like: 4000 33 and 39, 16000 99 and 81).  One sequence of 5 rows, 1.1B-like, over
-// 8000 keys: 47 and 13.
+// 8000 keys: 47 and 13.  The choice is up to a quarter slower than the other near its borders.
 bool wide_takes(int rps, int batch, int n_heads, int n_kv_heads, int head_dim, int max_ctx) {
   const int nq = rps * (n_heads / n_kv_heads), nb = (max_ctx + kF8Sub - 1) / kF8Sub;
   if (!is_wide(nq)) return false;
