@@ -65,6 +65,39 @@ def test_maxima_that_rise_from_chunk_to_chunk(hd, H, G, B, n, L, P):
     _check(_attend(prefix, kv, q), q, pk, pv, kvs, [L] * B)
 
 
+@pytest.mark.parametrize("hd,H,G,n", [(64, 32, 4, 5), (128, 8, 8, 70), (64, 32, 4, 9)])
+def test_replays_at_other_lengths(hd, H, G, n):
+    """Captured for texts of 6000 keys, replayed at shorter ones; two graphs of one workspace in turn."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(hd + n)
+    prefix, pk, pv = _prefix(rng, hd, G, 300, n_layers=1)
+    cap = 6144
+    kv = [_cache(_shape(hd, H, G, 1), 2, cap, 256) for _ in range(2)]
+    q = [_queries(rng, (2, n, H, hd), "bf16") for _ in kv]
+    out = [torch.empty_like(x) for x in q]
+    ws = binding.shared_attention_workspace(prefix, kv[0], H, n, torch.bfloat16)
+    ws.fill_(255)
+    graphs = []
+    for c, x, o in zip(kv, q, out):
+        c.kv.len_upper = 6000
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            binding.specdec_attention_shared(prefix, c, 0, x, o, ws, 1)
+        graphs.append(g)
+    for lens in ([6000, 64], [10, 4100], [0, 2500], [5900, 5999]):
+        held = [_fill(c, rng, lens, n, G, hd) for c in kv]
+        log(f"replays hd={hd} n={n} lengths {lens}")
+        for _ in range(2):
+            for o in out:
+                o.fill_(float("nan"))
+            for g in graphs:
+                g.replay()
+            torch.cuda.synchronize()
+            for i, c in enumerate(kv):
+                _check(out[i], q[i], pk, pv, held[i], lens)
+                assert c.read_state()["status"] == 0
+
+
 def _best_us(hd, H, G, B, n, L, dtype):
     """The fastest of six rounds of calls, microseconds (sums and codes of any values: the caches are filled with one row)."""
     torch = torch_cuda()
